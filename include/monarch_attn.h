@@ -383,6 +383,151 @@ int monarch_attn_set_path(int32_t path);
 int monarch_attn_timing_enable(int32_t flag);
 int32_t monarch_attn_timing_read(float *ms, int32_t *kind, int32_t cap);
 
+/*
+ * ---- Exact attention over packed sequences and paged caches ----
+ *
+ * Exact softmax attention (eq. softmax_attention) in the form in which a
+ * language model trains and serves with it, for the layers of a converted
+ * model that keep it.  B sequences lie one after another in the rows of one
+ * tensor: sequence i has the rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1
+ * (device int32, B + 1 of them, not decreasing; each is clamped to 0..total).
+ * Rows before the first and behind the last sequence are neither read nor
+ * written.  Sequences may be empty.
+ *
+ * Hq query heads share Hkv key heads in groups of G = Hq / Hkv: query head h
+ * reads key head h / G.  The scores are scaled by s = 1/sqrt(d).  With causal
+ * != 0 a row sees the keys up to its own position only; otherwise all keys of
+ * its sequence.  A row that sees no key gets a zero output and lse -infinity.
+ * Keys that a row does not see have no effect on its output, whatever they
+ * hold (infinities and NaN among them).
+ *
+ * d: a multiple of 8 (bf16, fp16) or 4 (fp32) up to 128.  Hq * d and the row
+ * strides are at most 2^20 elements, total * G and B below 2^31, else
+ * MA_EUNSUPPORTED.
+ * Tensors are DEVICE pointers, 16-byte aligned; integers 4- (slots: 8-) byte
+ * aligned.  No output overlaps another one or an input (inputs may overlap:
+ * q, k and v can be parts of one tensor).  Statistics, sums and gradients are
+ * held in fp32; in 16-bit types the weights (relative to a row's running
+ * maximum), and in the gradient the weights and dS, are rounded to the element
+ * type where they enter the matrix instructions.  Every sum has a fixed
+ * order: the same call gives the same bits.
+ * Errors, asynchrony, per-(device, stream) workspace and HIP graph capture
+ * are those of monarch_attn_fwd.
+ */
+
+/*
+ * monarch_attn_exact_packed_fwd -- the forward pass over whole sequences.
+ *
+ * q          : [total, Hq, d], rows ldq elements apart (heads of a row are
+ *              adjacent); k, v: [total, Hkv, d], rows ldk, ldv elements apart.
+ *              Strides are multiples of 16 bytes.
+ * out        : [total, Hq, d], contiguous.
+ * lse        : NULL, or [Hq, total] floats: every row's logsumexp of its
+ *              scaled scores (natural log), which the gradient needs.
+ * rest       : NULL, or (16-bit types) a tensor like out: what rounding out
+ *              to the element type leaves of it.  With it, rows of few keys
+ *              are computed with weights of twice the bits.  The gradient of
+ *              such rows is a small difference of large terms; with out and
+ *              rest it is as exact there as elsewhere.
+ * No workspace.
+ */
+int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
+                                  const int32_t *cu_seqlens, int64_t B, int64_t total, int64_t Hq, int64_t Hkv,
+                                  int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal, int32_t dtype,
+                                  void *stream);
+
+/*
+ * monarch_attn_exact_packed_bwd -- its gradient: from out, lse and rest (or
+ * NULL) of the forward pass and dout = dL/dout, dq = dL/dq, dk = dL/dk, dv = dL/dv, those
+ * of a key head summed over its query heads.
+ *
+ * out, dout, dq : [total, Hq, d], contiguous; dk, dv: [total, Hkv, d],
+ *                 contiguous.  Rows of no sequence are left as they were.
+ * In fp16, dS is formed relative to the largest norms of the rows of dout and
+ * v, so gradients of any scale keep their precision.  Values of a sequence
+ * that are not finite can reach all gradients of that sequence.
+ * Workspace: 8 bytes a row and query head.
+ */
+int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,
+                                  const void *rest, const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_seqlens,
+                                  int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq,
+                                  int64_t ldk, int64_t ldv, int32_t causal, int32_t dtype, void *stream);
+
+/*
+ * monarch_attn_exact_paged_fwd -- the new tokens of every sequence (one, or a
+ * chunk) over the keys and values of its pages.
+ *
+ * q, out, lse : as in monarch_attn_exact_packed_fwd; sequence i's new tokens
+ *               are its rows by cu_seqlens, and are the last of its tokens.
+ * kv_lens     : [B] device int32, the tokens of sequence i in the cache, the
+ *               new ones among them (clamped to 0..blocks * page).  With
+ *               causal, new token r of n sees the first kv_lens[i] - n + r + 1
+ *               (none where that is not positive); otherwise all kv_lens[i].
+ * k_pages,    : [pages, Hkv, page, d], contiguous; page is a power of two from
+ * v_pages       8 to 4096.  Token t of sequence i lies in row t % page of page
+ *               block_table[i, t / page].
+ * block_table : [B, blocks] device int32, contiguous.  Entries past the last
+ *               token are not read.  A page number outside 0..pages - 1 leads
+ *               to no read: the rows that see a token on it become NaN.
+ * Calls with few rows and long contexts are split over the keys and joined by
+ * a second launch, from partial results in the workspace.
+ */
+int monarch_attn_exact_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out, float *lse,
+                                 const int32_t *cu_seqlens, const int32_t *kv_lens, const int32_t *block_table,
+                                 int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq,
+                                 int64_t pages, int64_t page, int64_t blocks, int32_t causal, int32_t dtype,
+                                 void *stream);
+
+/* Bits of monarch_attn_paged_plan's status. */
+#define MA_PLAN_NO_PAGES 1   /* more pages needed than are free               */
+#define MA_PLAN_TABLE_FULL 2 /* a request has more tokens than blocks * page   */
+#define MA_PLAN_BAD_LENGTH 4 /* a negative length (taken for zero)             */
+#define MA_PLAN_NO_SLOTS 8   /* more new tokens than capacity                  */
+
+#define MONARCH_ATTN_PLAN_MAX_B 8192
+
+/*
+ * monarch_attn_paged_plan -- the tables of a step from the lengths of its
+ * requests, on the GPU: request i has past[i] tokens in the cache and gets
+ * fresh[i] new ones.
+ *
+ * past, fresh : [B] device int32.  B <= MONARCH_ATTN_PLAN_MAX_B.
+ * ring        : [ring_len] device int32, page numbers; free_in: device int32
+ *               (first, count): the free pages are ring[(first + k) % ring_len],
+ *               k = 0..count - 1.  They are taken in order, request by
+ *               request; to give pages back, write them behind the last free
+ *               one and raise count.
+ * block_table : [B, blocks] device int32.  The entries of the pages that a
+ *               request needs beyond those of its past tokens are written, the
+ *               others left (and those of the past read).
+ * cu_seqlens  : [B + 1] device int32, written: row starts of the new tokens.
+ * kv_lens     : [B] device int32, written: past[i] + fresh[i].
+ * slots       : [capacity] device int64, written: page * page size + row of
+ *               every new token, in row order; -1 behind the last.
+ * free_out    : device int32 (first, count), written: what stays free.
+ * status      : device int32, written: 0, or bits MA_PLAN_*.  What could not
+ *               be served is marked: table entries and slots without a page
+ *               are -1, cu_seqlens ends at capacity and kv_lens at
+ *               blocks * page.
+ * Inputs and outputs must not overlap (free_out and free_in take turns).  One
+ * launch, no workspace; it runs for B or capacity zero too.
+ */
+int monarch_attn_paged_plan(const int32_t *past, const int32_t *fresh, const int32_t *ring, const int32_t *free_in,
+                            int32_t *block_table, int32_t *cu_seqlens, int32_t *kv_lens, int64_t *slots,
+                            int32_t *free_out, int32_t *status, int64_t B, int64_t ring_len, int64_t blocks,
+                            int64_t page, int64_t capacity, void *stream);
+
+/*
+ * monarch_attn_paged_write -- row r of k and v ([rows, Hkv, d], rows ldk, ldv
+ * elements apart) into slot slots[r] (device int64) of k_pages and v_pages
+ * (as in monarch_attn_exact_paged_fwd).  A slot outside the cache (-1) is
+ * skipped.  Slots must differ from each other; of two rows with one slot
+ * either may be found there, chunk by chunk of 16 bytes.
+ */
+int monarch_attn_paged_write(const void *k, const void *v, void *k_pages, void *v_pages, const int64_t *slots,
+                             int64_t rows, int64_t Hkv, int64_t d, int64_t ldk, int64_t ldv, int64_t pages,
+                             int64_t page, int32_t dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

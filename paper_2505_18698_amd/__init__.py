@@ -15,6 +15,11 @@ try:
         MAX_T_16BIT,
         MAX_T_16BIT_BWD,
         NOALLOC_SCRATCH_BYTES,
+        PLAN_BAD_LENGTH,
+        PLAN_MAX_B,
+        PLAN_NO_PAGES,
+        PLAN_NO_SLOTS,
+        PLAN_TABLE_FULL,
         MA_BF16,
         MA_EHIP,
         MA_EINVAL,
@@ -29,6 +34,7 @@ try:
         PATH_GROUPED,
         MonarchAttnError,
         dtype_code,
+        exact_attention_packed,
         fused_applies,
         grouped_applies,
         monarch_attention,
@@ -45,8 +51,13 @@ try:
         monarch_attn_fwd_prepad,
         monarch_attn_fwd_varlen,
         monarch_attn_exact_fwd,
+        monarch_attn_exact_packed_bwd,
+        monarch_attn_exact_packed_fwd,
+        monarch_attn_exact_paged_fwd,
         monarch_attn_fwd_raw,
         monarch_attn_last_error,
+        monarch_attn_paged_plan,
+        monarch_attn_paged_write,
         monarch_attn_release_workspace,
         monarch_attn_set_path,
         monarch_attn_timing_enable,

@@ -16,7 +16,8 @@ MA_OK, MA_EINVAL, MA_EUNSUPPORTED, MA_EHIP, MA_ENOMEM = 0, 1, 2, 3, 4
 STATUS_NAMES = {0: "MA_OK", 1: "MA_EINVAL", 2: "MA_EUNSUPPORTED", 3: "MA_EHIP", 4: "MA_ENOMEM"}
 KIND_NAMES = {0: "r_half_step", 1: "l_half_step", 2: "r_half_step_final", 3: "monarch_apply",
               4: "monarch_fused_head", 5: "objective_sum", 6: "exact_attention", 7: "l_bwd", 8: "r_bwd",
-              9: "monarch_fused_group"}
+              9: "monarch_fused_group", 10: "seq_attention", 11: "seq_join", 12: "seq_stats", 13: "seq_bwd_k",
+              14: "seq_bwd_q", 15: "paged_plan", 16: "paged_write"}
 PATH_AUTO, PATH_HALF_STEPS, PATH_FUSED, PATH_GROUPED = 0, 1, 2, 3
 
 # Every symbol declared in include/monarch_attn.h.
@@ -39,6 +40,11 @@ EXPORTS = (
     "monarch_attn_build_id",
     "monarch_attn_fwd_noalloc",
     "monarch_attn_fwd_prepad",
+    "monarch_attn_exact_packed_fwd",
+    "monarch_attn_exact_packed_bwd",
+    "monarch_attn_exact_paged_fwd",
+    "monarch_attn_paged_plan",
+    "monarch_attn_paged_write",
 )
 
 
@@ -89,6 +95,15 @@ def _load() -> ctypes.CDLL:
     lib.monarch_attn_fwd_prepad.restype = ctypes.c_int
     lib.monarch_attn_fwd_noalloc.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i32, i32, vp]
     lib.monarch_attn_fwd_noalloc.restype = ctypes.c_int
+    for name, argtypes in (
+        ("monarch_attn_exact_packed_fwd", [vp] * 7 + [i64] * 8 + [i32, i32, vp]),
+        ("monarch_attn_exact_packed_bwd", [vp] * 11 + [i64] * 8 + [i32, i32, vp]),
+        ("monarch_attn_exact_paged_fwd", [vp] * 8 + [i64] * 9 + [i32, i32, vp]),
+        ("monarch_attn_paged_plan", [vp] * 10 + [i64] * 5 + [vp]),
+        ("monarch_attn_paged_write", [vp] * 5 + [i64] * 7 + [i32, vp]),
+    ):
+        getattr(lib, name).argtypes = argtypes
+        getattr(lib, name).restype = ctypes.c_int
     lib.monarch_attn_build_id.argtypes = []
     lib.monarch_attn_build_id.restype = ctypes.c_char_p
     _check_provenance(lib)
@@ -148,7 +163,7 @@ class _Torch:
         import torch
 
         self.Tensor = torch.Tensor
-        self.int32, self.float32 = torch.int32, torch.float32
+        self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
         self.codes = {torch.float32: MA_F32, torch.bfloat16: MA_BF16, torch.float16: MA_F16}
         self.device = torch.cuda.device
         self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -397,6 +412,218 @@ def monarch_attention_autograd(q, k, v, m: int, b: int, T: int, lens=None):
     device tensor [B]) the batch is padded per sequence, as in
     monarch_attn_fwd_varlen."""
     return _autograd_function().apply(q, k, v, m, b, T, lens)
+
+
+# ---- exact attention over packed sequences and paged caches ----
+
+PLAN_NO_PAGES, PLAN_TABLE_FULL, PLAN_BAD_LENGTH, PLAN_NO_SLOTS = 1, 2, 4, 8  # MA_PLAN_*: bits of the plan's status
+PLAN_MAX_B = 8192  # MONARCH_ATTN_PLAN_MAX_B
+
+
+def _check_rows(name, t, like, like_name="q"):
+    """t: [rows, heads, d] on the device and of the dtype of `like`, the heads
+    of a row adjacent; rows may be further apart.  Returns the row stride."""
+    rt = _torch()
+    if not isinstance(t, rt.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dim() != 3 or t.stride(2) != 1 and t.shape[2] > 1 or t.stride(1) != t.shape[2] and t.shape[1] > 1:
+        raise ValueError(f"{name} must be a [rows, heads, d] tensor whose rows are contiguous")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must match {like_name} in dtype and device")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _check_like(name, t, shape, like, dtype=None):
+    """t: a contiguous device tensor of `shape` on the device of `like` (and of its dtype, or `dtype`)."""
+    rt = _torch()
+    if not isinstance(t, rt.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != like.device \
+            or t.dtype != (like.dtype if dtype is None else dtype):
+        raise ValueError(f"{name} must be a contiguous {dtype or like.dtype} tensor {list(shape)} on the device of the others")
+
+
+def _check_packed(q, k, v, cu_seqlens):
+    """Row strides and sizes of packed q [total, Hq, d], k and v [total, Hkv, d]."""
+    ldq, ldk, ldv = (_check_rows(name, t, q) for name, t in (("q", q), ("k", k), ("v", v)))
+    total, Hq, d = q.shape
+    if k.shape != v.shape or k.shape[0] != total or k.shape[2] != d:
+        raise ValueError("k and v must be [total, Hkv, d] tensors with the rows and head dimension of q")
+    if not isinstance(cu_seqlens, _torch().Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+        raise ValueError("cu_seqlens must be an int32 tensor [B + 1]")
+    _check_like("cu_seqlens", cu_seqlens, cu_seqlens.shape, q, _torch().int32)
+    return (cu_seqlens.shape[0] - 1, total, Hq, k.shape[1], d), (ldq, ldk, ldv)
+
+
+def monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal: bool = True, lse=None, rest=None, stream=None):
+    """Exact softmax attention over sequences that lie one after another:
+    q [total, Hq, d], k and v [total, Hkv, d] (rows may be strided, as in parts
+    of a joint projection), sequence i the rows cu_seqlens[i] to
+    cu_seqlens[i + 1] (int32 device tensor [B + 1]).  Writes the rows of the
+    sequences in out [total, Hq, d] and, with lse (float32 device tensor
+    [Hq, total]), every row's logsumexp; with rest (like out, 16-bit types) also
+    what rounding out leaves, for the gradient.  Returns (out, lse)."""
+    sizes, strides = _check_packed(q, k, v, cu_seqlens)
+    _check_like("out", out, q.shape, q)
+    if lse is not None:
+        _check_like("lse", lse, (q.shape[1], q.shape[0]), q, _torch().float32)
+    if rest is not None:
+        _check_like("rest", rest, q.shape, q)
+    _call(LIB.monarch_attn_exact_packed_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+          None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(), cu_seqlens.data_ptr(), *sizes, *strides, bool(causal),
+          dtype_code(q.dtype), _stream(q, stream) or None)
+    return out, lse
+
+
+def monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal: bool = True, rest=None,
+                                  stream=None):
+    """The gradient of monarch_attn_exact_packed_fwd from its out, lse and rest
+    (None: without) and dout = dL/dout, into dq [total, Hq, d], dk and dv [total, Hkv, d]
+    (contiguous; rows of no sequence are left).  Returns (dq, dk, dv)."""
+    sizes, strides = _check_packed(q, k, v, cu_seqlens)
+    for name, t in (("out", out), ("dout", dout), ("dq", dq)):
+        _check_like(name, t, q.shape, q)
+    for name, t in (("dk", dk), ("dv", dv)):
+        _check_like(name, t, k.shape, q)
+    if rest is not None:
+        _check_like("rest", rest, q.shape, q)
+    _check_like("lse", lse, (q.shape[1], q.shape[0]), q, _torch().float32)
+    _call(LIB.monarch_attn_exact_packed_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+          lse.data_ptr(), None if rest is None else rest.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_seqlens.data_ptr(), *sizes,
+          *strides, bool(causal), dtype_code(q.dtype), _stream(q, stream) or None)
+    return dq, dk, dv
+
+
+_PACKED_FN = None
+
+
+def _packed_function():
+    """torch.autograd.Function of monarch_attn_exact_packed_fwd and _bwd."""
+    global _PACKED_FN
+    if _PACKED_FN is None:
+        import torch
+
+        def rows(t):  # the kernels' layout: heads of a row adjacent, rows 16-byte aligned
+            n = t.element_size()
+            fits = t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.stride(0) * n % 16 == 0 \
+                and t.stride(0) >= t.shape[1] * t.shape[2] and t.data_ptr() % 16 == 0
+            return t if fits else t.contiguous()
+
+        class ExactAttentionPackedFn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, cu_seqlens, causal):
+                q, k, v = rows(q), rows(k), rows(v)
+                out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+                lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+                # (the gradient reads no row of no sequence: rest stays as it is there)
+                rest = torch.empty_like(out) if out.element_size() == 2 else None
+                monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest)
+                ctx.save_for_backward(q, k, v, out, lse, cu_seqlens, *(() if rest is None else (rest,)))
+                ctx.causal = causal
+                return out
+
+            @staticmethod
+            def backward(ctx, dout):
+                q, k, v, out, lse, cu_seqlens, *rest = ctx.saved_tensors
+                dq, dk, dv = (torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+                monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout.contiguous(), dq, dk, dv, cu_seqlens, ctx.causal,
+                                              *rest)
+                return dq, dk, dv, None, None
+
+        _PACKED_FN = ExactAttentionPackedFn
+    return _PACKED_FN
+
+
+def exact_attention_packed(q, k, v, cu_seqlens, causal: bool = True):
+    """Exact attention over packed sequences as a differentiable torch op (see
+    monarch_attn_exact_packed_fwd).  Rows of no sequence get zero output and
+    zero gradients."""
+    return _packed_function().apply(q, k, v, cu_seqlens, causal)
+
+
+def _check_cache(k_pages, v_pages):
+    """Sizes (pages, page) of a paged cache [pages, Hkv, page, d]."""
+    rt = _torch()
+    if not isinstance(k_pages, rt.Tensor) or not k_pages.is_cuda:
+        raise TypeError("k_pages must be a device tensor")
+    if k_pages.dim() != 4 or not k_pages.is_contiguous():
+        raise ValueError("k_pages must be a contiguous [pages, Hkv, page, d] tensor")
+    _check_like("v_pages", v_pages, k_pages.shape, k_pages)
+
+
+def monarch_attn_exact_paged_fwd(q, k_pages, v_pages, out, cu_seqlens, kv_lens, block_table, causal: bool = True,
+                                 lse=None, stream=None):
+    """Exact softmax attention of new tokens, q [total, Hq, d] packed by
+    cu_seqlens (int32 [B + 1]), over the cached ones: token t of sequence i in
+    row t % page of page block_table[i, t // page] (int32 [B, blocks]) of
+    k_pages and v_pages [pages, Hkv, page, d].  kv_lens (int32 [B]): tokens in
+    the cache, the new ones (its last) among them.  Writes out [total, Hq, d]
+    and, if given, lse (float32 [Hq, total]).  Returns (out, lse)."""
+    rt = _torch()
+    ldq = _check_rows("q", q, q)
+    _check_cache(k_pages, v_pages)
+    total, Hq, d = q.shape
+    pages, Hkv, page, dk = k_pages.shape
+    if dk != d or k_pages.dtype != q.dtype or k_pages.device != q.device:
+        raise ValueError("k_pages must match q in head dimension, dtype and device")
+    _check_like("out", out, q.shape, q)
+    if not isinstance(block_table, rt.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be an int32 tensor [B, blocks]")
+    B, blocks = block_table.shape
+    _check_like("block_table", block_table, (B, blocks), q, rt.int32)
+    _check_like("kv_lens", kv_lens, (B,), q, rt.int32)
+    _check_like("cu_seqlens", cu_seqlens, (B + 1,), q, rt.int32)
+    if lse is not None:
+        _check_like("lse", lse, (Hq, total), q, rt.float32)
+    _call(LIB.monarch_attn_exact_paged_fwd, q, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
+          None if lse is None else lse.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr(),
+          B, total, Hq, Hkv, d, ldq, pages, page, blocks, bool(causal), dtype_code(q.dtype), _stream(q, stream) or None)
+    return out, lse
+
+
+def monarch_attn_paged_plan(past, fresh, ring, free_in, block_table, cu_seqlens, kv_lens, slots, free_out, status,
+                            page: int, stream=None):
+    """The tables of a step on the GPU, from past[B] cached and fresh[B] new
+    tokens of every request: pages from the ring of free ones (`ring`, and
+    free_in = (first, count)) into block_table [B, blocks], row starts
+    cu_seqlens [B + 1], kv_lens [B], the slot of every new token in slots
+    (int64 [capacity], -1 behind the last), what stays free in free_out [2] and
+    0 or PLAN_* bits in status [1].  All int32 device tensors but slots."""
+    rt = _torch()
+    for name, t in (("past", past), ("fresh", fresh), ("ring", ring), ("slots", slots), ("block_table", block_table)):
+        if not isinstance(t, rt.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        if t.dim() != (2 if name == "block_table" else 1):
+            raise ValueError(f"{name} must have {2 if name == 'block_table' else 1} dimension(s)")
+    B, blocks = past.shape[0], block_table.shape[1]
+    for name, t, shape in (("past", past, (B,)), ("fresh", fresh, (B,)), ("ring", ring, ring.shape),
+                           ("free_in", free_in, (2,)), ("block_table", block_table, (B, blocks)),
+                           ("cu_seqlens", cu_seqlens, (B + 1,)), ("kv_lens", kv_lens, (B,)), ("free_out", free_out, (2,)),
+                           ("status", status, (1,))):
+        _check_like(name, t, shape, past, rt.int32)
+    _check_like("slots", slots, slots.shape, past, rt.int64)
+    _call(LIB.monarch_attn_paged_plan, past, past.data_ptr(), fresh.data_ptr(), ring.data_ptr(), free_in.data_ptr(),
+          block_table.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), free_out.data_ptr(),
+          status.data_ptr(), B, ring.shape[0], blocks, page, slots.shape[0], _stream(past, stream) or None)
+    return block_table, cu_seqlens, kv_lens, slots, free_out, status
+
+
+def monarch_attn_paged_write(k, v, k_pages, v_pages, slots, stream=None):
+    """Rows of k and v [rows, Hkv, d] (may be strided) into the slots (int64
+    [rows], all different; -1: nowhere) of k_pages and v_pages
+    [pages, Hkv, page, d].  Returns (k_pages, v_pages)."""
+    ldk, ldv = _check_rows("k", k, k, "k"), _check_rows("v", v, k, "k")
+    _check_cache(k_pages, v_pages)
+    rows, Hkv, d = k.shape
+    pages, heads, page, dk = k_pages.shape
+    if v.shape != k.shape:
+        raise ValueError("v must match k in shape")
+    if (heads, dk) != (Hkv, d) or k_pages.dtype != k.dtype or k_pages.device != k.device:
+        raise ValueError("k_pages must match k in heads, head dimension, dtype and device")
+    _check_like("slots", slots, (rows,), k, _torch().int64)
+    _call(LIB.monarch_attn_paged_write, k, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+          slots.data_ptr(), rows, Hkv, d, ldk, ldv, pages, page, dtype_code(k.dtype), _stream(k, stream) or None)
+    return k_pages, v_pages
 
 
 def monarch_attn_check(N: int, d: int, m: int, b: int, T: int, dtype: int) -> int:

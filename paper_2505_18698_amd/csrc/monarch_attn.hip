@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "host_common.hpp"
+#include "seq_host.hpp"
 
 namespace ma_host {
 
@@ -443,6 +444,42 @@ int backward(const void *q, const void *k, const void *v, const void *dout, void
 }
 
 }  // namespace
+
+// ---- what the exact attention over sequences (seq_abi.hip) shares of the above ----
+
+namespace ma_host {
+
+int begin_call(hipStream_t stream, CallScope &c)
+{
+    const int rc = current_device(c.dev, c.num_cus);
+    return rc != MA_OK ? rc : check_capture(stream, c.capturing);
+}
+
+int call_workspace(hipStream_t stream, size_t need, CallScope &c)
+{
+    return acquire_workspace(c.dev, stream, c.capturing, need, &c.ws, c.hold);
+}
+
+int run_launches(hipStream_t stream, int (*f)(Launcher &, void *), void *arg)
+{
+    std::unique_lock<std::mutex> tlock(g_timing_mutex);
+    Launcher L{stream, g_timing.enabled};
+    if (!L.timed) tlock.unlock();
+    (void)hipGetLastError();  // clear a stale error so the check below is ours
+    const int rc = f(L, arg);
+    if (L.timed) {
+        g_timing.nlaunch = L.n;
+        g_timing.ready = (rc == MA_OK && L.n > 0);
+    }
+    if (rc != MA_OK) return rc;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(MA_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return MA_OK;
+}
+
+bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb) { return overlaps(a, na, b, nb); }
+
+}  // namespace ma_host
 
 #ifndef MA_BUILD_ID
 #error "MA_BUILD_ID (the source hash) is defined by paper_2505_18698_amd/build.py"

@@ -1,0 +1,24 @@
+// Launches of the paged cache's plan and write.
+#include <algorithm>
+
+#include "paged.hpp"
+#include "seq_host.hpp"
+
+namespace ma_host {
+
+int run_paged_plan(Launcher &L, const ma::PagedPlan &p)
+{
+    // one workgroup per 1024 slots; more than 128 repeat the sums for less than they save
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(128, (p.capacity + 1023) / 1024));
+    return L.run(kPagedPlan, [&] { return launched([&] { ma::paged_plan<<<dim3(blocks), dim3(256), 0, L.stream>>>(p); }); });
+}
+
+int run_paged_write(Launcher &L, const ma::PagedWrite &p)
+{
+    // about four 16-byte chunks of K and of V a thread
+    const int chunks = p.Hkv * p.d * p.size / 16, per = std::max(1, 1024 / chunks);
+    const unsigned blocks = (unsigned)(((int64_t)p.rows + per - 1) / per);
+    return L.run(kPagedWrite, [&] { return launched([&] { ma::paged_write<<<dim3(blocks), dim3(256), 0, L.stream>>>(p, per); }); });
+}
+
+}  // namespace ma_host

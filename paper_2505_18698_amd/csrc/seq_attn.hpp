@@ -1,0 +1,457 @@
+// Exact attention over packed sequences and over paged caches.
+//
+// For every sequence, key head and group of query heads on it:
+//   O_i = sum_j P_ij v_j,  P_ij = exp(s q_i.k_j - lse_i),  lse_i = log sum_j exp(s q_i.k_j),
+// j over the keys that row i sees: the first vis(i) of the sequence.
+#pragma once
+
+#include "seq_tiles.hpp"
+
+namespace ma {
+
+// How a split call divides its work: every sequence's row tiles (R rows) times
+// its pieces of `piece` key tiles (BN keys).  All sequences share one piece
+// length, the shortest that gives about `target` units, so that long and short
+// contexts of a batch end together.
+struct Pieces {
+    int seq, tile, split, splits, piece;  // of the unit or tile searched for (seq = -1: none)
+    int64_t unit0;                        // number of its tile's first unit
+};
+
+template <int R, int BN, int NTH>
+__device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, bool by_tile, int max_keys, char *lds)
+{
+    int64_t *sh = reinterpret_cast<int64_t *>(lds);
+    constexpr int W = NTH / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    auto shape = [&](int s, int &rt, int &kt) {
+        rt = s < p.seqs.B ? (int)(((int64_t)p.seqs.length(s) * p.G + R - 1) / R) : 0;
+        const int kv = s < p.seqs.B ? max(0, min(p.kv_lens[s], max_keys)) : 0;
+        kt = max(1, (kv + BN - 1) / BN);
+    };
+    // all work, in row tiles times key tiles
+    int64_t sum = 0;
+    for (int s = tid; s < p.seqs.B; s += NTH) {
+        int rt, kt;
+        shape(s, rt, kt);
+        sum += (int64_t)rt * kt;
+    }
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+    if (lane == 0) sh[wave] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int i = 0; i < W; ++i) sum += sh[i];
+    __syncthreads();
+    Pieces r{-1, 0, 0, 1, (int)max((int64_t)2, (sum + p.target - 1) / p.target), 0};
+    int64_t tiles_before = 0, units_before = 0;
+    for (int s0 = 0; s0 < p.seqs.B; s0 += NTH) {
+        int rt, kt;
+        shape(s0 + tid, rt, kt);
+        const int splits = (kt + r.piece - 1) / r.piece;
+        int64_t t = rt, u = (int64_t)rt * splits;  // inclusive sums over the threads
+        for (int x = 1; x < 64; x <<= 1) {
+            const int64_t a = __shfl_up(t, x), b = __shfl_up(u, x);
+            if (lane >= x) t += a, u += b;
+        }
+        if (lane == 63) sh[2 * wave] = t, sh[2 * wave + 1] = u;
+        __syncthreads();
+        int64_t at = 0, au = 0;
+        for (int i = 0; i < W; ++i) {
+            if (i < wave) t += sh[2 * i], u += sh[2 * i + 1];
+            at += sh[2 * i], au += sh[2 * i + 1];
+        }
+        __syncthreads();
+        const int64_t t0 = tiles_before + t - rt, u0 = units_before + u - (int64_t)rt * splits;
+        const int64_t k = want - (by_tile ? t0 : u0);
+        const int64_t have = by_tile ? (int64_t)rt : (int64_t)rt * splits;
+        if (k >= 0 && k < have) {  // one thread at most
+            const int tile = (int)(by_tile ? k : k / splits);
+            sh[0] = s0 + tid, sh[1] = tile, sh[2] = by_tile ? 0 : k - (int64_t)tile * splits;
+            sh[3] = splits, sh[4] = u0 + (int64_t)tile * splits;
+        }
+        const bool found = some_thread<NTH>(k >= 0 && k < have, reinterpret_cast<int *>(lds + 64));
+        if (found) {
+            r.seq = (int)sh[0], r.tile = (int)sh[1], r.split = (int)sh[2], r.splits = (int)sh[3], r.unit0 = sh[4];
+            break;
+        }
+        tiles_before += at, units_before += au;
+    }
+    __syncthreads();
+    return r;
+}
+
+// One workgroup of 4 waves per tile of R = 128 RB packed rows (token, head of
+// the group) of one key head: the heads of a group read the same K and V, so
+// they share the tile's copies.  Wave w owns 32 RB rows.  Scores are formed
+// transposed, S^T = K Q^T: a lane holds one query row's scores, so the softmax
+// statistics and the rescaling are lane scalars with one exchange between the
+// two lane halves, and the weights feed O^T = V^T P^T straight from registers.
+template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
+    using S = SeqTile<T, D>;
+    using frag = typename S::frag;
+    static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * W;
+    static constexpr int BN = S::kF32 ? 32 : 64, KT = BN / 32;  // keys a tile
+    static constexpr int TILE = BN * S::ROW;
+    static constexpr int LDS_BYTES = 4 * TILE + 16;  // K and V, two of each, from address 0: a copy's target has 16 bits
+    using Copy = TileCopy<T, D, BN, W>;
+    // A row's weights are taken relative to a reference that follows its running
+    // maximum only when that has grown by more than 2^kSlack: the sums stay exact
+    // to fp32 (weights up to 2^kSlack), and the output is rescaled a few times a row instead of once a tile.
+    static constexpr float kSlack = 8.f;
+
+    struct State {
+        f32x16 o[RB][S::ND];  // O^T: lane 32 h + c, row c, columns 32 dt + kRow32(r) + 4 h
+        float ref[RB], sum[RB];
+    };
+
+    // One key tile.  MASK: some row of the wave sees only a part of it.  There
+    // `fine` weights take part with twice the bits: rows of few keys, all of which
+    // are in such tiles, have outputs as exact as the statistics.
+    template <bool MASK>
+    __device__ static void step(const char *kt, const char *vt, const frag (*qf)[S::NS], const int *vis, int key0,
+                                float c, bool fine, State &st, int lane)
+    {
+        f32x16 s[RB][KT];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int t = 0; t < KT; ++t) s[rb][t] = f32x16{};
+        // (one read of K feeds all RB row blocks)
+        const char *x = kt + (lane & 31) * S::ROW;
+        const int flip = (lane >> 5) ^ S::swz(lane & 7);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int i = 0; i < S::NS; ++i) {
+                const frag a = *reinterpret_cast<const frag *>(x + t * 32 * S::ROW + ((2 * i) ^ flip) * 16);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) s[rb][t] = S::M::mma(a, qf[rb][i], s[rb][t]);
+            }
+        Probs32<T> pf[KT][RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int see = vis[rb] - key0 - 4 * (lane >> 5);
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (MASK && 32 * t + kRow32(r) >= see) s[rb][t][r] = -INFINITY;
+                    mx = max_nan(mx, s[rb][t][r]);
+                }
+            mx = wave_xor_max<32>(mx) * c;
+            if (__any(mx > st.ref[rb] + kSlack)) {
+                const float up = fmaxf(mx, st.ref[rb]);
+                // (a row's first keys: all it has so far is zero, or infinities that take_foreign() added)
+                const float by = st.ref[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref[rb] - up);
+                st.ref[rb] = up;
+                st.sum[rb] *= by;
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt) st.o[rb][dt] *= by;
+            }
+            const float ref = st.ref[rb] == -INFINITY ? 0.f : st.ref[rb];
+            float sum = 0.f;
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[rb][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][t][r], c, -ref));
+                    sum += s[rb][t][r];
+                }
+                pf[t][rb].pack(s[rb][t]);
+            }
+            st.sum[rb] += sum;
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t) aggregate<T, D, RB>(vt + t * 32 * S::ROW, pf[t], st.o, lane);
+        if constexpr (MASK && !S::kF32) {
+            if (fine) {
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    Probs32<T> low[RB];
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) low[rb] = pf[t][rb].rest(s[rb][t]);
+                    aggregate<T, D, RB>(vt + t * 32 * S::ROW, low, st.o, lane);
+                }
+            }
+        }
+    }
+
+    // A value of V that is not finite meets weights of zero in the rows of a masked
+    // tile that do not see it, where the product would make it NaN.  So such
+    // values are looked for (`foreign`), added to the rows that see them, and then
+    // taken for zero.
+    __device__ static bool foreign(const char *vt)
+    {
+        bool bad = false;
+        for (int i = threadIdx.x; i < TILE / 16; i += NTH) {
+            T x[S::V];
+            __builtin_memcpy(x, vt + i * 16, 16);
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) bad |= !(fabsf((float)x[e]) < INFINITY);
+        }
+        return bad;
+    }
+    __device__ static void take_foreign(char *vt, const int *vis, int key0, State &st, int lane)
+    {
+#pragma unroll 1
+        for (int key = 0; key < BN; ++key) {
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int col = 32 * dt + kRow32(r) + 4 * (lane >> 5);
+                    const float y = (float)*reinterpret_cast<const T *>(vt + key * S::ROW + (((col / S::V) ^ S::swz(key)) * 16) + col % S::V * (int)sizeof(T));
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt][r] += fabsf(y) < INFINITY || key0 + key >= vis[rb] ? 0.f : y;
+                }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < TILE / (int)sizeof(T); i += NTH) {
+            T &x = reinterpret_cast<T *>(vt)[i];
+            if (!(fabsf((float)x) < INFINITY)) x = (T)0.f;
+        }
+        __syncthreads();
+    }
+
+    // The K and V rows that a wave copies.
+    struct Rows {
+        const T *k, *v;    // packed: the sequence's rows; paged: the key head's part of page 0
+        const int *table;  // paged: the sequence's pages
+        int kv;            // rows from this one on read as zero
+        int off_k, off_v;
+        int page[Copy::COPIES];  // paged: of the tile that is copied next
+
+        // the pages of the tile from key0 on (a tile ahead of their use)
+        __device__ void look(const SeqFwd &p, int key0, int wave)
+        {
+#pragma unroll
+            for (int i = 0; i < Copy::COPIES; ++i) {
+                const int key = key0 + Copy::row(i, wave);
+                page[i] = key < kv ? table[key >> p.page_log2] : 0;
+            }
+        }
+        // the tile from key0 on
+        __device__ void copy(const SeqFwd &p, int key0, char *kt, char *vt, int wave)
+        {
+            if constexpr (PAGED) {
+                // a page holds the rows of a copy or several copies'
+#pragma unroll
+                for (int i = 0; i < Copy::COPIES; ++i) {
+                    const int key = key0 + Copy::row(i, wave), ld = p.d * (int)sizeof(T);
+                    const int pg = uniform(page[i]);
+                    const bool ok = (unsigned)pg < (unsigned)p.pages;
+                    const int64_t at = ok ? (((int64_t)pg * p.Hkv << p.page_log2) + (key & ((1 << p.page_log2) - 1))) * p.d : 0;
+                    Copy::copy(Copy::source(ok ? (const void *)(k + at) : &kNanRows, kv - key, ld), off_k, kt, i, wave);
+                    Copy::copy(Copy::source(v + at, ok ? kv - key : 0, ld), off_k, vt, i, wave);
+                }
+            } else {
+                const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
+                Copy::tile(k + key0 * p.ldk, kv - key0, ldk, off_k, kt, wave);
+                Copy::tile(v + key0 * p.ldv, kv - key0, ldv, off_v, vt, wave);
+            }
+        }
+    };
+
+    __device__ static void run(const SeqFwd &p, char *lds)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int kvh = uniform((int)(blockIdx.x % p.Hkv));
+        int seq, tile, key_tile0 = 0, key_tiles = 0x7fffffff;
+        int64_t unit = 0;
+        bool parts = false;
+        const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0) : 0;
+        if constexpr (SPLIT) {
+            const Pieces f = find_piece<R, BN, NTH>(p, blockIdx.x / p.Hkv, false, max_keys, lds);
+            if (f.seq < 0) return;
+            seq = uniform(f.seq), tile = uniform(f.tile), parts = f.splits > 1;
+            key_tile0 = uniform(f.split * f.piece), key_tiles = uniform(f.piece);
+            unit = uniform((f.unit0 + f.split) * p.Hkv + kvh);
+        } else {
+            const int64_t t = p.tiles - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
+            seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
+            if (seq < 0) return;
+            tile = uniform((int)(t - tile0(p.seqs, seq, p.G, R)));
+        }
+        const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
+        const int kv = PAGED ? uniform(max(0, min(p.kv_lens[seq], max_keys))) : n;
+        const int rows = n * p.G, r0 = tile * R;
+        auto visible = [&](int r) {  // keys that packed row r sees (the last row stands for those behind it)
+            const int64_t i = (int64_t)min(r, rows - 1) / p.G + (PAGED ? kv - n : 0) + 1;
+            return p.causal ? (int)max((int64_t)0, min(i, (int64_t)kv)) : kv;
+        };
+        const int wr0 = r0 + wave * 32 * RB;
+        const int see_most = uniform(visible(wr0 + 32 * RB - 1));  // keys that some row of the wave sees
+        const int see_all = uniform(visible(r0));  // keys that every row of the tile sees
+        const int first = key_tile0 * BN;
+        const int last = uniform((int)min((int64_t)visible(r0 + R - 1), key_tiles == 0x7fffffff ? (int64_t)0x7fffffff : (int64_t)(key_tile0 + key_tiles) * BN));
+
+        // this lane's query rows; offsets of q and out from the tile's first token
+        const int tok0 = r0 / p.G;
+        const Span qs((const T *)p.q + (row0 + tok0) * p.ldq + (int64_t)kvh * p.G * p.d);
+        int vis[RB], tok[RB], head[RB];
+        frag qf[RB][S::NS];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int r = min(wr0 + 32 * rb + (lane & 31), rows - 1);
+            vis[rb] = visible(r);
+            tok[rb] = r / p.G - tok0;
+            head[rb] = r % p.G;
+            const int at = tok[rb] * (int)p.ldq + head[rb] * p.d;
+#pragma unroll
+            for (int i = 0; i < S::NS; ++i) {
+                const int col = (2 * i + (lane >> 5)) * S::V;
+                const u32x4 x = qs.load16((at + col) * (int)sizeof(T), col < p.d);
+                __builtin_memcpy(&qf[rb][i], &x, 16);
+            }
+        }
+
+        Rows src;
+        src.kv = kv;
+        if constexpr (PAGED) {
+            src.k = (const T *)p.k + ((int64_t)kvh << p.page_log2) * p.d;
+            src.v = (const T *)p.v + ((int64_t)kvh << p.page_log2) * p.d;
+            src.table = p.table + (int64_t)seq * p.blocks;
+            src.off_k = Copy::offset(p.d * (int)sizeof(T), p.d, wave, lane);
+        } else {
+            const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
+            src.k = (const T *)p.k + row0 * p.ldk + kvh * p.d;
+            src.v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
+            src.off_k = Copy::offset(ldk, p.d, wave, lane) + Copy::row(0, wave) * ldk;
+            src.off_v = Copy::offset(ldv, p.d, wave, lane) + Copy::row(0, wave) * ldv;
+        }
+
+        State st;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            st.ref[rb] = -INFINITY, st.sum[rb] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt) st.o[rb][dt] = f32x16{};
+        }
+        // The tile from `key0` on arrives while the one before it is computed.  Two
+        // loops, the tiles that every row sees whole and the others: one loop
+        // with both kinds of step keeps the output registers twice.
+        auto bring = [&](int key0, int buf) {
+            if (key0 >= last) return;
+            src.copy(p, key0, lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, wave);
+            if constexpr (PAGED) src.look(p, key0 + BN, wave);
+        };
+        if constexpr (PAGED) src.look(p, first, wave);
+        bring(first, 0);
+        int key0 = first, buf = 0;
+#pragma unroll 1
+        for (; key0 + BN <= min(see_all, last); key0 += BN, buf ^= 1) {
+            tile_barrier();
+            bring(key0 + BN, buf ^ 1);
+            step<false>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, qf, vis, key0, p.c, p.rest != nullptr, st, lane);
+        }
+#pragma unroll 1
+        for (; key0 < last; key0 += BN, buf ^= 1) {
+            tile_barrier();
+            bring(key0 + BN, buf ^ 1);
+            char *vt = lds + 2 * TILE * buf + TILE;
+            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 4 * TILE))) take_foreign(vt, vis, key0, st, lane);
+            if (key0 < see_most) step<true>(lds + 2 * TILE * buf, vt, qf, vis, key0, p.c, p.rest != nullptr, st, lane);
+        }
+
+        const Span os((T *)p.out + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int r = wr0 + 32 * rb + (lane & 31);
+            const float sum = wave_xor_sum<32>(st.sum[rb]);
+            const bool none = vis[rb] <= first;  // no key to see
+            const float inv = none ? 0.f : 1.f / sum;
+            const float l2 = none ? -INFINITY : st.ref[rb] + __builtin_amdgcn_logf(sum);
+            const bool real = r < rows;
+            if (SPLIT && parts) {
+                const int64_t at = unit * R + wave * 32 * RB + 32 * rb;
+                const Span ps(p.part_o + at * D);
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x16 &x = st.o[rb][dt];
+                        ps.store<float>(f32x4{x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv},
+                                        ((lane & 31) * D + 32 * dt + 8 * e + 4 * (lane >> 5)) * 4, real);
+                    }
+                if (real && lane < 32) p.part_l[at + lane] = l2;
+                continue;
+            }
+            const int at = (tok[rb] * p.Hkv * p.G + head[rb]) * p.d;
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
+                    const f32x16 &x = st.o[rb][dt];
+                    os.store<T>(f32x4{x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv},
+                                (at + col) * (int)sizeof(T), real && col < p.d);
+                }
+            if constexpr (!S::kF32) {
+                if (p.rest) {
+                    const Span es((T *)p.rest + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
+#pragma unroll
+                    for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
+                            f32x4 x;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                x[i] = st.o[rb][dt][4 * e + i] * inv;
+                                x[i] -= (float)to_elem<T>(x[i]);
+                            }
+                            es.store<T>(x, (at + col) * (int)sizeof(T), real && col < p.d);
+                        }
+                }
+            }
+            if (p.lse && real && lane < 32)
+                p.lse[(int64_t)(kvh * p.G + head[rb]) * p.seqs.total + row0 + tok0 + tok[rb]] = l2 * kLn2;
+        }
+    }
+};
+
+template <typename T, int D, int RB, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void seq_attention(SeqFwd p)
+{
+    using U = SeqAttn<T, D, RB, PAGED, SPLIT>;
+    __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
+    U::run(p, lds);
+}
+
+// The pieces of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x).
+// One workgroup per row tile and key head, one thread per 4 columns of a row.
+template <typename T, int D, int R, int BN>
+__global__ __launch_bounds__(256) void seq_join(SeqFwd p)
+{
+    __shared__ __attribute__((aligned(16))) char lds[128];
+    const int kvh = blockIdx.x % p.Hkv;
+    const int max_keys = (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0);
+    const Pieces f = find_piece<R, BN, 256>(p, blockIdx.x / p.Hkv, true, max_keys, lds);
+    if (f.seq < 0 || f.splits == 1) return;
+    const int row0 = p.seqs.start(f.seq), rows = p.seqs.length(f.seq) * p.G;
+    for (int i = threadIdx.x; i < R * (D / 4); i += 256) {
+        const int r = i / (D / 4), col = i % (D / 4) * 4, at = f.tile * R + r;
+        if (at >= rows || col >= p.d) continue;
+        const int64_t base = (f.unit0 * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
+        float mx = -INFINITY;
+        for (int x = 0; x < f.splits; ++x) mx = max_nan(mx, p.part_l[base + x * each]);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float sum = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < f.splits; ++x) {
+            const float l = p.part_l[base + x * each];
+            if (l == -INFINITY) continue;  // a piece of which this row sees nothing
+            const float w = __builtin_amdgcn_exp2f(l - ref);
+            sum += w;
+            o += w * *reinterpret_cast<const f32x4 *>(p.part_o + (base + x * each) * D + col);
+        }
+        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+        const int64_t row = row0 + at / p.G;
+        const int head = kvh * p.G + at % p.G;
+        store4<T>((T *)p.out + (row * p.Hkv * p.G + head) * p.d + col, o * inv);
+        if (p.lse && col == 0) p.lse[(int64_t)head * p.seqs.total + row] = (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+
+}  // namespace ma

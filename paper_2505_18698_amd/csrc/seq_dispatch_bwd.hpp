@@ -1,0 +1,34 @@
+// Launches of the exact attention gradient (included by seq_bwd_*.hip).
+#pragma once
+
+#include "seq_bwd.hpp"
+#include "seq_host.hpp"
+
+namespace ma_host {
+
+template <typename T, int D> int run_seq_bwd_d(Launcher &L, const ma::SeqBwd &p)
+{
+    const dim3 block(256);
+    int rc = L.run(kSeqStats, [&] {
+        return launched([&] { ma::seq_stats<T><<<dim3((unsigned)p.norm_blocks), block, 0, L.stream>>>(p); });
+    });
+    if (rc != MA_OK) return rc;
+    rc = L.run(kSeqBwdK, [&] {
+        return launched([&] { ma::seq_bwd_k<T, D><<<dim3((unsigned)((int64_t)p.tiles_k * p.Hkv)), block, 0, L.stream>>>(p); });
+    });
+    if (rc != MA_OK) return rc;
+    return L.run(kSeqBwdQ, [&] {
+        return launched([&] { ma::seq_bwd_q<T, D><<<dim3((unsigned)((int64_t)p.tiles_q * p.Hkv)), block, 0, L.stream>>>(p); });
+    });
+}
+
+template <typename T> int run_seq_bwd_impl(Launcher &L, const ma::SeqBwd &p)
+{
+    switch (tile_d(p.d)) {
+    case 64: return run_seq_bwd_d<T, 64>(L, p);
+    case 96: return run_seq_bwd_d<T, 96>(L, p);
+    default: return run_seq_bwd_d<T, 128>(L, p);
+    }
+}
+
+}  // namespace ma_host

@@ -1,0 +1,39 @@
+// Launches of the exact attention forward (included by seq_fwd_*.hip).
+#pragma once
+
+#include "seq_attn.hpp"
+#include "seq_host.hpp"
+
+namespace ma_host {
+
+template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how)
+{
+    const dim3 grid((unsigned)(how.units * p.Hkv)), block(256);
+    int rc = L.run(kSeqFwd, [&] {
+        return launched([&] {
+            if (!how.paged)
+                ma::seq_attention<T, D, 1, false, false><<<grid, block, 0, L.stream>>>(p);
+            else if (!how.split)
+                ma::seq_attention<T, D, 1, true, false><<<grid, block, 0, L.stream>>>(p);
+            else
+                ma::seq_attention<T, D, 1, true, true><<<grid, block, 0, L.stream>>>(p);
+        });
+    });
+    if (rc != MA_OK || !how.split) return rc;
+    return L.run(kSeqJoin, [&] {
+        return launched([&] {
+            ma::seq_join<T, D, kSeqRows, sizeof(T) == 4 ? 32 : 64><<<dim3((unsigned)((int64_t)p.tiles * p.Hkv)), block, 0, L.stream>>>(p);
+        });
+    });
+}
+
+template <typename T> int run_seq_fwd_impl(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how)
+{
+    switch (tile_d(p.d)) {
+    case 64: return run_seq_fwd_d<T, 64>(L, p, how);
+    case 96: return run_seq_fwd_d<T, 96>(L, p, how);
+    default: return run_seq_fwd_d<T, 128>(L, p, how);
+    }
+}
+
+}  // namespace ma_host

@@ -1,0 +1,57 @@
+// Host-side pieces of the exact attention over sequences and of the paged
+// cache: what a call needs of the library's streams and workspaces
+// (monarch_attn.hip), and the per-dtype dispatch (seq_fwd_*.hip, seq_bwd_*.hip).
+#pragma once
+
+#include <mutex>
+
+#include "host_common.hpp"
+
+namespace ma {
+struct SeqFwd;
+struct SeqBwd;
+struct PagedPlan;
+struct PagedWrite;
+}  // namespace ma
+
+namespace ma_host {
+
+extern thread_local char g_err[512];  // what monarch_attn_last_error() returns
+
+// Kernel kinds of the timing interface, after those of Kind.
+enum SeqKind { kSeqFwd = 10, kSeqJoin = 11, kSeqStats = 12, kSeqBwdK = 13, kSeqBwdQ = 14, kPagedPlan = 15, kPagedWrite = 16 };
+
+// The device, capture state and workspace of one call; `hold` keeps the
+// workspace until the call's launches are enqueued.
+struct CallScope {
+    int dev = 0, num_cus = 0;
+    bool capturing = false;
+    char *ws = nullptr;
+    std::unique_lock<std::mutex> hold;
+};
+// The current device and whether `stream` is under capture.
+int begin_call(hipStream_t stream, CallScope &c);
+// Its workspace, grown to `need` bytes (acquire_workspace).
+int call_workspace(hipStream_t stream, size_t need, CallScope &c);
+// Run the launches of one call, timed if timing is on, and check for launch errors.
+int run_launches(hipStream_t stream, int (*f)(Launcher &, void *), void *arg);
+
+bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb);
+
+// How a forward call runs.
+struct SeqPlan {
+    bool paged, split;
+    int row_blocks;  // 32-row blocks a wave
+    int64_t units;   // workgroups of one key head
+};
+
+// packed rows a workgroup takes, and keys a tile
+constexpr int kSeqRows = 128;
+inline int seq_tile_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }
+
+template <typename T> int run_seq_fwd(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how);
+template <typename T> int run_seq_bwd(Launcher &L, const ma::SeqBwd &p);
+int run_paged_plan(Launcher &L, const ma::PagedPlan &p);
+int run_paged_write(Launcher &L, const ma::PagedWrite &p);
+
+}  // namespace ma_host

@@ -1,0 +1,245 @@
+// Tiles of the exact attention over packed and paged sequences: 32 x 32
+// products whose left operand comes from swizzled row-major LDS tiles, the
+// copies that fill those tiles from global memory, and the search for the
+// sequence that a tile of packed rows belongs to.
+#pragma once
+
+#include "seq_params.hpp"
+#include "tiles.hpp"
+
+namespace ma {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef const __attribute__((address_space(1))) void *global_ptr;
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// One 32 x 32 step: 16 elements of the contraction in 16-bit types; 8 in fp32,
+// as four instructions of depth 2, operand slot (half, i) being element 4 half + i.
+template <typename T> struct Mma32;
+template <> struct Mma32<__bf16> {
+    using frag = bf16x8;
+    __device__ static f32x16 mma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma32<_Float16> {
+    using frag = f16x8;
+    __device__ static f32x16 mma(frag a, frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma32<float> {
+    using frag = f32x4;
+    __device__ static f32x16 mma(frag a, frag b, f32x16 c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// Result layout of a 32 x 32 step: lane 32 h + c holds column c, rows kRow32(r) + 4 h, r = 0..15.
+__device__ constexpr int kRow32(int r) { return 8 * (r / 4) + r % 4; }
+
+// A row-major LDS tile of rows of D elements in 16-byte chunks, PC chunks a
+// row.  Chunk c of row r lies at c ^ swz(r): the 8 rows that one pass of a
+// 16-byte read takes from the same column fall on 8 different bank groups, and
+// so do the two halves of the 4 rows that a transposing read takes.
+template <typename T, int D> struct SeqTile {
+    static constexpr int V = 16 / (int)sizeof(T);           // elements a chunk
+    static constexpr int PC = D * (int)sizeof(T) <= 128 ? 8 : D * (int)sizeof(T) <= 256 ? 16 : 32;
+    static constexpr int ROW = PC * 16;                     // bytes a row
+    static constexpr int NS = D / (2 * V);                  // steps of a product over D
+    static constexpr int ND = D / 32;                       // 32-wide tiles of D
+    static constexpr bool kF32 = sizeof(T) == 4;
+    using M = Mma32<T>;
+    using frag = typename M::frag;
+
+    __device__ static int swz(int row) { return ((row & 1) << 2) | ((row >> 1) & 3); }
+
+    // acc += X Y^T of the tile's 32 rows from `rows` on and 32 rows Y held as
+    // operand fragments (lane 32 h + c: row c, chunks 2 st + h).
+    __device__ static f32x16 scores(const char *rows, const frag *y, int lane, f32x16 acc)
+    {
+        const char *x = rows + (lane & 31) * ROW;
+        const int flip = (lane >> 5) ^ swz(lane & 7);
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+            acc = M::mma(*reinterpret_cast<const frag *>(x + ((2 * st) ^ flip) * 16), y[st], acc);
+        return acc;
+    }
+
+    // Operand fragment X^T: lane 32 h + c holds column 32 dt + c of the rows
+    // 4 h + 0..3 and 8 + 4 h + 0..3 of the 16 rows from `rows` on (16-bit types).
+    __device__ static frag columns(const char *rows, int dt, int lane)
+    {
+        const int j = lane & 15, r = 4 * (lane >> 5) + (j >> 2);
+        const int chunk = 4 * dt + 2 * ((lane >> 4) & 1) + ((j >> 1) & 1);
+        const char *x = rows + r * ROW + ((chunk ^ swz(r)) * 16) + (j & 1) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x + 8 * ROW));
+        frag f;
+        __builtin_memcpy(&f, &lo, 8);
+        __builtin_memcpy((char *)&f + 8, &hi, 8);
+        return f;
+    }
+
+    // Element (row, 32 dt + lane % 32) of the tile (fp32).
+    __device__ static float element(const char *tile, int row, int dt, int lane)
+    {
+        const int c = lane & 31;
+        return *reinterpret_cast<const float *>(tile + row * ROW + (((8 * dt + (c >> 2)) ^ swz(row)) * 16) + (c & 3) * 4);
+    }
+};
+
+// The 32 x 32 result `s` as the right operand of products that contract over
+// its rows: two fragments of 16 rows in 16-bit types, the values themselves in fp32.
+template <typename T> struct Probs32 {
+    typename Mma32<T>::frag f[2];
+    __device__ inline void pack(f32x16 s)
+    {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) f[r / 8][r % 8] = to_elem<T>(s[r]);
+    }
+    // what pack(s) left of s
+    __device__ inline Probs32 rest(f32x16 s) const
+    {
+        Probs32 x;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x.f[r / 8][r % 8] = to_elem<T>(s[r] - (float)f[r / 8][r % 8]);
+        return x;
+    }
+};
+template <> struct Probs32<float> {
+    f32x16 s;
+    __device__ inline void pack(f32x16 x) { s = x; }
+};
+
+// acc[dt] += X^T B of 32 tile rows from `rows` on; B: one Probs32 for each of NB column blocks.
+template <typename T, int D, int NB>
+__device__ inline void aggregate(const char *rows, const Probs32<T> *b, f32x16 (*acc)[SeqTile<T, D>::ND], int lane)
+{
+    using S = SeqTile<T, D>;
+    if constexpr (S::kF32) {
+#pragma unroll
+        for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float x = S::element(rows, kRow32(r) + 4 * (lane >> 5), dt, lane);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    acc[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, b[n].s[r], acc[n][dt], 0, 0, 0);
+            }
+    } else {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt) {
+                const typename S::frag x = S::columns(rows + ks * 16 * S::ROW, dt, lane);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) acc[n][dt] = S::M::mma(x, b[n].f[ks], acc[n][dt]);
+            }
+    }
+}
+
+// A value that all lanes of the wave share, in a scalar register: the address of a copy has to be there.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// What a page outside the cache reads as: NaN in every type.
+static __device__ __align__(16) const struct NanRows { uint32_t x[256]; } kNanRows = [] {
+    NanRows n{};
+    for (uint32_t &x : n.x) x = 0x7fff7fffu;
+    return n;
+}();
+
+// The copies global -> LDS that fill a tile of BN rows: copy i of wave w fills
+// the RPC rows from (i NW + w) RPC on, 16 bytes a lane, from rows `ld` bytes
+// apart that start at a uniform address.  Rows past the `valid` ones and
+// columns past d read as zero, by the range check of the buffer access.
+template <typename T, int D, int BN, int NW> struct TileCopy {
+    using S = SeqTile<T, D>;
+    static constexpr int RPC = 64 / S::PC, COPIES = BN / RPC / NW;
+    static_assert(COPIES * NW * RPC == BN && NW * RPC % 8 == 0, "whole copies, one column a lane");
+
+    // first row of copy i in the tile
+    __device__ static int row(int i, int wave) { return (i * NW + wave) * RPC; }
+    // byte offset of this lane's chunk from the first row of the wave's copies
+    __device__ static int offset(int ld, int d, int wave, int lane)
+    {
+        const int r = lane / S::PC, col = ((lane % S::PC) ^ S::swz((wave * RPC + r) & 7)) * S::V;
+        return col < d ? r * ld + col * (int)sizeof(T) : (int)0x80000000;
+    }
+    // the descriptor of a buffer access that reads zero behind `valid` rows
+    __device__ static u32x4 source(const void *rows, int valid, int ld)
+    {
+        const int64_t at = uniform((int64_t)rows);
+        return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)uniform(max(0, min(valid, BN)) * ld), (uint32_t)Span::kDefault};
+    }
+    // The copy itself, in assembly: behind the builtin the compiler waits for it
+    // before every later LDS read, those of the other tiles among them, so that
+    // a tile would not arrive while another is computed.  The instruction writes LDS and
+    // no register; tile_barrier() waits for it.
+    // (The compiler does not see into it either: the five wait states are
+    // those between a vector write of a scalar register and its use here.)
+    __device__ static void copy(u32x4 r, int off, char *tile, int i, int wave)
+    {
+        const int to = (int)(uintptr_t)(lds_ptr)tile + row(i, wave) * S::ROW;
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                     :: "v"(off), "s"(r), "s"(uniform(to)) : "memory", "m0");
+    }
+    // the whole tile; `rows`: its first row, `off`: offset() of the wave's first row in it
+    __device__ static void tile(const void *rows, int valid, int ld, int off, char *to, int wave)
+    {
+        const u32x4 r = source(rows, valid, ld);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) copy(r, off + i * NW * RPC * ld, to, i, wave);
+    }
+};
+
+// Every copy of this wave has arrived, and every wave of the workgroup is here.
+__device__ inline void tile_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Whether `x` holds on some thread of a workgroup of NTH (`shared`: NTH / 64 integers of LDS).
+template <int NTH> __device__ inline bool some_thread(bool x, int *shared)
+{
+    const int tid = threadIdx.x;
+    const bool mine = __any(x);
+    if (tid % 64 == 0) shared[tid / 64] = mine;
+    __syncthreads();
+    int any = 0;
+#pragma unroll
+    for (int i = 0; i < NTH / 64; ++i) any |= shared[i];
+    __syncthreads();
+    return uniform(any) != 0;
+}
+
+// ---- sequences ----
+
+// Sequence s holds tiles tile0(s) .. tile0(s) + ceil(rows / R) - 1 of R packed
+// rows, tile0(s) = floor(first row / R) + s: with ceil(n / R) <= floor((x + n) / R)
+// - floor(x / R) + 1 the ranges of two sequences never meet, and no prefix sum
+// over the sequences is needed.  G: packed rows a token.
+__device__ inline int64_t tile0(const Seqs &q, int s, int G, int R) { return (int64_t)q.start(s) * G / R + s; }
+
+// The sequence of tile t (all lanes of a wave together; 64 candidates a step),
+// or -1 where t is no tile of any.
+__device__ inline int seq_of_tile(const Seqs &q, int64_t t, int G, int R, int lane)
+{
+    int lo = 0, n = q.B;
+    while (n > 1) {
+        const int step = (n + 63) / 64;
+        const int64_t at = (int64_t)lane * step;
+        const int cnt = __popcll(__ballot(at < n && tile0(q, lo + (int)at, G, R) <= t));
+        if (cnt == 0) return -1;
+        lo += (cnt - 1) * step;
+        n = min(step, n - (cnt - 1) * step);
+    }
+    const int64_t k = t - tile0(q, lo, G, R);
+    return k >= 0 && k * R < (int64_t)q.length(lo) * G ? lo : -1;
+}
+
+}  // namespace ma
