@@ -166,7 +166,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
     p.c = log2_scale(d), p.causal = causal != 0, p.tiles = (int)tiles;
-    x.how = SeqPlan{false, false, 1, tiles};
+    x.how = SeqPlan{false, false, kSeqRows, tiles};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
 }
@@ -236,25 +236,32 @@ int log2_of(int64_t page)
     return x;
 }
 
-// How a paged call is split.  Units to aim at: two workgroups a compute unit,
-// what it holds at a time.  A call whose row tiles fill that by themselves is not split, nor
-// is one whose longest possible context is a few key tiles.
+// How a paged call runs.  Sequences of few new rows (on average no more than 32
+// packed ones: single tokens) take 32-row tiles, whose waves share the keys.
+// The keys are split into units of equal length, a few times as many as the
+// device holds workgroups (two a compute unit), so that long and short contexts of a
+// batch fill it evenly: the more rows a tile has, the more a unit's partial result costs.  A call
+// with many times as many row tiles is not split, nor is one whose longest possible context is a few key tiles.
 struct PagedSplit {
+    int rows;
     bool split;
-    int64_t target, units;
-    size_t bytes_o, bytes_l;
+    int64_t tiles, target, units;
+    size_t bytes_o, bytes_l, bytes_parts;
 };
 
-PagedSplit paged_split(int64_t tiles, int64_t Hkv, int64_t d, int64_t max_keys, int64_t num_cus, int32_t dtype)
+PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t max_keys, int64_t num_cus, int32_t dtype)
 {
-    PagedSplit s{false, 0, tiles, 0, 0};
-    s.target = std::max<int64_t>(1, 2 * num_cus / Hkv);
-    if (tiles >= s.target || max_keys <= 8 * seq_tile_keys(dtype)) return s;
+    const bool few = total * G <= B * kSeqFewRows;
+    PagedSplit s{few ? kSeqFewRows : kSeqRows, false, 0, 0, 0, 0, 0, 0};
+    s.tiles = s.units = tiles_of(total, G, B, s.rows);
+    s.target = std::max<int64_t>(1, (few ? 8 : 4) * num_cus / Hkv);
+    if (s.tiles >= 4 * s.target || max_keys <= 16 * seq_tile_keys(dtype)) return s;
     s.split = true;
-    s.units = s.target + tiles;
-    const size_t rows = (size_t)s.units * Hkv * kSeqRows;
+    s.units = s.target + s.tiles;
+    const size_t rows = (size_t)s.units * Hkv * s.rows;
     s.bytes_o = align_up(rows * tile_d(d) * 4);
     s.bytes_l = align_up(rows * 4);
+    s.bytes_parts = align_up((size_t)(s.tiles + 1) * sizeof(ma::SeqTileParts));
     return s;
 }
 
@@ -266,8 +273,8 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
     MA_TRY(check_pages(pages, page));
     if (blocks < 0 || blocks > 0x7fffffff) return fail(MA_EINVAL, "blocks must be in 0..2^31 - 1");
-    const int64_t G = Hq / Hkv, tiles = tiles_of(total, G, B, kSeqRows);
-    MA_TRY(check_grid(tiles, Hkv));
+    const int64_t G = Hq / Hkv;
+    MA_TRY(check_grid(tiles_of(total, G, B, kSeqFewRows), Hkv));
     if (B == 0 || total == 0) return MA_OK;
     const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
@@ -287,10 +294,10 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
     MA_TRY(begin_call(stream, c));
-    const PagedSplit s = paged_split(tiles, Hkv, d, blocks * page, c.num_cus, dtype);
+    const PagedSplit s = paged_split(total, B, G, Hkv, d, blocks * page, c.num_cus, dtype);
     if (s.split) {
         MA_TRY(check_grid(s.units, Hkv));
-        MA_TRY(call_workspace(stream, s.bytes_o + s.bytes_l, c));
+        MA_TRY(call_workspace(stream, s.bytes_o + s.bytes_l + s.bytes_parts, c));
     }
     FwdLaunch x{};
     ma::SeqFwd &p = x.p;
@@ -300,10 +307,11 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq;
     p.page_log2 = log2_of(page), p.pages = (int)pages, p.blocks = (int)blocks;
-    p.c = log2_scale(d), p.causal = causal != 0, p.tiles = (int)tiles;
+    p.c = log2_scale(d), p.causal = causal != 0, p.tiles = (int)s.tiles;
     p.part_o = (float *)c.ws, p.part_l = (float *)(c.ws + s.bytes_o);
+    p.parts = (ma::SeqTileParts *)(c.ws + s.bytes_o + s.bytes_l);
     p.target = (int)s.target;
-    x.how = SeqPlan{true, s.split, 1, s.units};
+    x.how = SeqPlan{true, s.split, s.rows, s.units};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
 }

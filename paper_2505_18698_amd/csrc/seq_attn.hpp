@@ -14,12 +14,12 @@ namespace ma {
 // length, the shortest that gives about `target` units, so that long and short
 // contexts of a batch end together.
 struct Pieces {
-    int seq, tile, split, splits, piece;  // of the unit or tile searched for (seq = -1: none)
-    int64_t unit0;                        // number of its tile's first unit
+    int seq, tile, split, splits, piece;  // of the unit searched for (seq = -1: none)
+    int index, unit0;                     // number of its tile, and of the tile's first unit
 };
 
 template <int R, int BN, int NTH>
-__device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, bool by_tile, int max_keys, char *lds)
+__device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, int max_keys, char *lds)
 {
     int64_t *sh = reinterpret_cast<int64_t *>(lds);
     constexpr int W = NTH / 64;
@@ -29,20 +29,21 @@ __device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, bool by_tile,
         const int kv = s < p.seqs.B ? max(0, min(p.kv_lens[s], max_keys)) : 0;
         kt = max(1, (kv + BN - 1) / BN);
     };
-    // all work, in row tiles times key tiles
-    int64_t sum = 0;
+    // all work, in row tiles times key tiles, and all row tiles
+    int64_t sum = 0, all = 0;
     for (int s = tid; s < p.seqs.B; s += NTH) {
         int rt, kt;
         shape(s, rt, kt);
-        sum += (int64_t)rt * kt;
+        sum += (int64_t)rt * kt, all += rt;
     }
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
-    if (lane == 0) sh[wave] = sum;
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x), all += __shfl_xor(all, x);
+    if (lane == 0) sh[2 * wave] = sum, sh[2 * wave + 1] = all;
     __syncthreads();
-    sum = 0;
-    for (int i = 0; i < W; ++i) sum += sh[i];
+    sum = all = 0;
+    for (int i = 0; i < W; ++i) sum += sh[2 * i], all += sh[2 * i + 1];
     __syncthreads();
-    Pieces r{-1, 0, 0, 1, (int)max((int64_t)2, (sum + p.target - 1) / p.target), 0};
+    if (blockIdx.x == 0 && tid == 0) p.parts[0].splits = (int)all;
+    Pieces r{-1, 0, 0, 1, (int)max((int64_t)2, (sum + p.target - 1) / p.target), 0, 0};
     int64_t tiles_before = 0, units_before = 0;
     for (int s0 = 0; s0 < p.seqs.B; s0 += NTH) {
         int rt, kt;
@@ -61,17 +62,16 @@ __device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, bool by_tile,
             at += sh[2 * i], au += sh[2 * i + 1];
         }
         __syncthreads();
-        const int64_t t0 = tiles_before + t - rt, u0 = units_before + u - (int64_t)rt * splits;
-        const int64_t k = want - (by_tile ? t0 : u0);
-        const int64_t have = by_tile ? (int64_t)rt : (int64_t)rt * splits;
-        if (k >= 0 && k < have) {  // one thread at most
-            const int tile = (int)(by_tile ? k : k / splits);
-            sh[0] = s0 + tid, sh[1] = tile, sh[2] = by_tile ? 0 : k - (int64_t)tile * splits;
-            sh[3] = splits, sh[4] = u0 + (int64_t)tile * splits;
+        const int64_t u0 = units_before + u - (int64_t)rt * splits, k = want - u0;
+        const bool mine = k >= 0 && k < (int64_t)rt * splits;  // one thread at most
+        if (mine) {
+            const int tile = (int)(k / splits);
+            sh[0] = s0 + tid, sh[1] = tile, sh[2] = k - (int64_t)tile * splits, sh[3] = splits;
+            sh[4] = tiles_before + t - rt + tile, sh[5] = u0 + (int64_t)tile * splits;
         }
-        const bool found = some_thread<NTH>(k >= 0 && k < have, reinterpret_cast<int *>(lds + 64));
-        if (found) {
-            r.seq = (int)sh[0], r.tile = (int)sh[1], r.split = (int)sh[2], r.splits = (int)sh[3], r.unit0 = sh[4];
+        if (some_thread<NTH>(mine, reinterpret_cast<int *>(lds + 64))) {
+            r.seq = (int)sh[0], r.tile = (int)sh[1], r.split = (int)sh[2], r.splits = (int)sh[3];
+            r.index = (int)sh[4], r.unit0 = (int)sh[5];
             break;
         }
         tiles_before += at, units_before += au;
@@ -80,17 +80,22 @@ __device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, bool by_tile,
     return r;
 }
 
-// One workgroup of 4 waves per tile of R = 128 RB packed rows (token, head of
+// One workgroup of 4 waves per tile of R = 32 RB WR packed rows (token, head of
 // the group) of one key head: the heads of a group read the same K and V, so
-// they share the tile's copies.  Wave w owns 32 RB rows.  Scores are formed
+// they share the tile's copies.  With WR = 4 each wave owns 32 RB rows.  With WR = 1, for
+// the few rows of single tokens, all waves copy, every wave takes one of the
+// tile's 32-key parts, and the first joins them at the end.  Scores are formed
 // transposed, S^T = K Q^T: a lane holds one query row's scores, so the softmax
 // statistics and the rescaling are lane scalars with one exchange between the
 // two lane halves, and the weights feed O^T = V^T P^T straight from registers.
-template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
+template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * W;
-    static constexpr int BN = S::kF32 ? 32 : 64, KT = BN / 32;  // keys a tile
+    static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
+    static constexpr int BN = S::kF32 ? 32 : 64;           // keys a tile
+    static constexpr int KT = WR == 1 ? 1 : BN / 32;       // 32-key parts that a wave takes
+    static constexpr int KW = WR == 1 ? BN / 32 : 1;       // waves that share a tile's keys
+    static_assert(WR == W || WR == 1, "rows or keys over the waves");
     static constexpr int TILE = BN * S::ROW;
     static constexpr int LDS_BYTES = 4 * TILE + 16;  // K and V, two of each, from address 0: a copy's target has 16 bits
     using Copy = TileCopy<T, D, BN, W>;
@@ -192,10 +197,10 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
         }
         return bad;
     }
-    __device__ static void take_foreign(char *vt, const int *vis, int key0, State &st, int lane)
+    __device__ static void take_foreign(char *vt, const int *vis, int key0, bool mine, State &st, int lane)
     {
 #pragma unroll 1
-        for (int key = 0; key < BN; ++key) {
+        for (int key = 0; key < (mine ? BN : 0); ++key) {
 #pragma unroll
             for (int dt = 0; dt < S::ND; ++dt)
 #pragma unroll
@@ -212,6 +217,44 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
             if (!(fabsf((float)x) < INFINITY)) x = (T)0.f;
         }
         __syncthreads();
+    }
+
+    // The states of the waves that shared the tiles' keys, into the first one's.
+    __device__ static void join_waves(char *lds, int wave, int lane, State &st)
+    {
+        constexpr int N = S::ND * 16 + 2;  // a lane's values of a row block
+        static_assert((KW - 1) * RB * N * 256 <= 4 * TILE, "the tiles' room holds them");
+        float *mine = reinterpret_cast<float *>(lds) + (wave - 1) * RB * N * 64 + lane;
+        __syncthreads();
+        if (wave > 0 && wave < KW) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                mine[(rb * N + N - 2) * 64] = st.ref[rb], mine[(rb * N + N - 1) * 64] = st.sum[rb];
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mine[(rb * N + dt * 16 + r) * 64] = st.o[rb][dt][r];
+            }
+        }
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int w = 1; w < KW; ++w) {
+            const float *other = reinterpret_cast<float *>(lds) + (w - 1) * RB * N * 64 + lane;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float ref = other[(rb * N + N - 2) * 64], up = fmaxf(ref, st.ref[rb]), base = up == -INFINITY ? 0.f : up;
+                // (a part without a key adds zeros, or infinities that take_foreign() added)
+                const float a = st.ref[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref[rb] - base);
+                const float b = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - base);
+                st.ref[rb] = up;
+                st.sum[rb] = st.sum[rb] * a + other[(rb * N + N - 1) * 64] * b;
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) st.o[rb][dt][r] = st.o[rb][dt][r] * a + other[(rb * N + dt * 16 + r) * 64] * b;
+            }
+        }
     }
 
     // The K and V rows that a wave copies.
@@ -262,11 +305,12 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
         bool parts = false;
         const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0) : 0;
         if constexpr (SPLIT) {
-            const Pieces f = find_piece<R, BN, NTH>(p, blockIdx.x / p.Hkv, false, max_keys, lds);
+            const Pieces f = find_piece<R, BN, NTH>(p, blockIdx.x / p.Hkv, max_keys, lds);
             if (f.seq < 0) return;
             seq = uniform(f.seq), tile = uniform(f.tile), parts = f.splits > 1;
             key_tile0 = uniform(f.split * f.piece), key_tiles = uniform(f.piece);
-            unit = uniform((f.unit0 + f.split) * p.Hkv + kvh);
+            unit = uniform((int64_t)(f.unit0 + f.split) * p.Hkv + kvh);
+            if (f.split == 0 && kvh == 0 && tid == 0) p.parts[1 + f.index] = SeqTileParts{seq, tile, f.splits, f.unit0};
         } else {
             const int64_t t = p.tiles - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
             seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
@@ -280,7 +324,9 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
             const int64_t i = (int64_t)min(r, rows - 1) / p.G + (PAGED ? kv - n : 0) + 1;
             return p.causal ? (int)max((int64_t)0, min(i, (int64_t)kv)) : kv;
         };
-        const int wr0 = r0 + wave * 32 * RB;
+        const int wr0 = r0 + (WR == 1 ? 0 : wave) * 32 * RB;
+        const int part = WR == 1 ? min(wave, KW - 1) : 0;  // this wave's keys in a tile, in parts of 32
+        const bool idle = wave >= KW && WR == 1;
         const int see_most = uniform(visible(wr0 + 32 * RB - 1));  // keys that some row of the wave sees
         const int see_all = uniform(visible(r0));  // keys that every row of the tile sees
         const int first = key_tile0 * BN;
@@ -343,15 +389,24 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
         for (; key0 + BN <= min(see_all, last); key0 += BN, buf ^= 1) {
             tile_barrier();
             bring(key0 + BN, buf ^ 1);
-            step<false>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, qf, vis, key0, p.c, p.rest != nullptr, st, lane);
+            if (idle) continue;
+            step<false>(lds + 2 * TILE * buf + part * 32 * S::ROW, lds + 2 * TILE * buf + TILE + part * 32 * S::ROW, qf, vis,
+                        key0 + 32 * part, p.c, p.rest != nullptr, st, lane);
         }
 #pragma unroll 1
         for (; key0 < last; key0 += BN, buf ^= 1) {
             tile_barrier();
             bring(key0 + BN, buf ^ 1);
             char *vt = lds + 2 * TILE * buf + TILE;
-            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 4 * TILE))) take_foreign(vt, vis, key0, st, lane);
-            if (key0 < see_most) step<true>(lds + 2 * TILE * buf, vt, qf, vis, key0, p.c, p.rest != nullptr, st, lane);
+            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 4 * TILE)))
+                take_foreign(vt, vis, key0, wave == 0 || WR != 1, st, lane);
+            if (key0 + 32 * part < see_most && !idle)
+                step<true>(lds + 2 * TILE * buf + part * 32 * S::ROW, vt + part * 32 * S::ROW, qf, vis, key0 + 32 * part, p.c,
+                           p.rest != nullptr, st, lane);
+        }
+        if constexpr (KW > 1) {
+            join_waves(lds, wave, lane, st);
+            if (wave > 0) return;
         }
 
         const Span os((T *)p.out + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
@@ -364,7 +419,7 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
             const float l2 = none ? -INFINITY : st.ref[rb] + __builtin_amdgcn_logf(sum);
             const bool real = r < rows;
             if (SPLIT && parts) {
-                const int64_t at = unit * R + wave * 32 * RB + 32 * rb;
+                const int64_t at = unit * R + wr0 - r0 + 32 * rb;
                 const Span ps(p.part_o + at * D);
 #pragma unroll
                 for (int dt = 0; dt < S::ND; ++dt)
@@ -411,46 +466,60 @@ template <typename T, int D, int RB, bool PAGED, bool SPLIT> struct SeqAttn {
     }
 };
 
-template <typename T, int D, int RB, bool PAGED, bool SPLIT>
+template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT>
 __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void seq_attention(SeqFwd p)
 {
-    using U = SeqAttn<T, D, RB, PAGED, SPLIT>;
+    using U = SeqAttn<T, D, RB, WR, PAGED, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
 }
 
 // The pieces of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x).
-// One workgroup per row tile and key head, one thread per 4 columns of a row.
-template <typename T, int D, int R, int BN>
+// One workgroup per row tile, key head and `gridDim.y`-th of the tile's rows; it takes a row at a
+// time, 32 threads a piece and 8 pieces at once.
+template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
 {
-    __shared__ __attribute__((aligned(16))) char lds[128];
-    const int kvh = blockIdx.x % p.Hkv;
-    const int max_keys = (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0);
-    const Pieces f = find_piece<R, BN, 256>(p, blockIdx.x / p.Hkv, true, max_keys, lds);
-    if (f.seq < 0 || f.splits == 1) return;
-    const int row0 = p.seqs.start(f.seq), rows = p.seqs.length(f.seq) * p.G;
-    for (int i = threadIdx.x; i < R * (D / 4); i += 256) {
-        const int r = i / (D / 4), col = i % (D / 4) * 4, at = f.tile * R + r;
-        if (at >= rows || col >= p.d) continue;
-        const int64_t base = (f.unit0 * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
+    constexpr int C = D / 32;  // columns a thread
+    __shared__ float sh_o[8][D], sh_l[8];
+    const int kvh = blockIdx.x % p.Hkv, tile = blockIdx.x / p.Hkv;
+    if (tile >= p.parts[0].splits) return;
+    const SeqTileParts f = p.parts[1 + tile];
+    if (f.splits == 1) return;
+    const int tid = threadIdx.x, g = tid / 32, c = tid % 32;
+    const int row0 = p.seqs.start(f.seq), rows = min(p.seqs.length(f.seq) * p.G - f.tile * R, R);
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        const int64_t base = ((int64_t)f.unit0 * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY;
-        for (int x = 0; x < f.splits; ++x) mx = max_nan(mx, p.part_l[base + x * each]);
+        for (int x = c; x < f.splits; x += 32) mx = max_nan(mx, p.part_l[base + x * each]);
+#pragma unroll
+        for (int x = 1; x < 32; x <<= 1) mx = max_nan(mx, __shfl_xor(mx, x));
         const float ref = mx == -INFINITY ? 0.f : mx;
-        float sum = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        for (int x = 0; x < f.splits; ++x) {
+        float sum = 0.f, o[C] = {};
+#pragma unroll 4
+        for (int x = g; x < f.splits; x += 8) {
             const float l = p.part_l[base + x * each];
-            if (l == -INFINITY) continue;  // a piece of which this row sees nothing
-            const float w = __builtin_amdgcn_exp2f(l - ref);
+            const float w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);  // (a piece of which this row sees nothing is zero)
+            const float *src = p.part_o + (base + x * each) * D + c * C;
             sum += w;
-            o += w * *reinterpret_cast<const f32x4 *>(p.part_o + (base + x * each) * D + col);
+#pragma unroll
+            for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);
         }
-        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-        const int64_t row = row0 + at / p.G;
-        const int head = kvh * p.G + at % p.G;
-        store4<T>((T *)p.out + (row * p.Hkv * p.G + head) * p.d + col, o * inv);
-        if (p.lse && col == 0) p.lse[(int64_t)head * p.seqs.total + row] = (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+#pragma unroll
+        for (int i = 0; i < C; ++i) sh_o[g][c * C + i] = o[i];
+        if (c == 0) sh_l[g] = sum;
+        __syncthreads();
+        if (tid < D) {
+            float all = 0.f, y = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) all += sh_l[i], y += sh_o[i][tid];
+            const int at = f.tile * R + r;
+            const int64_t row = row0 + at / p.G;
+            const int head = kvh * p.G + at % p.G;
+            if (tid < p.d) ((T *)p.out)[(row * p.Hkv * p.G + head) * p.d + tid] = to_elem<T>(mx == -INFINITY ? 0.f : y / all);
+            if (p.lse && tid == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(all)) * kLn2;
+        }
+        __syncthreads();
     }
 }
 

@@ -9,20 +9,29 @@ namespace ma_host {
 template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how)
 {
     const dim3 grid((unsigned)(how.units * p.Hkv)), block(256);
+    const bool few = how.rows == kSeqFewRows;
     int rc = L.run(kSeqFwd, [&] {
         return launched([&] {
             if (!how.paged)
-                ma::seq_attention<T, D, 1, false, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, 4, false, false><<<grid, block, 0, L.stream>>>(p);
+            else if (!how.split && !few)
+                ma::seq_attention<T, D, 1, 4, true, false><<<grid, block, 0, L.stream>>>(p);
             else if (!how.split)
-                ma::seq_attention<T, D, 1, true, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, 1, true, false><<<grid, block, 0, L.stream>>>(p);
+            else if (!few)
+                ma::seq_attention<T, D, 1, 4, true, true><<<grid, block, 0, L.stream>>>(p);
             else
-                ma::seq_attention<T, D, 1, true, true><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, 1, true, true><<<grid, block, 0, L.stream>>>(p);
         });
     });
     if (rc != MA_OK || !how.split) return rc;
+    const unsigned tiles = (unsigned)((int64_t)p.tiles * p.Hkv);
     return L.run(kSeqJoin, [&] {
         return launched([&] {
-            ma::seq_join<T, D, kSeqRows, sizeof(T) == 4 ? 32 : 64><<<dim3((unsigned)((int64_t)p.tiles * p.Hkv)), block, 0, L.stream>>>(p);
+            if (few)
+                ma::seq_join<T, D, kSeqFewRows><<<dim3(tiles, 8), block, 0, L.stream>>>(p);
+            else
+                ma::seq_join<T, D, kSeqRows><<<dim3(tiles, 16), block, 0, L.stream>>>(p);
         });
     });
 }

@@ -41,12 +41,12 @@ bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb);
 // How a forward call runs.
 struct SeqPlan {
     bool paged, split;
-    int row_blocks;  // 32-row blocks a wave
-    int64_t units;   // workgroups of one key head
+    int rows;       // packed rows a workgroup takes
+    int64_t units;  // workgroups of one key head
 };
 
-// packed rows a workgroup takes, and keys a tile
-constexpr int kSeqRows = 128;
+// packed rows a workgroup takes: usually, and where sequences have few; keys a tile
+constexpr int kSeqRows = 128, kSeqFewRows = 32;
 inline int seq_tile_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }
 
 template <typename T> int run_seq_fwd(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how);

@@ -30,9 +30,16 @@ struct SeqFwd {
     float c;                // s log2(e)
     int causal;
     int tiles;              // row tiles of one key head (an upper bound)
-    // split over the keys: `part` of the units' rows, normalised, and their log2-sum-exp
+    // split over the keys: the units' rows, normalised, and their log2-sum-exp,
+    // and for every row tile what its units are
     float *part_o, *part_l;
+    struct SeqTileParts *parts;
     int target;             // units of one key head to aim at
+};
+
+// parts[0].splits: how many row tiles there are; parts[1 + i]: of tile i, the first of its units.
+struct SeqTileParts {
+    int seq, tile, splits, unit0;
 };
 
 struct SeqBwd {
