@@ -97,7 +97,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     static constexpr int KW = WR == 1 ? BN / 32 : 1;       // waves that share a tile's keys
     static_assert(WR == W || WR == 1, "rows or keys over the waves");
     static constexpr int TILE = BN * S::ROW;
-    static constexpr int LDS_BYTES = 4 * TILE + 16;  // K and V, two of each, from address 0: a copy's target has 16 bits
+    static constexpr int LDS_BYTES = 4 * TILE + 16;  // K and V, two of each
     using Copy = TileCopy<T, D, BN, W>;
     // A row's weights are taken relative to a reference that follows its running
     // maximum only when that has grown by more than 2^kSlack: the sums stay exact
@@ -123,7 +123,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             for (int t = 0; t < KT; ++t) s[rb][t] = f32x16{};
         // (one read of K feeds all RB row blocks)
         const char *x = kt + (lane & 31) * S::ROW;
-        const int flip = (lane >> 5) ^ S::swz(lane & 7);
+        const int flip = (lane >> 5) ^ S::swz(lane & 15);
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -262,7 +262,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         const T *k, *v;    // packed: the sequence's rows; paged: the key head's part of page 0
         const int *table;  // paged: the sequence's pages
         int kv;            // rows from this one on read as zero
-        int off_k, off_v;
+        Copy ck, cv;
         int page[Copy::COPIES];  // paged: of the tile that is copied next
 
         // the pages of the tile from key0 on (a tile ahead of their use)
@@ -285,13 +285,13 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
                     const int pg = uniform(page[i]);
                     const bool ok = (unsigned)pg < (unsigned)p.pages;
                     const int64_t at = ok ? (((int64_t)pg * p.Hkv << p.page_log2) + (key & ((1 << p.page_log2) - 1))) * p.d : 0;
-                    Copy::copy(Copy::source(ok ? (const void *)(k + at) : &kNanRows, kv - key, ld), off_k, kt, i, wave);
-                    Copy::copy(Copy::source(v + at, ok ? kv - key : 0, ld), off_k, vt, i, wave);
+                    ck.one(ok ? (const void *)(k + at) : &kNanRows, min(kv - key, Copy::RPC), ld, kt, i, wave);
+                    ck.one(v + at, ok ? min(kv - key, Copy::RPC) : 0, ld, vt, i, wave);
                 }
             } else {
                 const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
-                Copy::tile(k + key0 * p.ldk, kv - key0, ldk, off_k, kt, wave);
-                Copy::tile(v + key0 * p.ldv, kv - key0, ldv, off_v, vt, wave);
+                ck.tile(k + key0 * p.ldk, kv - key0, ldk, kt, wave);
+                cv.tile(v + key0 * p.ldv, kv - key0, ldv, vt, wave);
             }
         }
     };
@@ -358,13 +358,13 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             src.k = (const T *)p.k + ((int64_t)kvh << p.page_log2) * p.d;
             src.v = (const T *)p.v + ((int64_t)kvh << p.page_log2) * p.d;
             src.table = p.table + (int64_t)seq * p.blocks;
-            src.off_k = Copy::offset(p.d * (int)sizeof(T), p.d, wave, lane);
+            src.ck.init(p.d * (int)sizeof(T), p.d, wave, lane);
         } else {
             const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
             src.k = (const T *)p.k + row0 * p.ldk + kvh * p.d;
             src.v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
-            src.off_k = Copy::offset(ldk, p.d, wave, lane) + Copy::row(0, wave) * ldk;
-            src.off_v = Copy::offset(ldv, p.d, wave, lane) + Copy::row(0, wave) * ldv;
+            src.ck.init(ldk, p.d, wave, lane);
+            src.cv.init(ldv, p.d, wave, lane);
         }
 
         State st;
@@ -467,7 +467,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 };
 
 template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void seq_attention(SeqFwd p)
+__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64) ? 1 : 2) void seq_attention(SeqFwd p)
 {
     using U = SeqAttn<T, D, RB, WR, PAGED, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];

@@ -8,7 +8,7 @@
 // A row that sees one key has the weight 1 whatever the score: its dS is zero,
 // which dP - delta would give up to rounding only.
 //
-// Three launches: the row statistics; dK and dV, a workgroup per 128 keys that
+// Three launches: the row statistics; dK and dV, a workgroup per 64 keys (32 in fp32) that
 // walks the query rows; dQ, a workgroup per 128 packed rows that walks the
 // keys.  The scores and dP are formed twice (7 products instead of 5), so that
 // each sum has one owner that adds in a fixed order in fp32 registers: no
@@ -191,12 +191,13 @@ template <typename T, int D> struct SeqBwdQ {
 
         const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
         const T *k = (const T *)p.k + row0 * p.ldk + kvh * p.d, *v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
-        const int off_k = Copy::offset(ldk, p.d, wave, lane) + Copy::row(0, wave) * ldk;
-        const int off_v = Copy::offset(ldv, p.d, wave, lane) + Copy::row(0, wave) * ldv;
+        Copy ck, cv;
+        ck.init(ldk, p.d, wave, lane);
+        cv.init(ldv, p.d, wave, lane);
         auto bring = [&](int key0, int buf) {
             if (key0 >= last) return;
-            Copy::tile(k + key0 * p.ldk, n - key0, ldk, off_k, lds + 2 * TILE * buf, wave);
-            Copy::tile(v + key0 * p.ldv, n - key0, ldv, off_v, lds + 2 * TILE * buf + TILE, wave);
+            ck.tile(k + key0 * p.ldk, n - key0, ldk, lds + 2 * TILE * buf, wave);
+            cv.tile(v + key0 * p.ldv, n - key0, ldv, lds + 2 * TILE * buf + TILE, wave);
         };
 
         f32x16 dq[1][S::ND];
@@ -223,52 +224,88 @@ template <typename T, int D> struct SeqBwdQ {
     }
 };
 
-// dK and dV: one workgroup per 128 keys of a key head, 32 a wave, whose K and V
-// rows stay in registers as right operands.  It walks the query rows of every
-// head of the group in tiles of BQ; S = Q K^T and dP = dO V^T hold one key a lane, so P and dS
-// feed dV^T += dO^T P and dK^T += Q^T dS from registers.
+// dK and dV: one workgroup per R = 32 KB keys of a key head, whose K and V rows
+// every wave keeps in registers as right operands.  The waves divide the query
+// rows of the group's heads among them in tiles of 32, each with its own copies
+// and without a barrier, and add up their sums at the end.  S = Q K^T and dP = dO V^T hold one key a
+// lane, so P and dS feed dV^T += dO^T P and dK^T += Q^T dS from registers.
+//
+// A tile is read from LDS twice as rows and twice as columns, 32 D bytes each
+// in 16-bit types, for 4 KB 32 x 32 x D products: with one key block a wave
+// (KB = 1) the LDS is busy longer than the matrix pipes, with two it is not.  The price
+// is the registers of a wave per SIMD (K, V, dK and dV of 64 keys: 384 at D = 128).
 template <typename T, int D> struct SeqBwdK {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int W = 4, NTH = 64 * W, R = 32 * W;
-    static constexpr int BQ = S::kF32 ? 32 : 64;
-    static constexpr int TILE = BQ * S::ROW, STATS = 2 * BQ * 4;
-    static constexpr int LDS_BYTES = 4 * TILE + 2 * STATS;
-    using Copy = TileCopy<T, D, BQ, W>;
+    static constexpr int W = S::kF32 && D > 64 ? 2 : 4, NTH = 64 * W, KB = S::kF32 ? 1 : 2, R = 32 * KB;
+    static constexpr int TILE = 32 * S::ROW, STATS = 64 * 4;
+    static constexpr int OWN = 4 * TILE + STATS;  // a wave's: Q and dO, two of each, and a tile's lse and delta
+    static constexpr int LDS_BYTES = W * OWN;
+    using Copy = TileCopy<T, D, 32, 1>;
 
     struct Grads {
-        f32x16 dk[1][S::ND], dv[1][S::ND];
+        f32x16 dk[KB][S::ND], dv[KB][S::ND];
     };
 
-    // `ahead`: first query row of the tile minus this lane's key, `ahead_s`: minus the first row that passes it a gradient
+    // `ahead`: first query row of the tile minus this lane's key of the first
+    // block; rows of the tile before `first` (row 0, which sees one key) pass no gradient to scores
     template <bool MASK>
-    __device__ static void step(const char *qt, const char *gt, const float *stats, const frag *kf, const frag *vf, int ahead,
-                                int ahead_s, float c, float scale, Grads &x, int lane)
+    __device__ static void step(const char *qt, const char *gt, const float *stats, const frag (*kf)[S::NS], const frag (*vf)[S::NS],
+                                int ahead, int first, float c, float scale, Grads &x, int lane)
     {
+        Probs32<T> pf[KB], sf[KB];
 #pragma unroll
-        for (int b = 0; b < BQ / 32; ++b) {
-            f32x16 s = S::scores(qt + b * 32 * S::ROW, kf, lane, f32x16{});
-            f32x16 dp = S::scores(gt + b * 32 * S::ROW, vf, lane, f32x16{});
+        for (int b = 0; b < KB; ++b) {
+            f32x16 s = S::scores(qt, kf[b], lane, f32x16{});
+            f32x16 dp = S::scores(gt, vf[b], lane, f32x16{});
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(stats + 32 * b + 8 * e + 4 * (lane >> 5));
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + BQ + 32 * b + 8 * e + 4 * (lane >> 5));
+                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(stats + 8 * e + 4 * (lane >> 5));
+                const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + 32 + 8 * e + 4 * (lane >> 5));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = 4 * e + i;
+                    const int r = 4 * e + i, at = kRow32(r) + 4 * (lane >> 5) + ahead - 32 * b;  // query row minus key
                     float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2[i]));
-                    if (MASK && 32 * b + kRow32(r) + 4 * (lane >> 5) + ahead < 0) w = 0.f;
+                    if (MASK && at < 0) w = 0.f;
                     float y = w * (dp[r] - delta[i]);
                     if constexpr (BwdScale<T>::kScaled) y *= scale;
                     s[r] = w;
-                    dp[r] = MASK && 32 * b + kRow32(r) + 4 * (lane >> 5) + ahead_s < 0 ? 0.f : y;
+                    dp[r] = MASK && (at < 0 || kRow32(r) + 4 * (lane >> 5) < first) ? 0.f : y;
                 }
             }
-            Probs32<T> pf, sf;
-            pf.pack(s);
-            sf.pack(dp);
-            aggregate<T, D, 1>(gt + b * 32 * S::ROW, &pf, x.dv, lane);
-            aggregate<T, D, 1>(qt + b * 32 * S::ROW, &sf, x.dk, lane);
+            pf[b].pack(s);
+            sf[b].pack(dp);
+            if constexpr (KB > 1) __builtin_amdgcn_sched_barrier(0);  // one block's scores at a time: the registers hold no more
+        }
+        aggregate<T, D, KB>(gt, pf, x.dv, lane);
+        aggregate<T, D, KB>(qt, sf, x.dk, lane);
+    }
+
+    // The waves' sums of one gradient, scaled, to the keys' rows of `out`.
+    __device__ static void add_up(char *lds, const f32x16 (*x)[S::ND], const Span &out, float by, int at, int d, int keys, int wave, int lane)
+    {
+        constexpr int N = KB * S::ND * 16 * 64;  // a wave's values
+        static_assert(W * N * 4 <= LDS_BYTES, "the tiles' room holds them");
+        f32x4 *mine = reinterpret_cast<f32x4 *>(lds) + wave * (N / 4) + lane;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KB * S::ND; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f32x16 &y = x[i / S::ND][i % S::ND];
+                mine[(i * 4 + e) * 64] = f32x4{y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]};
+            }
+        __syncthreads();
+        for (int i = wave; i < KB * S::ND; i += W) {
+            const f32x4 *src = reinterpret_cast<const f32x4 *>(lds) + i * 4 * 64 + lane;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f32x4 sum = src[e * 64];
+#pragma unroll
+                for (int w = 1; w < W; ++w) sum += src[w * (N / 4) + e * 64];
+                const int key = 32 * (i / S::ND) + (lane & 31), col = 32 * (i % S::ND) + 8 * e + 4 * (lane >> 5);
+                out.store<T>(sum * by, (key * at + col) * (int)sizeof(T), key < keys && col < d);
+            }
         }
     }
 
@@ -284,82 +321,89 @@ template <typename T, int D> struct SeqBwdK {
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
         const int k0 = uniform((int)(t - tile0(p.seqs, seq, 1, R)) * R), Hq = p.Hkv * p.G;
 
-        const int key = k0 + wave * 32 + (lane & 31), kc = min(key, n - 1) - k0;
         const Span ks((const T *)p.k + (row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d);
-        frag kf[S::NS], vf[S::NS];
+        frag kf[KB][S::NS], vf[KB][S::NS];
 #pragma unroll
-        for (int i = 0; i < S::NS; ++i) {
-            const int col = (2 * i + (lane >> 5)) * S::V;
-            u32x4 x = ks.load16((kc * (int)p.ldk + col) * (int)sizeof(T), col < p.d);
-            __builtin_memcpy(&kf[i], &x, 16);
-            x = vs.load16((kc * (int)p.ldv + col) * (int)sizeof(T), col < p.d);
-            __builtin_memcpy(&vf[i], &x, 16);
+        for (int b = 0; b < KB; ++b) {
+            const int kc = min(32 * b + (lane & 31), n - 1 - k0);
+#pragma unroll
+            for (int i = 0; i < S::NS; ++i) {
+                const int col = (2 * i + (lane >> 5)) * S::V;
+                u32x4 x = ks.load16((kc * (int)p.ldk + col) * (int)sizeof(T), col < p.d);
+                __builtin_memcpy(&kf[b][i], &x, 16);
+                x = vs.load16((kc * (int)p.ldv + col) * (int)sizeof(T), col < p.d);
+                __builtin_memcpy(&vf[b][i], &x, 16);
+            }
         }
 
-        float *stats = reinterpret_cast<float *>(lds + 4 * TILE);
+        char *own = lds + wave * OWN;
+        float *stats = reinterpret_cast<float *>(own + 4 * TILE);
         const int ldq = (int)p.ldq * (int)sizeof(T), ldg = Hq * p.d * (int)sizeof(T);
-        const int off_q = Copy::offset(ldq, p.d, wave, lane) + Copy::row(0, wave) * ldq;
-        const int off_g = Copy::offset(ldg, p.d, wave, lane) + Copy::row(0, wave) * ldg;
-        const int from = p.causal ? k0 / BQ * BQ : 0;  // first query row that sees a key of the tile
-        float stat = 0.f;  // threads 0..BQ-1: lse of a row of the next tile, BQ..2 BQ-1: delta
-        auto bring = [&](int g, int q0, int buf) {
-            if (q0 >= n) q0 = from, ++g;
-            if (g >= p.G) return;
-            const int head = kvh * p.G + g;
-            Copy::tile((const T *)p.q + (row0 + q0) * p.ldq + head * p.d, n - q0, ldq, off_q, lds + 2 * TILE * buf, wave);
-            Copy::tile((const T *)p.dout + ((int64_t)(row0 + q0) * Hq + head) * p.d, n - q0, ldg, off_g, lds + 2 * TILE * buf + TILE, wave);
-            if (tid < 2 * BQ) {
-                const int i = tid % BQ;
-                const bool is_lse = tid < BQ;
-                const float none = is_lse ? INFINITY : 0.f;  // a row that is not there has weights of zero
-                stat = q0 + i < n ? (is_lse ? p.lse2 : p.delta)[(int64_t)head * p.seqs.total + row0 + q0 + i] : none;
-                if (is_lse) stat -= BwdScale<T>::kP;
-            }
+        Copy cq, cg;
+        cq.init(ldq, p.d, 0, lane);
+        cg.init(ldg, p.d, 0, lane);
+        // The query tiles that see keys of this workgroup: of every head, first the
+        // `part` ones that see some of them, then the others.
+        const int from = p.causal ? k0 / 32 : 0, tiles = (n + 31) / 32 - from;
+        const int part = p.causal ? min(KB, tiles) : 0;
+        const int parts = p.G * part, all = p.G * tiles;
+        float stat = 0.f;  // lanes 0..31: lse of a row of the next tile, 32..63: delta
+        auto place = [&](int i, int &head, int &q0) {
+            const int j = i < parts ? i : i - parts, each = i < parts ? part : tiles - part;
+            const int g = j / each;
+            head = uniform(kvh * p.G + g);
+            q0 = uniform((from + (i < parts ? 0 : part) + j - g * each) * 32);
         };
-        auto keep = [&](int buf) {
-            if (tid < 2 * BQ) stats[buf * 2 * BQ + tid] = stat;
+        auto bring = [&](int i, int buf) {
+            if (i >= all) return;
+            int head, q0;
+            place(i, head, q0);
+            cq.tile((const T *)p.q + (row0 + q0) * p.ldq + head * p.d, n - q0, ldq, own + 2 * TILE * buf, 0);
+            cg.tile((const T *)p.dout + ((int64_t)(row0 + q0) * Hq + head) * p.d, n - q0, ldg, own + 2 * TILE * buf + TILE, 0);
+            const int r = q0 + (lane & 31);
+            // (a row that is not there has weights of zero)
+            stat = r < n ? (lane < 32 ? p.lse2 : p.delta)[(int64_t)head * p.seqs.total + row0 + r] : lane < 32 ? INFINITY : 0.f;
+            if (lane < 32) stat -= BwdScale<T>::kP;
         };
 
         Grads x;
 #pragma unroll
-        for (int dt = 0; dt < S::ND; ++dt) x.dk[0][dt] = x.dv[0][dt] = f32x16{};
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt) x.dk[b][dt] = x.dv[b][dt] = f32x16{};
         const float scale = BwdScale<T>::kScaled ? sc.ds * 0x1p-14f : 1.f;
-        bring(0, from, 0);
-        keep(0);
-        int buf = 0;
+        bring(wave, 0);
+        int i = wave, buf = 0;
 #pragma unroll 1
-        for (int g = 0; g < p.G; ++g) {
-            int q0 = from;
-#pragma unroll 1
-            for (; q0 < n && p.causal && q0 < k0 + R - 1; q0 += BQ, buf ^= 1) {
-                tile_barrier();
-                bring(g, q0 + BQ, buf ^ 1);
-                step<true>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, stats + buf * 2 * BQ, kf, vf, q0 - key, q0 - max(key, 1), p.c, scale, x, lane);
-                keep(buf ^ 1);
-            }
-#pragma unroll 1
-            for (; q0 < n; q0 += BQ, buf ^= 1) {
-                tile_barrier();
-                bring(g, q0 + BQ, buf ^ 1);
-                step<false>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, stats + buf * 2 * BQ, kf, vf, 0, 0, p.c, scale, x, lane);
-                keep(buf ^ 1);
-            }
+        for (; i < parts; i += W, buf ^= 1) {
+            int head, q0;
+            place(i, head, q0);
+            wave_arrived();
+            stats[lane] = stat;
+            bring(i + W, buf ^ 1);
+            step<true>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, stats, kf, vf, q0 - k0 - (lane & 31), 1 - q0, p.c, scale, x, lane);
         }
-        const int at = (key - k0) * p.Hkv * p.d;
+#pragma unroll 1
+        for (; i < all; i += W, buf ^= 1) {
+            wave_arrived();
+            stats[lane] = stat;
+            bring(i + W, buf ^ 1);
+            step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, stats, kf, vf, 0, 0, p.c, scale, x, lane);
+        }
         const int64_t out0 = ((int64_t)(row0 + k0) * p.Hkv + kvh) * p.d;
-        store_transposed<T, S::ND>(Span((T *)p.dk + out0), x.dk[0], n == 1 ? 0.f : p.c * kLn2 / sc.ds, at, p.d, key < n, lane);
-        store_transposed<T, S::ND>(Span((T *)p.dv + out0), x.dv[0], BwdScale<T>::kScaled ? 0x1p-14f : 1.f, at, p.d, key < n, lane);
+        add_up(lds, x.dk, Span((T *)p.dk + out0), n == 1 ? 0.f : p.c * kLn2 / sc.ds, p.Hkv * p.d, p.d, n - k0, wave, lane);
+        add_up(lds, x.dv, Span((T *)p.dv + out0), BwdScale<T>::kScaled ? 0x1p-14f : 1.f, p.Hkv * p.d, p.d, n - k0, wave, lane);
     }
 };
 
-template <typename T, int D> __global__ __launch_bounds__(256, 2) void seq_bwd_q(SeqBwd p)
+template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd_q(SeqBwd p)
 {
     using U = SeqBwdQ<T, D>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
 }
 
-template <typename T, int D> __global__ __launch_bounds__(256, D == 64 && sizeof(T) == 2 ? 2 : 1) void seq_bwd_k(SeqBwd p)
+template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), 1) void seq_bwd_k(SeqBwd p)
 {
     using U = SeqBwdK<T, D>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];

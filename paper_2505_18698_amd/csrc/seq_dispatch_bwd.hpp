@@ -14,7 +14,7 @@ template <typename T, int D> int run_seq_bwd_d(Launcher &L, const ma::SeqBwd &p)
     });
     if (rc != MA_OK) return rc;
     rc = L.run(kSeqBwdK, [&] {
-        return launched([&] { ma::seq_bwd_k<T, D><<<dim3((unsigned)((int64_t)p.tiles_k * p.Hkv)), block, 0, L.stream>>>(p); });
+        return launched([&] { ma::seq_bwd_k<T, D><<<dim3((unsigned)((int64_t)p.tiles_k * p.Hkv)), dim3(ma::SeqBwdK<T, D>::NTH), 0, L.stream>>>(p); });
     });
     if (rc != MA_OK) return rc;
     return L.run(kSeqBwdQ, [&] {

@@ -38,9 +38,12 @@ template <> struct Mma32<float> {
 __device__ constexpr int kRow32(int r) { return 8 * (r / 4) + r % 4; }
 
 // A row-major LDS tile of rows of D elements in 16-byte chunks, PC chunks a
-// row.  Chunk c of row r lies at c ^ swz(r): the 8 rows that one pass of a
-// 16-byte read takes from the same column fall on 8 different bank groups, and
-// so do the two halves of the 4 rows that a transposing read takes.
+// row.  Chunk c of row r lies at c ^ swz(r).  The LDS has 64 banks of 4 bytes,
+// 16 chunks: a pass of a 16-byte read takes one column of 16 rows, all different
+// modulo 16; of a transposing read, 4 columns of 4 consecutive rows; of a
+// 4-byte read, 8 columns of the rows r and r + 4.  swz puts each on 16 different
+// chunks of banks.  (With 8 different ones, c ^ f(r % 8), the counters showed 4 cycles more
+// for each 16-byte read and 2 for each transposing one.)
 template <typename T, int D> struct SeqTile {
     static constexpr int V = 16 / (int)sizeof(T);           // elements a chunk
     static constexpr int PC = D * (int)sizeof(T) <= 128 ? 8 : D * (int)sizeof(T) <= 256 ? 16 : 32;
@@ -51,14 +54,19 @@ template <typename T, int D> struct SeqTile {
     using M = Mma32<T>;
     using frag = typename M::frag;
 
-    __device__ static int swz(int row) { return ((row & 1) << 2) | ((row >> 1) & 3); }
+    __device__ static int swz(int row)
+    {
+        if constexpr (kF32) return ((row >> 2) & 1) << 3 | (row & 3) << 1 | ((row >> 3) & 1);
+        else if constexpr (PC == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);  // (two rows to the 64 banks)
+        else return (row & 3) << 2 | ((row >> 2) & 3);
+    }
 
     // acc += X Y^T of the tile's 32 rows from `rows` on and 32 rows Y held as
     // operand fragments (lane 32 h + c: row c, chunks 2 st + h).
     __device__ static f32x16 scores(const char *rows, const frag *y, int lane, f32x16 acc)
     {
         const char *x = rows + (lane & 31) * ROW;
-        const int flip = (lane >> 5) ^ swz(lane & 7);
+        const int flip = (lane >> 5) ^ swz(lane & 15);
 #pragma unroll
         for (int st = 0; st < NS; ++st)
             acc = M::mma(*reinterpret_cast<const frag *>(x + ((2 * st) ^ flip) * 16), y[st], acc);
@@ -71,9 +79,9 @@ template <typename T, int D> struct SeqTile {
     {
         const int j = lane & 15, r = 4 * (lane >> 5) + (j >> 2);
         const int chunk = 4 * dt + 2 * ((lane >> 4) & 1) + ((j >> 1) & 1);
-        const char *x = rows + r * ROW + ((chunk ^ swz(r)) * 16) + (j & 1) * 8;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x + 8 * ROW));
+        const char *x = rows + r * ROW + (j & 1) * 8;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x + ((chunk ^ swz(r)) * 16)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(x + 8 * ROW + ((chunk ^ swz(r + 8)) * 16)));
         frag f;
         __builtin_memcpy(&f, &lo, 8);
         __builtin_memcpy((char *)&f + 8, &hi, 8);
@@ -160,16 +168,20 @@ static __device__ __align__(16) const struct NanRows { uint32_t x[256]; } kNanRo
 template <typename T, int D, int BN, int NW> struct TileCopy {
     using S = SeqTile<T, D>;
     static constexpr int RPC = 64 / S::PC, COPIES = BN / RPC / NW;
-    static_assert(COPIES * NW * RPC == BN && NW * RPC % 8 == 0, "whole copies, one column a lane");
+    static constexpr int VAR = NW * RPC >= 16 ? 1 : 16 / (NW * RPC);  // copies after which a lane's column comes again
+    static_assert(COPIES * NW * RPC == BN && COPIES % VAR == 0, "whole copies");
+    int off[VAR];  // this lane's chunk, from the first row of the copy
 
+    __device__ void init(int ld, int d, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < VAR; ++i) {
+            const int r = lane / S::PC, col = ((lane % S::PC) ^ S::swz((row(i, wave) + r) & 15)) * S::V;
+            off[i] = col < d ? r * ld + col * (int)sizeof(T) : (int)0x80000000;
+        }
+    }
     // first row of copy i in the tile
     __device__ static int row(int i, int wave) { return (i * NW + wave) * RPC; }
-    // byte offset of this lane's chunk from the first row of the wave's copies
-    __device__ static int offset(int ld, int d, int wave, int lane)
-    {
-        const int r = lane / S::PC, col = ((lane % S::PC) ^ S::swz((wave * RPC + r) & 7)) * S::V;
-        return col < d ? r * ld + col * (int)sizeof(T) : (int)0x80000000;
-    }
     // the descriptor of a buffer access that reads zero behind `valid` rows
     __device__ static u32x4 source(const void *rows, int valid, int ld)
     {
@@ -179,7 +191,7 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
     // The copy itself, in assembly: behind the builtin the compiler waits for it
     // before every later LDS read, those of the other tiles among them, so that
     // a tile would not arrive while another is computed.  The instruction writes LDS and
-    // no register; tile_barrier() waits for it.
+    // no register; tile_barrier() or wave_arrived() waits for it.
     // (The compiler does not see into it either: the five wait states are
     // those between a vector write of a scalar register and its use here.)
     __device__ static void copy(u32x4 r, int off, char *tile, int i, int wave)
@@ -188,12 +200,25 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                      :: "v"(off), "s"(r), "s"(uniform(to)) : "memory", "m0");
     }
-    // the whole tile; `rows`: its first row, `off`: offset() of the wave's first row in it
-    __device__ static void tile(const void *rows, int valid, int ld, int off, char *to, int wave)
+    // copy i alone, from its own first row
+    __device__ void one(const void *rows, int valid, int ld, char *to, int i, int wave) const
     {
-        const u32x4 r = source(rows, valid, ld);
+        copy(source(rows, valid, ld), off[i % VAR], to, i, wave);
+    }
+    // the whole tile from its first row.  With one wave a tile the addresses that differ from copy to
+    // copy stay in scalar registers (the user of those has no others left), else in the lanes'.
+    __device__ void tile(const void *rows, int valid, int ld, char *to, int wave) const
+    {
+        if constexpr (NW == 1) {
+            const int64_t at = uniform((int64_t)rows);
+            valid = uniform(valid);
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy(r, off + i * NW * RPC * ld, to, i, wave);
+            for (int i = 0; i < COPIES; ++i) one((const void *)(at + (int64_t)row(i, 0) * ld), valid - row(i, 0), ld, to, i, 0);
+        } else {
+            const u32x4 r = source(rows, valid, ld);
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) copy(r, off[i % VAR] + row(i, wave) * ld, to, i, wave);
+        }
     }
 };
 
@@ -202,6 +227,9 @@ __device__ inline void tile_barrier()
 {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+
+// Every copy and load of this wave has arrived.
+__device__ inline void wave_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Whether `x` holds on some thread of a workgroup of NTH (`shared`: NTH / 64 integers of LDS).
 template <int NTH> __device__ inline bool some_thread(bool x, int *shared)
