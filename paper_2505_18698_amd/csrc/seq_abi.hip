@@ -184,7 +184,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
     MA_TRY(check_stride("ldk", ldk, Hkv * d, dtype));
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
-    const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, kSeqRows), tiles_k = tiles_of(total, 1, B, seq_bwd_keys(dtype));
+    const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, kSeqRows), tiles_k = tiles_of(total, 1, B, kSeqBwdKeys);
     MA_TRY(check_grid(std::max(tiles_q, tiles_k), Hkv));
     if (B == 0 || total == 0) return MA_OK;
     const size_t qb = span_bytes(total, Hq * d, Hq * d, dtype), kb = span_bytes(total, Hkv * d, Hkv * d, dtype);

@@ -121,17 +121,25 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int t = 0; t < KT; ++t) s[rb][t] = f32x16{};
-        // (one read of K feeds all RB row blocks)
-        const char *x = kt + (lane & 31) * S::ROW;
-        const int flip = (lane >> 5) ^ S::swz(lane & 15);
+        // (one read of K or V feeds all RB row blocks)
+        constexpr int NK = KT * S::NS, NV = S::kF32 ? KT * 16 * S::ND : KT * 2 * S::ND, AHEAD = 4;
+        FragStream<frag, S::kF32 ? NK : NK + NV, AHEAD> stream;
+        auto load = [&](int u) {
+            if constexpr (!S::kF32)
+                if (u >= NK) return S::columns(vt + (u - NK) / S::ND * 16 * S::ROW, (u - NK) % S::ND, lane);
+            return S::row_frag(kt + u / S::NS * 32 * S::ROW, u % S::NS, lane);
+        };
+        auto reads = [&](int u) { return u + AHEAD < NK ? 1 : S::kF32 || u + AHEAD >= NK + NV ? 0 : 2; };
+        stream.start(load);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, AHEAD, 0);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+        for (int u = 0; u < NK; ++u) {
+            stream.next(u, load, [&](const frag &x) {
 #pragma unroll
-            for (int i = 0; i < S::NS; ++i) {
-                const frag a = *reinterpret_cast<const frag *>(x + t * 32 * S::ROW + ((2 * i) ^ flip) * 16);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) s[rb][t] = S::M::mma(a, qf[rb][i], s[rb][t]);
-            }
+                for (int rb = 0; rb < RB; ++rb) s[rb][u / S::NS] = S::M::mma(x, qf[rb][u % S::NS], s[rb][u / S::NS]);
+            });
+            sched_step<RB * (S::kF32 ? 4 : 1)>(reads(u));
+        }
         Probs32<T> pf[KT][RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -167,19 +175,47 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             }
             st.sum[rb] += sum;
         }
+        if constexpr (S::kF32) {
+            add_columns(vt, pf, st, lane);
+        } else {
 #pragma unroll
-        for (int t = 0; t < KT; ++t) aggregate<T, D, RB>(vt + t * 32 * S::ROW, pf[t], st.o, lane);
+            for (int u = NK; u < NK + NV; ++u) {
+                const int ks = (u - NK) / S::ND, dt = (u - NK) % S::ND;
+                stream.next(u, load, [&](const frag &x) {
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = S::M::mma(x, pf[ks / 2][rb].f[ks % 2], st.o[rb][dt]);
+                });
+                sched_step<RB>(reads(u));
+            }
+        }
         if constexpr (MASK && !S::kF32) {
             if (fine) {
 #pragma unroll
-                for (int t = 0; t < KT; ++t) {
-                    Probs32<T> low[RB];
+                for (int t = 0; t < KT; ++t)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) low[rb] = pf[t][rb].rest(s[rb][t]);
-                    aggregate<T, D, RB>(vt + t * 32 * S::ROW, low, st.o, lane);
-                }
+                    for (int rb = 0; rb < RB; ++rb) pf[t][rb] = pf[t][rb].rest(s[rb][t]);
+                add_columns(vt, pf, st, lane);
             }
         }
+    }
+
+    // O^T += V^T P^T of a tile.
+    __device__ static void add_columns(const char *vt, const Probs32<T> (*pf)[RB], State &st, int lane)
+    {
+#pragma unroll
+        for (int k = 0; k < KT * (S::kF32 ? 16 : 2); ++k)
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt) {
+                if constexpr (S::kF32) {
+                    const float x = S::element(vt, 32 * (k / 16) + kRow32(k % 16) + 4 * (lane >> 5), dt, lane);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, pf[k / 16][rb].s[k % 16], st.o[rb][dt], 0, 0, 0);
+                } else {
+                    const frag x = S::columns(vt + k * 16 * S::ROW, dt, lane);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = S::M::mma(x, pf[k / 2][rb].f[k % 2], st.o[rb][dt]);
+                }
+            }
     }
 
     // A value of V that is not finite meets weights of zero in the rows of a masked

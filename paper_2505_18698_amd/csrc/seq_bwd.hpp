@@ -8,7 +8,7 @@
 // A row that sees one key has the weight 1 whatever the score: its dS is zero,
 // which dP - delta would give up to rounding only.
 //
-// Three launches: the row statistics; dK and dV, a workgroup per 64 keys (32 in fp32) that
+// Three launches: the row statistics; dK and dV, a workgroup per 64 keys that
 // walks the query rows; dQ, a workgroup per 128 packed rows that walks the
 // keys.  The scores and dP are formed twice (7 products instead of 5), so that
 // each sum has one owner that adds in a fixed order in fp32 registers: no
@@ -27,20 +27,19 @@ template <typename T> struct BwdScale {
     static constexpr bool kScaled = std::is_same<T, _Float16>::value;
     static constexpr float kP = kScaled ? 14.f : 0.f;  // log2
     float ds = 1.f;                                    // of dS
-    __device__ void find(const SeqBwd &p, char *lds)
+    template <int NTH> __device__ void find(const SeqBwd &p, char *lds)
     {
         if constexpr (kScaled) {
             float a = 0.f, b = 0.f;
-            for (int i = threadIdx.x; i < p.norm_blocks; i += 256) {
+            for (int i = threadIdx.x; i < p.norm_blocks; i += NTH) {
                 const float2 x = p.norms[i];
                 a = fmaxf(a, x.x), b = fmaxf(b, x.y);
             }
             for (int x = 1; x < 64; x <<= 1) a = fmaxf(a, __shfl_xor(a, x)), b = fmaxf(b, __shfl_xor(b, x));
             float *sh = reinterpret_cast<float *>(lds);
-            if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = a, sh[4 + threadIdx.x / 64] = b;
+            if (threadIdx.x % 64 == 0) sh[threadIdx.x / 32] = a, sh[threadIdx.x / 32 + 1] = b;
             __syncthreads();
-            a = fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-            b = fmaxf(fmaxf(sh[4], sh[5]), fmaxf(sh[6], sh[7]));
+            for (int i = 0; i < NTH / 64; ++i) a = fmaxf(a, sh[2 * i]), b = fmaxf(b, sh[2 * i + 1]);
             __syncthreads();
             const float most = 2.f * sqrtf(a) * sqrtf(b);
             const int e = most > 0.f ? 14 - ilogbf(most) : 0;
@@ -139,12 +138,31 @@ template <typename T, int D> struct SeqBwdQ {
 
     template <bool MASK>
     __device__ static void step(const char *kt, const char *vt, const frag *qf, const frag *gf, int see, float c, float lse2,
-                                float delta, float scale, f32x16 (*dq)[S::ND], int lane)
+                                float delta, float scale, f32x16 *dq, int lane)
     {
+        // fragments of a 32-key part: the rows of K, the rows of V, the columns of K
+        constexpr int NA = S::kF32 ? 0 : 2 * S::ND, NP = 2 * S::NS + NA, N = KT * NP, AHEAD = 4;
+        FragStream<frag, N, AHEAD> stream;
+        auto load = [&](int u) {
+            const int off = u / NP * 32 * S::ROW, i = u % NP;
+            if constexpr (!S::kF32)
+                if (i >= 2 * S::NS) return S::columns(kt + off + (i - 2 * S::NS) / S::ND * 16 * S::ROW, (i - 2 * S::NS) % S::ND, lane);
+            return S::row_frag((i < S::NS ? kt : vt) + off, i % S::NS, lane);
+        };
+        auto reads = [&](int u) { return u + AHEAD >= N ? 0 : (u + AHEAD) % NP >= 2 * S::NS ? 2 : 1; };
+        stream.start(load);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, AHEAD, 0);
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
-            f32x16 s = S::scores(kt + t * 32 * S::ROW, qf, lane, f32x16{});
-            const f32x16 dp = S::scores(vt + t * 32 * S::ROW, gf, lane, f32x16{});
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int i = 0; i < 2 * S::NS; ++i) {
+                stream.next(t * NP + i, load, [&](const frag &x) {
+                    if (i < S::NS) s = S::M::mma(x, qf[i], s);
+                    else dp = S::M::mma(x, gf[i - S::NS], dp);
+                });
+                sched_step<(S::kF32 ? 4 : 1)>(reads(t * NP + i));
+            }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2));
@@ -154,7 +172,20 @@ template <typename T, int D> struct SeqBwdQ {
             }
             Probs32<T> pf;
             pf.pack(s);
-            aggregate<T, D, 1>(kt + t * 32 * S::ROW, &pf, dq, lane);
+            if constexpr (S::kF32) {
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        dq[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(S::element(kt, 32 * t + kRow32(r) + 4 * (lane >> 5), dt, lane), pf.s[r], dq[dt], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 2 * S::NS; i < NP; ++i) {
+                    const int ks = (i - 2 * S::NS) / S::ND, dt = (i - 2 * S::NS) % S::ND;
+                    stream.next(t * NP + i, load, [&](const frag &x) { dq[dt] = S::M::mma(x, pf.f[ks], dq[dt]); });
+                    sched_step<1>(reads(t * NP + i));
+                }
+            }
         }
     }
 
@@ -162,7 +193,7 @@ template <typename T, int D> struct SeqBwdQ {
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         BwdScale<T> sc;
-        sc.find(p, lds);
+        sc.template find<NTH>(p, lds);
         const int kvh = uniform((int)(blockIdx.x % p.Hkv));
         const int64_t t = p.tiles_q - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
         const int seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
@@ -200,9 +231,9 @@ template <typename T, int D> struct SeqBwdQ {
             cv.tile(v + key0 * p.ldv, n - key0, ldv, lds + 2 * TILE * buf + TILE, wave);
         };
 
-        f32x16 dq[1][S::ND];
+        f32x16 dq[S::ND];
 #pragma unroll
-        for (int dt = 0; dt < S::ND; ++dt) dq[0][dt] = f32x16{};
+        for (int dt = 0; dt < S::ND; ++dt) dq[dt] = f32x16{};
         bring(0, 0);
         int key0 = 0, buf = 0;
 #pragma unroll 1
@@ -220,100 +251,146 @@ template <typename T, int D> struct SeqBwdQ {
                            delta, sc.ds, dq, lane);
         }
         const Span os((T *)p.dq + (int64_t)(row0 + tok0) * Hq * p.d);
-        store_transposed<T, S::ND>(os, dq[0], vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, r0 + wave * 32 + (lane & 31) < rows, lane);
+        store_transposed<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, r0 + wave * 32 + (lane & 31) < rows, lane);
     }
 };
 
-// dK and dV: one workgroup per R = 32 KB keys of a key head, whose K and V rows
-// every wave keeps in registers as right operands.  The waves divide the query
-// rows of the group's heads among them in tiles of 32, each with its own copies
-// and without a barrier, and add up their sums at the end.  S = Q K^T and dP = dO V^T hold one key a
-// lane, so P and dS feed dV^T += dO^T P and dK^T += Q^T dS from registers.
+// dK and dV: one workgroup per R = 64 keys of a key head, which walks the query
+// rows of the group's heads in tiles of 32 NQ.  Wave (kb, qb) takes key block kb
+// and the tile's rows 32 qb on; the NQ sums of a key block are added up at the end.
+// S = Q K^T and dP = dO V^T hold one key a lane, so P and dS feed
+// dV^T += dO^T P and dK^T += Q^T dS from registers.
 //
-// A tile is read from LDS twice as rows and twice as columns, 32 D bytes each
-// in 16-bit types, for 4 KB 32 x 32 x D products: with one key block a wave
-// (KB = 1) the LDS is busy longer than the matrix pipes, with two it is not.  The price
-// is the registers of a wave per SIMD (K, V, dK and dV of 64 keys: 384 at D = 128).
+// A key block is 32 keys, so that K, dK and dV of it leave room for a second
+// wave on the SIMD (past D = 64 with V read from LDS); of 64 keys they take all registers, and
+// what does not fit goes through memory (530 us on 9550 packed tokens of 16
+// heads on 4; XXX us so).  Few keys and many rows a workgroup, because the
+// longest walk, that of a long sequence's first keys, bounds the call.
 template <typename T, int D> struct SeqBwdK {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int W = S::kF32 && D > 64 ? 2 : 4, NTH = 64 * W, KB = S::kF32 ? 1 : 2, R = 32 * KB;
-    static constexpr int TILE = 32 * S::ROW, STATS = 64 * 4;
-    static constexpr int OWN = 4 * TILE + STATS;  // a wave's: Q and dO, two of each, and a tile's lse and delta
-    static constexpr int LDS_BYTES = W * OWN;
-    using Copy = TileCopy<T, D, 32, 1>;
+    static constexpr int NK = 2, NQ = S::ROW <= 256 ? 4 : 2, W = NK * NQ, NTH = 64 * W, R = 32 * NK;
+    static constexpr int BQ = 32 * NQ, TILE = BQ * S::ROW, STATS = 2 * BQ * 4;
+    static constexpr bool kVInLds = !S::kF32 && D > 64;
+    static constexpr int LDS_BYTES = 4 * TILE + 2 * STATS + (kVInLds ? R * S::ROW : 0);
+    using Copy = TileCopy<T, D, BQ, W>;
 
     struct Grads {
-        f32x16 dk[KB][S::ND], dv[KB][S::ND];
+        f32x16 dk[S::ND], dv[S::ND];
     };
 
-    // `ahead`: first query row of the tile minus this lane's key of the first
-    // block; rows of the tile before `first` (row 0, which sees one key) pass no gradient to scores
+    // 32 rows of Q and dO (qt, gt), their lse and delta.  `ahead`: the first of them minus
+    // this lane's key; rows before `first` (row 0, which sees one key) pass no gradient to scores.
+    // vt: the key block's V rows in LDS, where they are there.
     template <bool MASK>
-    __device__ static void step(const char *qt, const char *gt, const float *stats, const frag (*kf)[S::NS], const frag (*vf)[S::NS],
-                                int ahead, int first, float c, float scale, Grads &x, int lane)
+    __device__ static void step(const char *qt, const char *gt, const float *lse2, const float *delta, const frag *kf, const frag *vf,
+                                const char *vt, int ahead, int first, float c, float scale, Grads &x, int lane)
     {
-        Probs32<T> pf[KB], sf[KB];
-#pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            f32x16 s = S::scores(qt, kf[b], lane, f32x16{});
-            f32x16 dp = S::scores(gt, vf[b], lane, f32x16{});
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x4 lse2 = *reinterpret_cast<const f32x4 *>(stats + 8 * e + 4 * (lane >> 5));
-                const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + 32 + 8 * e + 4 * (lane >> 5));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = 4 * e + i, at = kRow32(r) + 4 * (lane >> 5) + ahead - 32 * b;  // query row minus key
-                    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse2[i]));
-                    if (MASK && at < 0) w = 0.f;
-                    float y = w * (dp[r] - delta[i]);
-                    if constexpr (BwdScale<T>::kScaled) y *= scale;
-                    s[r] = w;
-                    dp[r] = MASK && (at < 0 || kRow32(r) + 4 * (lane >> 5) < first) ? 0.f : y;
+        // fragments: the rows of Q, then of dO (each with V's behind it), then the columns of dO and of Q
+        constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = D > 96 ? 3 : 4;
+        FragStream<frag, N, AHEAD> stream;
+        auto load = [&](int u) {
+            if constexpr (!S::kF32)
+                if (u >= NR) {
+                    const int i = (u - NR) % NA;
+                    return S::columns((u < NR + NA ? gt : qt) + i / S::ND * 16 * S::ROW, i % S::ND, lane);
                 }
-            }
-            pf[b].pack(s);
-            sf[b].pack(dp);
-            if constexpr (KB > 1) __builtin_amdgcn_sched_barrier(0);  // one block's scores at a time: the registers hold no more
+            const int i = (u - S::NS) / NV;
+            return u < S::NS ? S::row_frag(qt, u, lane) : S::row_frag((u - S::NS) % NV ? vt : gt, i, lane);
+        };
+        auto reads = [&](int u) { return u + AHEAD >= N ? 0 : u + AHEAD >= NR ? 2 : 1; };
+        stream.start(load);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, AHEAD, 0);
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int u = 0; u < S::NS; ++u) {
+            stream.next(u, load, [&](const frag &y) { s = S::M::mma(y, kf[u], s); });
+            sched_step<(S::kF32 ? 4 : 1)>(reads(u));
         }
-        aggregate<T, D, KB>(gt, pf, x.dv, lane);
-        aggregate<T, D, KB>(qt, sf, x.dk, lane);
+#pragma unroll
+        for (int i = 0; i < S::NS; ++i) {
+            const int u = S::NS + i * NV;
+            frag g;
+            stream.next(u, load, [&](const frag &y) { g = y; });
+            if constexpr (kVInLds) {
+                stream.next(u + 1, load, [&](const frag &y) { dp = S::M::mma(g, y, dp); });
+                sched_step<1>(u + 1 + AHEAD >= NR ? 2 : 1);
+            } else {
+                dp = S::M::mma(g, vf[i], dp);
+                sched_step<(S::kF32 ? 4 : 1)>(reads(u));
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x4 l = *reinterpret_cast<const f32x4 *>(lse2 + 8 * e + 4 * (lane >> 5));
+            const f32x4 del = *reinterpret_cast<const f32x4 *>(delta + 8 * e + 4 * (lane >> 5));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * e + i, row = kRow32(r) + 4 * (lane >> 5);
+                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -l[i]));
+                if (MASK && row + ahead < 0) w = 0.f;
+                float y = w * (dp[r] - del[i]);
+                if constexpr (BwdScale<T>::kScaled) y *= scale;
+                s[r] = w;
+                dp[r] = MASK && (row + ahead < 0 || row < first) ? 0.f : y;
+            }
+        }
+        Probs32<T> pf, sf;
+        pf.pack(s);
+        sf.pack(dp);
+        if constexpr (S::kF32) {
+#pragma unroll
+            for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int row = kRow32(r) + 4 * (lane >> 5);
+                    x.dv[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(S::element(gt, row, dt, lane), pf.s[r], x.dv[dt], 0, 0, 0);
+                    x.dk[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(S::element(qt, row, dt, lane), sf.s[r], x.dk[dt], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int u = NR; u < N; ++u) {
+                const int i = (u - NR) % NA, ks = i / S::ND, dt = i % S::ND;
+                stream.next(u, load, [&](const frag &y) {
+                    if (u < NR + NA) x.dv[dt] = S::M::mma(y, pf.f[ks], x.dv[dt]);
+                    else x.dk[dt] = S::M::mma(y, sf.f[ks], x.dk[dt]);
+                });
+                sched_step<1>(reads(u));
+            }
+        }
     }
 
     // The waves' sums of one gradient, scaled, to the keys' rows of `out`.
-    __device__ static void add_up(char *lds, const f32x16 (*x)[S::ND], const Span &out, float by, int at, int d, int keys, int wave, int lane)
+    __device__ static void add_up(char *lds, const f32x16 *x, const Span &out, float by, int ld, int d, int keys, int wave, int lane)
     {
-        constexpr int N = KB * S::ND * 16 * 64;  // a wave's values
-        static_assert(W * N * 4 <= LDS_BYTES, "the tiles' room holds them");
-        f32x4 *mine = reinterpret_cast<f32x4 *>(lds) + wave * (N / 4) + lane;
+        constexpr int N = S::ND * 4 * 64;  // a wave's sums, in 4 values
+        static_assert(W * N * 16 <= 4 * TILE, "the tiles' room holds them");
+        f32x4 *mine = reinterpret_cast<f32x4 *>(lds) + wave * N + lane;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < KB * S::ND; ++i)
+        for (int dt = 0; dt < S::ND; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const f32x16 &y = x[i / S::ND][i % S::ND];
-                mine[(i * 4 + e) * 64] = f32x4{y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]};
-            }
+            for (int e = 0; e < 4; ++e) mine[(dt * 4 + e) * 64] = f32x4{x[dt][4 * e], x[dt][4 * e + 1], x[dt][4 * e + 2], x[dt][4 * e + 3]};
         __syncthreads();
-        for (int i = wave; i < KB * S::ND; i += W) {
-            const f32x4 *src = reinterpret_cast<const f32x4 *>(lds) + i * 4 * 64 + lane;
+        for (int i = wave; i < NK * S::ND; i += W) {
+            const int kb = i / S::ND, dt = i % S::ND;
+            const f32x4 *src = reinterpret_cast<const f32x4 *>(lds) + kb * N + dt * 256 + lane;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 f32x4 sum = src[e * 64];
 #pragma unroll
-                for (int w = 1; w < W; ++w) sum += src[w * (N / 4) + e * 64];
-                const int key = 32 * (i / S::ND) + (lane & 31), col = 32 * (i % S::ND) + 8 * e + 4 * (lane >> 5);
-                out.store<T>(sum * by, (key * at + col) * (int)sizeof(T), key < keys && col < d);
+                for (int q = 1; q < NQ; ++q) sum += src[q * NK * N + e * 64];
+                const int key = 32 * kb + (lane & 31), col = 32 * dt + 8 * e + 4 * (lane >> 5);
+                out.store<T>(sum * by, (key * ld + col) * (int)sizeof(T), key < keys && col < d);
             }
         }
     }
 
     __device__ static void run(const SeqBwd &p, char *lds)
     {
-        const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+        const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kb = wave % NK, qb = wave / NK;
         BwdScale<T> sc;
-        sc.find(p, lds);
+        sc.template find<NTH>(p, lds);
         const int kvh = uniform((int)(blockIdx.x % p.Hkv));
         const int64_t t = (int)(blockIdx.x / p.Hkv);  // (earlier keys are seen by more rows: they start first)
         const int seq = uniform(seq_of_tile(p.seqs, t, 1, R, lane));
@@ -322,73 +399,81 @@ template <typename T, int D> struct SeqBwdK {
         const int k0 = uniform((int)(t - tile0(p.seqs, seq, 1, R)) * R), Hq = p.Hkv * p.G;
 
         const Span ks((const T *)p.k + (row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d);
-        frag kf[KB][S::NS], vf[KB][S::NS];
+        const int ldv = (int)p.ldv * (int)sizeof(T), kc = min(32 * kb + (lane & 31), n - 1 - k0);
+        char *vt = lds + 4 * TILE + 2 * STATS;
+        frag kf[S::NS], vf[kVInLds ? 1 : S::NS];
+        if constexpr (kVInLds) {
+            TileCopy<T, D, R, W> cv;
+            cv.init(ldv, p.d, wave, lane);
+            cv.tile((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d, n - k0, ldv, vt, wave);
+        }
 #pragma unroll
-        for (int b = 0; b < KB; ++b) {
-            const int kc = min(32 * b + (lane & 31), n - 1 - k0);
-#pragma unroll
-            for (int i = 0; i < S::NS; ++i) {
-                const int col = (2 * i + (lane >> 5)) * S::V;
-                u32x4 x = ks.load16((kc * (int)p.ldk + col) * (int)sizeof(T), col < p.d);
-                __builtin_memcpy(&kf[b][i], &x, 16);
-                x = vs.load16((kc * (int)p.ldv + col) * (int)sizeof(T), col < p.d);
-                __builtin_memcpy(&vf[b][i], &x, 16);
+        for (int i = 0; i < S::NS; ++i) {
+            const int col = (2 * i + (lane >> 5)) * S::V;
+            u32x4 x = ks.load16((kc * (int)p.ldk + col) * (int)sizeof(T), col < p.d);
+            __builtin_memcpy(&kf[i], &x, 16);
+            if constexpr (!kVInLds) {
+                x = vs.load16(kc * ldv + col * (int)sizeof(T), col < p.d);
+                __builtin_memcpy(&vf[i], &x, 16);
             }
         }
 
-        char *own = lds + wave * OWN;
-        float *stats = reinterpret_cast<float *>(own + 4 * TILE);
+        float *stats = reinterpret_cast<float *>(lds + 4 * TILE);
         const int ldq = (int)p.ldq * (int)sizeof(T), ldg = Hq * p.d * (int)sizeof(T);
         Copy cq, cg;
-        cq.init(ldq, p.d, 0, lane);
-        cg.init(ldg, p.d, 0, lane);
-        // The query tiles that see keys of this workgroup: of every head, first the
-        // `part` ones that see some of them, then the others.
-        const int from = p.causal ? k0 / 32 : 0, tiles = (n + 31) / 32 - from;
-        const int part = p.causal ? min(KB, tiles) : 0;
-        const int parts = p.G * part, all = p.G * tiles;
-        float stat = 0.f;  // lanes 0..31: lse of a row of the next tile, 32..63: delta
-        auto place = [&](int i, int &head, int &q0) {
-            const int j = i < parts ? i : i - parts, each = i < parts ? part : tiles - part;
-            const int g = j / each;
-            head = uniform(kvh * p.G + g);
-            q0 = uniform((from + (i < parts ? 0 : part) + j - g * each) * 32);
+        cq.init(ldq, p.d, wave, lane);
+        cg.init(ldg, p.d, wave, lane);
+        const int from = p.causal ? k0 : 0;  // the first query row that sees a key of this workgroup
+        float stat = 0.f;  // threads 0..BQ-1: lse of a row of the next tile, BQ..2 BQ-1: delta
+        auto bring = [&](int g, int q0, int buf) {
+            if (q0 >= n) q0 = from, ++g;
+            if (g >= p.G) return;
+            const int head = kvh * p.G + g;
+            char *to = lds + 2 * TILE * buf;
+            cq.tile((const T *)p.q + (row0 + q0) * p.ldq + head * p.d, n - q0, ldq, to, wave);
+            cg.tile((const T *)p.dout + ((int64_t)(row0 + q0) * Hq + head) * p.d, n - q0, ldg, to + TILE, wave);
+            if (tid < 2 * BQ) {
+                const int r = q0 + tid % BQ;
+                const bool is_lse = tid < BQ;
+                // (a row that is not there has weights of zero)
+                stat = r < n ? (is_lse ? p.lse2 : p.delta)[(int64_t)head * p.seqs.total + row0 + r] : is_lse ? INFINITY : 0.f;
+                if (is_lse) stat -= BwdScale<T>::kP;
+            }
         };
-        auto bring = [&](int i, int buf) {
-            if (i >= all) return;
-            int head, q0;
-            place(i, head, q0);
-            cq.tile((const T *)p.q + (row0 + q0) * p.ldq + head * p.d, n - q0, ldq, own + 2 * TILE * buf, 0);
-            cg.tile((const T *)p.dout + ((int64_t)(row0 + q0) * Hq + head) * p.d, n - q0, ldg, own + 2 * TILE * buf + TILE, 0);
-            const int r = q0 + (lane & 31);
-            // (a row that is not there has weights of zero)
-            stat = r < n ? (lane < 32 ? p.lse2 : p.delta)[(int64_t)head * p.seqs.total + row0 + r] : lane < 32 ? INFINITY : 0.f;
-            if (lane < 32) stat -= BwdScale<T>::kP;
+        auto keep = [&](int buf) {
+            if (tid < 2 * BQ) stats[buf * 2 * BQ + tid] = stat;
         };
 
         Grads x;
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int dt = 0; dt < S::ND; ++dt) x.dk[b][dt] = x.dv[b][dt] = f32x16{};
+        for (int dt = 0; dt < S::ND; ++dt) x.dk[dt] = x.dv[dt] = f32x16{};
         const float scale = BwdScale<T>::kScaled ? sc.ds * 0x1p-14f : 1.f;
-        bring(wave, 0);
-        int i = wave, buf = 0;
+        bring(0, from, 0);
+        keep(0);
+        int buf = 0;
+        const char *own = lds + 32 * qb * S::ROW, *vrows = vt + 32 * kb * S::ROW;
+        const float *own_stats = stats + 32 * qb;
 #pragma unroll 1
-        for (; i < parts; i += W, buf ^= 1) {
-            int head, q0;
-            place(i, head, q0);
-            wave_arrived();
-            stats[lane] = stat;
-            bring(i + W, buf ^ 1);
-            step<true>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, stats, kf, vf, q0 - k0 - (lane & 31), 1 - q0, p.c, scale, x, lane);
-        }
+        for (int g = 0; g < p.G; ++g) {
+            int q0 = from;
+            if (p.causal) {  // of a head's tiles the first holds rows that see a part of the keys
+                tile_barrier();
+                bring(g, q0 + BQ, buf ^ 1);
+                if (q0 + 32 * qb < n)
+                    step<true>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, own_stats + buf * 2 * BQ, own_stats + buf * 2 * BQ + BQ, kf, vf,
+                               vrows, q0 + 32 * qb - k0 - 32 * kb - (lane & 31), 1 - q0 - 32 * qb, p.c, scale, x, lane);
+                keep(buf ^ 1);
+                q0 += BQ, buf ^= 1;
+            }
 #pragma unroll 1
-        for (; i < all; i += W, buf ^= 1) {
-            wave_arrived();
-            stats[lane] = stat;
-            bring(i + W, buf ^ 1);
-            step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, stats, kf, vf, 0, 0, p.c, scale, x, lane);
+            for (; q0 < n; q0 += BQ, buf ^= 1) {
+                tile_barrier();
+                bring(g, q0 + BQ, buf ^ 1);
+                if (q0 + 32 * qb < n)
+                    step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, own_stats + buf * 2 * BQ, own_stats + buf * 2 * BQ + BQ, kf, vf,
+                                vrows, 0, 0, p.c, scale, x, lane);
+                keep(buf ^ 1);
+            }
         }
         const int64_t out0 = ((int64_t)(row0 + k0) * p.Hkv + kvh) * p.d;
         add_up(lds, x.dk, Span((T *)p.dk + out0), n == 1 ? 0.f : p.c * kLn2 / sc.ds, p.Hkv * p.d, p.d, n - k0, wave, lane);
@@ -403,7 +488,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     U::run(p, lds);
 }
 
-template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), 1) void seq_bwd_k(SeqBwd p)
+template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), (SeqBwdK<T, D>::W / 4)) void seq_bwd_k(SeqBwd p)
 {
     using U = SeqBwdK<T, D>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];

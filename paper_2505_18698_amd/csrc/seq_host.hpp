@@ -47,7 +47,7 @@ struct SeqPlan {
 
 // packed rows a workgroup takes: usually, and where sequences have few; keys a tile
 constexpr int kSeqRows = 128, kSeqFewRows = 32;
-inline int seq_bwd_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }  // keys a workgroup takes in the gradient
+constexpr int kSeqBwdKeys = 64;  // keys a workgroup takes in the gradient
 inline int seq_tile_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }
 
 template <typename T> int run_seq_fwd(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how);

@@ -61,16 +61,10 @@ template <typename T, int D> struct SeqTile {
         else return (row & 3) << 2 | ((row >> 2) & 3);
     }
 
-    // acc += X Y^T of the tile's 32 rows from `rows` on and 32 rows Y held as
-    // operand fragments (lane 32 h + c: row c, chunks 2 st + h).
-    __device__ static f32x16 scores(const char *rows, const frag *y, int lane, f32x16 acc)
+    // Operand fragment of the rows: lane 32 h + c holds chunk 2 st + h of row c of the 32 from `rows` on.
+    __device__ static frag row_frag(const char *rows, int st, int lane)
     {
-        const char *x = rows + (lane & 31) * ROW;
-        const int flip = (lane >> 5) ^ swz(lane & 15);
-#pragma unroll
-        for (int st = 0; st < NS; ++st)
-            acc = M::mma(*reinterpret_cast<const frag *>(x + ((2 * st) ^ flip) * 16), y[st], acc);
-        return acc;
+        return *reinterpret_cast<const frag *>(rows + (lane & 31) * ROW + ((2 * st) ^ (lane >> 5) ^ swz(lane & 15)) * 16);
     }
 
     // Operand fragment X^T: lane 32 h + c holds column 32 dt + c of the rows
@@ -119,31 +113,31 @@ template <> struct Probs32<float> {
     __device__ inline void pack(f32x16 x) { s = x; }
 };
 
-// acc[dt] += X^T B of 32 tile rows from `rows` on; B: one Probs32 for each of NB column blocks.
-template <typename T, int D, int NB>
-__device__ inline void aggregate(const char *rows, const Probs32<T> *b, f32x16 (*acc)[SeqTile<T, D>::ND], int lane)
-{
-    using S = SeqTile<T, D>;
-    if constexpr (S::kF32) {
+// A step's fragments, in the order in which its products use them, read from
+// LDS AHEAD of them in front of their use: a read takes as long as several
+// products, and left to itself the compiler waits for each read in front of its
+// own.  `load(u)`: fragment u of N; every loop over them is unrolled.
+enum SchedGroup { kSchedMfma = 0x8, kSchedDsRead = 0x100 };
+template <typename Frag, int N, int AHEAD> struct FragStream {
+    Frag f[AHEAD];
+    template <typename Load> __device__ __forceinline__ void start(Load &&load)
+    {
 #pragma unroll
-        for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float x = S::element(rows, kRow32(r) + 4 * (lane >> 5), dt, lane);
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-                    acc[n][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, b[n].s[r], acc[n][dt], 0, 0, 0);
-            }
-    } else {
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-            for (int dt = 0; dt < S::ND; ++dt) {
-                const typename S::frag x = S::columns(rows + ks * 16 * S::ROW, dt, lane);
-#pragma unroll
-                for (int n = 0; n < NB; ++n) acc[n][dt] = S::M::mma(x, b[n].f[ks], acc[n][dt]);
-            }
+        for (int u = 0; u < AHEAD; ++u) f[u] = load(u);
     }
+    // Fragment u for the products `use`, and the read of one that comes later.
+    template <typename Load, typename Use> __device__ __forceinline__ void next(int u, Load &&load, Use &&use)
+    {
+        use(f[u % AHEAD]);
+        if (u + AHEAD < N) f[u % AHEAD] = load(u + AHEAD);
+    }
+};
+// The order of one product (PRODUCTS instructions) and the `reads` (0 to 2) behind it.
+template <int PRODUCTS> __device__ __forceinline__ void sched_step(int reads)
+{
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, PRODUCTS, 0);
+    if (reads == 1) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+    if (reads == 2) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
 }
 
 // A value that all lanes of the wave share, in a scalar register: the address of a copy has to be there.
