@@ -174,7 +174,18 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
 // Workspace of the gradient: lse in log2 units and delta of every row and head,
 // and the largest norms of the workgroups that form them.
 constexpr int kNormBlocks = 512;
-size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * total) * 4) + kNormBlocks * sizeof(float2); }
+size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * total) * 4) + align_up(kNormBlocks * sizeof(float2)); }
+
+// Pieces that the query rows of a key tile are cut into.  The longest walk, of the
+// first keys of one causal sequence that fills the call, is twice the mean one,
+// so 1024 key tiles and heads (two rounds of two workgroups on 256 compute units) end with it; the
+// pieces make it half of the mean work of a compute unit's slot.  A piece of fewer than 8
+// tiles is not worth its sums' way through memory.
+int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
+{
+    const int64_t want = (8 * num_cus + tiles_k * Hkv - 1) / (tiles_k * Hkv);
+    return std::max<int64_t>(1, std::min<int64_t>({want, 4, G * tiles_k / 8}));
+}
 
 int packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
                const void *dout, void *dq, void *dk, void *dv, const int32_t *cu, int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d,
@@ -204,7 +215,10 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
     MA_TRY(begin_call(stream, c));
-    MA_TRY(call_workspace(stream, bwd_bytes(total, Hq), c));
+    const int64_t pieces = bwd_pieces(tiles_k, Hkv, G, c.num_cus);
+    const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq);
+    MA_TRY(check_grid(tiles_k * pieces, Hkv));
+    MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
     BwdLaunch x{};
     ma::SeqBwd &p = x.p;
     p.q = q, p.k = k, p.v = v, p.out = out, p.dout = dout, p.lse = lse, p.rest = rest;
@@ -217,6 +231,8 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     const size_t each = align_up((size_t)(Hq * total) * 4);
     p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each), p.norms = (float2 *)(c.ws + 2 * each);
     p.norm_blocks = (int)std::min<int64_t>(kNormBlocks, (total * Hq + 15) / 16);
+    p.pieces = (int)pieces;
+    p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;
     return run_launches(stream, BwdLaunch::run, &x);
 }

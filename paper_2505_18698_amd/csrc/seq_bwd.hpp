@@ -8,11 +8,11 @@
 // A row that sees one key has the weight 1 whatever the score: its dS is zero,
 // which dP - delta would give up to rounding only.
 //
-// Three launches: the row statistics; dK and dV, a workgroup per 64 keys that
-// walks the query rows; dQ, a workgroup per 128 packed rows that walks the
-// keys.  The scores and dP are formed twice (7 products instead of 5), so that
-// each sum has one owner that adds in a fixed order in fp32 registers: no
-// atomics, no partial sums in memory.
+// Launches: the row statistics; dK and dV, a workgroup per 64 keys that walks
+// the query rows, or several for pieces of them, whose sums a further launch
+// adds up; dQ, a workgroup per 128 packed rows that walks the keys.  The scores and dP are formed twice (7 products instead of 5), so that
+// each sum has one owner that adds in a fixed order in fp32 registers, without
+// atomics.
 #pragma once
 
 #include "seq_attn.hpp"
@@ -269,25 +269,25 @@ template <typename T, int D> struct SeqBwdQ {
 template <typename T, int D> struct SeqBwdK {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int NK = 2, NQ = S::ROW <= 256 ? 4 : 2, W = NK * NQ, NTH = 64 * W, R = 32 * NK;
-    static constexpr int BQ = 32 * NQ, TILE = BQ * S::ROW, STATS = 2 * BQ * 4;
+    static constexpr int NK = 2, NQ = 2, W = NK * NQ, NTH = 64 * W, R = 32 * NK;
+    static constexpr int BQ = 32 * NQ, TILE = BQ * S::ROW;
     static constexpr bool kVInLds = !S::kF32 && D > 64;
-    static constexpr int LDS_BYTES = 4 * TILE + 2 * STATS + (kVInLds ? R * S::ROW : 0);
+    static constexpr int LDS_BYTES = 4 * TILE + (kVInLds ? R * S::ROW : 0);
     using Copy = TileCopy<T, D, BQ, W>;
 
     struct Grads {
         f32x16 dk[S::ND], dv[S::ND];
     };
 
-    // 32 rows of Q and dO (qt, gt), their lse and delta.  `ahead`: the first of them minus
+    // 32 rows of Q and dO (qt, gt); terms: -lse / s, so that P = exp2(c S), and -delta of the rows.  `ahead`: the first of them minus
     // this lane's key; rows before `first` (row 0, which sees one key) pass no gradient to scores.
     // vt: the key block's V rows in LDS, where they are there.
     template <bool MASK>
-    __device__ static void step(const char *qt, const char *gt, const float *lse2, const float *delta, const frag *kf, const frag *vf,
+    __device__ static void step(const char *qt, const char *gt, const RowTerms<T> &terms, const frag *kf, const frag *vf,
                                 const char *vt, int ahead, int first, float c, float scale, Grads &x, int lane)
     {
         // fragments: the rows of Q, then of dO (each with V's behind it), then the columns of dO and of Q
-        constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = D > 96 ? 3 : 4;
+        constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = D > 96 ? 2 : 4;
         FragStream<frag, N, AHEAD> stream;
         auto load = [&](int u) {
             if constexpr (!S::kF32)
@@ -301,7 +301,7 @@ template <typename T, int D> struct SeqBwdK {
         auto reads = [&](int u) { return u + AHEAD >= N ? 0 : u + AHEAD >= NR ? 2 : 1; };
         stream.start(load);
         __builtin_amdgcn_sched_group_barrier(kSchedDsRead, AHEAD, 0);
-        f32x16 s = {}, dp = {};
+        f32x16 s = terms.template add<0>(f32x16{}, lane), dp = terms.template add<1>(f32x16{}, lane);
 #pragma unroll
         for (int u = 0; u < S::NS; ++u) {
             stream.next(u, load, [&](const frag &y) { s = S::M::mma(y, kf[u], s); });
@@ -321,19 +321,14 @@ template <typename T, int D> struct SeqBwdK {
             }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const f32x4 l = *reinterpret_cast<const f32x4 *>(lse2 + 8 * e + 4 * (lane >> 5));
-            const f32x4 del = *reinterpret_cast<const f32x4 *>(delta + 8 * e + 4 * (lane >> 5));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * e + i, row = kRow32(r) + 4 * (lane >> 5);
-                float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -l[i]));
-                if (MASK && row + ahead < 0) w = 0.f;
-                float y = w * (dp[r] - del[i]);
-                if constexpr (BwdScale<T>::kScaled) y *= scale;
-                s[r] = w;
-                dp[r] = MASK && (row + ahead < 0 || row < first) ? 0.f : y;
-            }
+        for (int r = 0; r < 16; ++r) {
+            const int row = kRow32(r) + 4 * (lane >> 5);
+            float w = __builtin_amdgcn_exp2f(s[r] * c);
+            if (MASK && row + ahead < 0) w = 0.f;
+            float y = w * dp[r];
+            if constexpr (BwdScale<T>::kScaled) y *= scale;
+            s[r] = w;
+            dp[r] = MASK && (row + ahead < 0 || row < first) ? 0.f : y;
         }
         Probs32<T> pf, sf;
         pf.pack(s);
@@ -361,6 +356,7 @@ template <typename T, int D> struct SeqBwdK {
     }
 
     // The waves' sums of one gradient, scaled, to the keys' rows of `out`.
+    template <typename O>
     __device__ static void add_up(char *lds, const f32x16 *x, const Span &out, float by, int ld, int d, int keys, int wave, int lane)
     {
         constexpr int N = S::ND * 4 * 64;  // a wave's sums, in 4 values
@@ -381,7 +377,7 @@ template <typename T, int D> struct SeqBwdK {
 #pragma unroll
                 for (int q = 1; q < NQ; ++q) sum += src[q * NK * N + e * 64];
                 const int key = 32 * kb + (lane & 31), col = 32 * dt + 8 * e + 4 * (lane >> 5);
-                out.store<T>(sum * by, (key * ld + col) * (int)sizeof(T), key < keys && col < d);
+                out.store<O>(sum * by, (key * ld + col) * (int)sizeof(O), key < keys && col < d);
             }
         }
     }
@@ -392,7 +388,8 @@ template <typename T, int D> struct SeqBwdK {
         BwdScale<T> sc;
         sc.template find<NTH>(p, lds);
         const int kvh = uniform((int)(blockIdx.x % p.Hkv));
-        const int64_t t = (int)(blockIdx.x / p.Hkv);  // (earlier keys are seen by more rows: they start first)
+        const int64_t t = (int)(blockIdx.x / p.Hkv / p.pieces);  // (earlier keys are seen by more rows: they start first)
+        const int piece = uniform((int)(blockIdx.x / p.Hkv % p.pieces));
         const int seq = uniform(seq_of_tile(p.seqs, t, 1, R, lane));
         if (seq < 0) return;
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
@@ -400,7 +397,7 @@ template <typename T, int D> struct SeqBwdK {
 
         const Span ks((const T *)p.k + (row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d);
         const int ldv = (int)p.ldv * (int)sizeof(T), kc = min(32 * kb + (lane & 31), n - 1 - k0);
-        char *vt = lds + 4 * TILE + 2 * STATS;
+        char *vt = lds + 4 * TILE;
         frag kf[S::NS], vf[kVInLds ? 1 : S::NS];
         if constexpr (kVInLds) {
             TileCopy<T, D, R, W> cv;
@@ -418,66 +415,68 @@ template <typename T, int D> struct SeqBwdK {
             }
         }
 
-        float *stats = reinterpret_cast<float *>(lds + 4 * TILE);
         const int ldq = (int)p.ldq * (int)sizeof(T), ldg = Hq * p.d * (int)sizeof(T);
         Copy cq, cg;
         cq.init(ldq, p.d, wave, lane);
         cg.init(ldg, p.d, wave, lane);
-        const int from = p.causal ? k0 : 0;  // the first query row that sees a key of this workgroup
-        float stat = 0.f;  // threads 0..BQ-1: lse of a row of the next tile, BQ..2 BQ-1: delta
-        auto bring = [&](int g, int q0, int buf) {
+        // The walk: every head's tiles from the first row that sees a key of this workgroup on, this piece's share of them.
+        const int from = p.causal ? k0 : 0, tiles = (n - from + BQ - 1) / BQ;
+        const int begin = uniform((int)((int64_t)p.G * tiles * piece / p.pieces)), end = uniform((int)((int64_t)p.G * tiles * (piece + 1) / p.pieces));
+        float lse2 = 0.f, delta = 0.f;  // of this lane's row of the tile that is copied
+        auto bring = [&](int i, int g, int q0, int buf) {  // tile i of the walk, at row q0 of head g or the next one's first
+            if (i >= end) return;
             if (q0 >= n) q0 = from, ++g;
-            if (g >= p.G) return;
             const int head = kvh * p.G + g;
             char *to = lds + 2 * TILE * buf;
             cq.tile((const T *)p.q + (row0 + q0) * p.ldq + head * p.d, n - q0, ldq, to, wave);
             cg.tile((const T *)p.dout + ((int64_t)(row0 + q0) * Hq + head) * p.d, n - q0, ldg, to + TILE, wave);
-            if (tid < 2 * BQ) {
-                const int r = q0 + tid % BQ;
-                const bool is_lse = tid < BQ;
-                // (a row that is not there has weights of zero)
-                stat = r < n ? (is_lse ? p.lse2 : p.delta)[(int64_t)head * p.seqs.total + row0 + r] : is_lse ? INFINITY : 0.f;
-                if (is_lse) stat -= BwdScale<T>::kP;
-            }
+            const int r = min(q0 + 32 * qb + (lane & 31), n - 1);
+            const int64_t at = (int64_t)head * p.seqs.total + row0 + r;
+            lse2 = p.lse2[at], delta = p.delta[at];
+            if (q0 + 32 * qb + (lane & 31) >= n) lse2 = 1e30f, delta = 0.f;  // a row that is not there has weights of zero
         };
-        auto keep = [&](int buf) {
-            if (tid < 2 * BQ) stats[buf * 2 * BQ + tid] = stat;
-        };
+        const float per_c = 1.f / p.c;
+        RowTerms<T> terms;
 
         Grads x;
 #pragma unroll
         for (int dt = 0; dt < S::ND; ++dt) x.dk[dt] = x.dv[dt] = f32x16{};
         const float scale = BwdScale<T>::kScaled ? sc.ds * 0x1p-14f : 1.f;
-        bring(0, from, 0);
-        keep(0);
-        int buf = 0;
+        int buf = 0, i = begin, g = begin / tiles;
+        int q0 = from + (begin - g * tiles) * BQ;
+        bring(i, g, q0, 0);
         const char *own = lds + 32 * qb * S::ROW, *vrows = vt + 32 * kb * S::ROW;
-        const float *own_stats = stats + 32 * qb;
 #pragma unroll 1
-        for (int g = 0; g < p.G; ++g) {
-            int q0 = from;
-            if (p.causal) {  // of a head's tiles the first holds rows that see a part of the keys
+        while (i < end) {
+            if (q0 >= n) q0 = from, ++g;
+            if (p.causal && q0 == from) {  // a head's first tile holds rows that see a part of the keys
                 tile_barrier();
-                bring(g, q0 + BQ, buf ^ 1);
+                terms.set((BwdScale<T>::kP - lse2) * per_c, -delta, lane);
+                bring(i + 1, g, q0 + BQ, buf ^ 1);
                 if (q0 + 32 * qb < n)
-                    step<true>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, own_stats + buf * 2 * BQ, own_stats + buf * 2 * BQ + BQ, kf, vf,
-                               vrows, q0 + 32 * qb - k0 - 32 * kb - (lane & 31), 1 - q0 - 32 * qb, p.c, scale, x, lane);
-                keep(buf ^ 1);
-                q0 += BQ, buf ^= 1;
+                    step<true>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, terms, kf, vf, vrows,
+                               q0 + 32 * qb - k0 - 32 * kb - (lane & 31), 1 - q0 - 32 * qb, p.c, scale, x, lane);
+                ++i, q0 += BQ, buf ^= 1;
             }
 #pragma unroll 1
-            for (; q0 < n; q0 += BQ, buf ^= 1) {
+            for (; i < end && q0 < n; ++i, q0 += BQ, buf ^= 1) {
                 tile_barrier();
-                bring(g, q0 + BQ, buf ^ 1);
+                terms.set((BwdScale<T>::kP - lse2) * per_c, -delta, lane);
+                bring(i + 1, g, q0 + BQ, buf ^ 1);
                 if (q0 + 32 * qb < n)
-                    step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, own_stats + buf * 2 * BQ, own_stats + buf * 2 * BQ + BQ, kf, vf,
-                                vrows, 0, 0, p.c, scale, x, lane);
-                keep(buf ^ 1);
+                    step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, terms, kf, vf, vrows, 0, 0, p.c, scale, x, lane);
             }
         }
+        const float by_k = n == 1 ? 0.f : p.c * kLn2 / sc.ds, by_v = BwdScale<T>::kScaled ? 0x1p-14f : 1.f;
+        if (p.pieces > 1) {
+            const int64_t at = (((int64_t)piece * p.seqs.total + row0 + k0) * p.Hkv + kvh) * D;
+            add_up<float>(lds, x.dk, Span(p.part_k + at), by_k, p.Hkv * D, D, n - k0, wave, lane);
+            add_up<float>(lds, x.dv, Span(p.part_v + at), by_v, p.Hkv * D, D, n - k0, wave, lane);
+            return;
+        }
         const int64_t out0 = ((int64_t)(row0 + k0) * p.Hkv + kvh) * p.d;
-        add_up(lds, x.dk, Span((T *)p.dk + out0), n == 1 ? 0.f : p.c * kLn2 / sc.ds, p.Hkv * p.d, p.d, n - k0, wave, lane);
-        add_up(lds, x.dv, Span((T *)p.dv + out0), BwdScale<T>::kScaled ? 0x1p-14f : 1.f, p.Hkv * p.d, p.d, n - k0, wave, lane);
+        add_up<T>(lds, x.dk, Span((T *)p.dk + out0), by_k, p.Hkv * p.d, p.d, n - k0, wave, lane);
+        add_up<T>(lds, x.dv, Span((T *)p.dv + out0), by_v, p.Hkv * p.d, p.d, n - k0, wave, lane);
     }
 };
 
@@ -488,11 +487,29 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
     U::run(p, lds);
 }
 
-template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), (SeqBwdK<T, D>::W / 4)) void seq_bwd_k(SeqBwd p)
+template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), (sizeof(T) == 4 && D > 64 ? 1 : 2)) void seq_bwd_k(SeqBwd p)
 {
     using U = SeqBwdK<T, D>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
+}
+
+// The pieces' sums of dK and dV added up, four columns a thread.
+template <typename T, int D> __global__ __launch_bounds__(256) void seq_bwd_join(SeqBwd p)
+{
+    constexpr int C = D / 4;
+    const int64_t first = (int64_t)p.seqs.start(0) * p.Hkv, rows = (int64_t)p.seqs.start(p.seqs.B) * p.Hkv - first;
+    const int64_t each = (int64_t)p.seqs.total * p.Hkv * D;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * C; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = first + i / C;
+        const int col = (int)(i % C) * 4;
+        if (col >= p.d) continue;
+        const float *k = p.part_k + row * D + col, *v = p.part_v + row * D + col;
+        f32x4 a = *(const f32x4 *)k, b = *(const f32x4 *)v;
+        for (int x = 1; x < p.pieces; ++x) a += *(const f32x4 *)(k + x * each), b += *(const f32x4 *)(v + x * each);
+        store4<T>((T *)p.dk + row * p.d + col, a);
+        store4<T>((T *)p.dv + row * p.d + col, b);
+    }
 }
 
 }  // namespace ma

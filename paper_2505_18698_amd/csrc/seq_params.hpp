@@ -56,6 +56,10 @@ struct SeqBwd {
     float *lse2, *delta;                 // [Hq, total]: lse in log2 units, delta
     float2 *norms;                       // fp16: the largest |dO_i|^2 and |v_j|^2 of every workgroup of seq_stats
     int norm_blocks;
+    // pieces that the query rows of a key tile are cut into; with more than one, their sums:
+    // dK and dV of every piece, row and key head, in rows of the tile width
+    int pieces;
+    float *part_k, *part_v;
 };
 
 struct PagedPlan {

@@ -90,6 +90,43 @@ template <typename T, int D> struct SeqTile {
     }
 };
 
+// Two values per row of a 32 x 32 result, each as a product of its own: a lane
+// of the left operand holds its row's x in three slots, as bf16 values whose sum
+// is x to 2^-24, and y in three others; the right operand holds ones in either's.
+// So they reach all results of the row without passing through LDS.  (fp32: x and y in the two slots.)
+template <typename T> struct RowTerms {
+    bf16x8 a;
+    // x and y finite: an infinity would meet itself in the second value
+    __device__ inline void set(float x, float y, int lane)
+    {
+        a = bf16x8{};
+        if (lane < 32) {
+            float z[2] = {x, y};
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                a[i] = (__bf16)z[i / 3];
+                z[i / 3] -= (float)a[i];
+            }
+        }
+    }
+    template <int I> __device__ inline f32x16 add(f32x16 c, int lane) const
+    {
+        const uint32_t one = lane < 32 ? 0x3f803f80u : 0u;  // two bf16 ones
+        const u32x4 ones = I == 0 ? u32x4{one, one & 0xffffu, 0u, 0u} : u32x4{0u, one & 0xffff0000u, one, 0u};
+        bf16x8 b;
+        __builtin_memcpy(&b, &ones, 16);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct RowTerms<float> {
+    float a;
+    __device__ inline void set(float x, float y, int lane) { a = lane < 32 ? x : y; }
+    template <int I> __device__ inline f32x16 add(f32x16 c, int lane) const
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(a, lane / 32 == I ? 1.f : 0.f, c, 0, 0, 0);
+    }
+};
+
 // The 32 x 32 result `s` as the right operand of products that contract over
 // its rows: two fragments of 16 rows in 16-bit types, the values themselves in fp32.
 template <typename T> struct Probs32 {
@@ -216,14 +253,15 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
     }
 };
 
-// Every copy of this wave has arrived, and every wave of the workgroup is here.
+// Every copy and load of this wave has arrived, and every wave of the workgroup
+// is here.  (The wait is the builtin, not assembly, so that the compiler knows of
+// it: it would wait again in front of the first use of what was loaded before the loop, in
+// every iteration, and there for copies that it does not know of.)
 __device__ inline void tile_barrier()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    asm volatile("s_barrier" ::: "memory");
 }
-
-// Every copy and load of this wave has arrived.
-__device__ inline void wave_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // Whether `x` holds on some thread of a workgroup of NTH (`shared`: NTH / 64 integers of LDS).
 template <int NTH> __device__ inline bool some_thread(bool x, int *shared)
