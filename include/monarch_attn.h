@@ -391,8 +391,9 @@ int32_t monarch_attn_timing_read(float *ms, int32_t *kind, int32_t cap);
  * model that keep it.  B sequences lie one after another in the rows of one
  * tensor: sequence i has the rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1
  * (device int32, B + 1 of them, not decreasing; each is clamped to 0..total).
- * Rows before the first and behind the last sequence are neither read nor
- * written.  Sequences may be empty.
+ * Rows before the first and behind the last sequence are not read, and left as
+ * they are in the outputs, or, with clear != 0, written as zero (in out, dq, dk
+ * and dv).  Sequences may be empty.
  *
  * Hq query heads share Hkv key heads in groups of G = Hq / Hkv: query head h
  * reads key head h / G.  The scores are scaled by s = 1/sqrt(d).  With causal
@@ -433,8 +434,8 @@ int32_t monarch_attn_timing_read(float *ms, int32_t *kind, int32_t cap);
  */
 int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
                                   const int32_t *cu_seqlens, int64_t B, int64_t total, int64_t Hq, int64_t Hkv,
-                                  int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal, int32_t dtype,
-                                  void *stream);
+                                  int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal, int32_t clear,
+                                  int32_t dtype, void *stream);
 
 /*
  * monarch_attn_exact_packed_bwd -- its gradient: from out, lse and rest (or
@@ -442,7 +443,7 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
  * of a key head summed over its query heads.
  *
  * out, dout, dq : [total, Hq, d], contiguous; dk, dv: [total, Hkv, d],
- *                 contiguous.  Rows of no sequence are left as they were.
+ *                 contiguous.
  * In fp16, dS is formed relative to the largest norms of the rows of dout and
  * v, so gradients of any scale keep their precision.  Values of a sequence
  * that are not finite can reach all gradients of that sequence.
@@ -451,7 +452,8 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
 int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,
                                   const void *rest, const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_seqlens,
                                   int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq,
-                                  int64_t ldk, int64_t ldv, int32_t causal, int32_t dtype, void *stream);
+                                  int64_t ldk, int64_t ldv, int32_t causal, int32_t clear, int32_t dtype,
+                                  void *stream);
 
 /*
  * monarch_attn_exact_paged_fwd -- the new tokens of every sequence (one, or a

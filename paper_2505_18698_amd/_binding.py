@@ -96,8 +96,8 @@ def _load() -> ctypes.CDLL:
     lib.monarch_attn_fwd_noalloc.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, i32, i32, vp]
     lib.monarch_attn_fwd_noalloc.restype = ctypes.c_int
     for name, argtypes in (
-        ("monarch_attn_exact_packed_fwd", [vp] * 7 + [i64] * 8 + [i32, i32, vp]),
-        ("monarch_attn_exact_packed_bwd", [vp] * 11 + [i64] * 8 + [i32, i32, vp]),
+        ("monarch_attn_exact_packed_fwd", [vp] * 7 + [i64] * 8 + [i32, i32, i32, vp]),
+        ("monarch_attn_exact_packed_bwd", [vp] * 11 + [i64] * 8 + [i32, i32, i32, vp]),
         ("monarch_attn_exact_paged_fwd", [vp] * 8 + [i64] * 9 + [i32, i32, vp]),
         ("monarch_attn_paged_plan", [vp] * 10 + [i64] * 5 + [vp]),
         ("monarch_attn_paged_write", [vp] * 5 + [i64] * 7 + [i32, vp]),
@@ -420,77 +420,114 @@ PLAN_NO_PAGES, PLAN_TABLE_FULL, PLAN_BAD_LENGTH, PLAN_NO_SLOTS = 1, 2, 4, 8  # M
 PLAN_MAX_B = 8192  # MONARCH_ATTN_PLAN_MAX_B
 
 
+def _rows(t, dtype, device):
+    """The row stride of t, [rows, heads, d] of that dtype on that device with
+    the heads of a row adjacent, or -1 where it is nothing of the kind."""
+    _, h, d = t.shape
+    x, y, z = t.stride()
+    if (z == 1 or d == 1) and (y == d or h == 1) and t.dtype == dtype and t.device == device:
+        return x if t.shape[0] > 1 else h * d
+    return -1
+
+
+def _is(t, shape, dtype, device):
+    """Whether t is a contiguous tensor of that shape, dtype and device."""
+    return t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous()
+
+
 def _check_rows(name, t, like, like_name="q"):
-    """t: [rows, heads, d] on the device and of the dtype of `like`, the heads
-    of a row adjacent; rows may be further apart.  Returns the row stride."""
-    rt = _torch()
-    if not isinstance(t, rt.Tensor) or not t.is_cuda:
+    """Raise unless t is [rows, heads, d] on the device and of the dtype of `like`, the heads of a row adjacent."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if t.dim() != 3 or t.stride(2) != 1 and t.shape[2] > 1 or t.stride(1) != t.shape[2] and t.shape[1] > 1:
+    if t.dim() != 3 or _rows(t, t.dtype, t.device) < 0:
         raise ValueError(f"{name} must be a [rows, heads, d] tensor whose rows are contiguous")
     if t.dtype != like.dtype or t.device != like.device:
         raise ValueError(f"{name} must match {like_name} in dtype and device")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
 
 def _check_like(name, t, shape, like, dtype=None):
-    """t: a contiguous device tensor of `shape` on the device of `like` (and of its dtype, or `dtype`)."""
-    rt = _torch()
-    if not isinstance(t, rt.Tensor) or not t.is_cuda:
+    """Raise unless t is a contiguous device tensor of `shape` on the device of `like` (and of its dtype, or `dtype`)."""
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != like.device \
-            or t.dtype != (like.dtype if dtype is None else dtype):
-        raise ValueError(f"{name} must be a contiguous {dtype or like.dtype} tensor {list(shape)} on the device of the others")
+    dtype = like.dtype if dtype is None else dtype
+    if not _is(t, shape, dtype, like.device):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the device of the others")
 
 
 def _check_packed(q, k, v, cu_seqlens):
-    """Row strides and sizes of packed q [total, Hq, d], k and v [total, Hkv, d]."""
-    ldq, ldk, ldv = (_check_rows(name, t, q) for name, t in (("q", q), ("k", k), ("v", v)))
-    total, Hq, d = q.shape
-    if k.shape != v.shape or k.shape[0] != total or k.shape[2] != d:
+    """Sizes (B, total, Hq, Hkv, d) and row strides of packed q [total, Hq, d], k and v [total, Hkv, d]."""
+    rt = _torch()
+    try:
+        # (one pass without names: a short call is bound by these checks as much as by the GPU)
+        total, Hq, d = q.shape
+        Hkv = k.shape[1]
+        dtype, device = q.dtype, q.device
+        ldq, ldk, ldv = _rows(q, dtype, device), _rows(k, dtype, device), _rows(v, dtype, device)
+        if q.is_cuda and ldq >= 0 and ldk >= 0 and ldv >= 0 and k.shape == v.shape == (total, Hkv, d) \
+                and cu_seqlens.dtype == rt.int32 and cu_seqlens.dim() == 1 and cu_seqlens.shape[0] > 0 \
+                and cu_seqlens.device == device and cu_seqlens.is_contiguous():
+            return (cu_seqlens.shape[0] - 1, total, Hq, Hkv, d), (ldq, ldk, ldv)
+    except (AttributeError, ValueError, IndexError):  # no tensor, or not of three dimensions
+        pass
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _check_rows(name, t, q)
+    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
         raise ValueError("k and v must be [total, Hkv, d] tensors with the rows and head dimension of q")
-    if not isinstance(cu_seqlens, _torch().Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+    if not isinstance(cu_seqlens, rt.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
         raise ValueError("cu_seqlens must be an int32 tensor [B + 1]")
-    _check_like("cu_seqlens", cu_seqlens, cu_seqlens.shape, q, _torch().int32)
-    return (cu_seqlens.shape[0] - 1, total, Hq, k.shape[1], d), (ldq, ldk, ldv)
+    _check_like("cu_seqlens", cu_seqlens, cu_seqlens.shape, q, rt.int32)
+    raise ValueError("q, k and v must be device tensors")
 
 
-def monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal: bool = True, lse=None, rest=None, stream=None):
+def _check_each(like, *tensors):
+    """Raise for the first of the (name, tensor, shape, dtype) that is no contiguous tensor of that kind on the device of `like`."""
+    device = like.device
+    for name, t, shape, dtype in tensors:
+        try:
+            if t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous():
+                continue
+        except AttributeError:
+            pass
+        _check_like(name, t, shape, like, dtype)
+
+
+def monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal: bool = True, lse=None, rest=None,
+                                  clear: bool = False, stream=None):
     """Exact softmax attention over sequences that lie one after another:
     q [total, Hq, d], k and v [total, Hkv, d] (rows may be strided, as in parts
     of a joint projection), sequence i the rows cu_seqlens[i] to
     cu_seqlens[i + 1] (int32 device tensor [B + 1]).  Writes the rows of the
     sequences in out [total, Hq, d] and, with lse (float32 device tensor
     [Hq, total]), every row's logsumexp; with rest (like out, 16-bit types) also
-    what rounding out leaves, for the gradient.  Returns (out, lse)."""
+    what rounding out leaves, for the gradient.  Rows of no sequence are left,
+    or, with clear, zero in out.  Returns (out, lse)."""
     sizes, strides = _check_packed(q, k, v, cu_seqlens)
-    _check_like("out", out, q.shape, q)
+    _check_each(q, ("out", out, q.shape, q.dtype))
     if lse is not None:
-        _check_like("lse", lse, (q.shape[1], q.shape[0]), q, _torch().float32)
+        _check_each(q, ("lse", lse, (q.shape[1], q.shape[0]), _torch().float32))
     if rest is not None:
-        _check_like("rest", rest, q.shape, q)
+        _check_each(q, ("rest", rest, q.shape, q.dtype))
     _call(LIB.monarch_attn_exact_packed_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-          None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(), cu_seqlens.data_ptr(), *sizes, *strides, bool(causal),
+          None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(), cu_seqlens.data_ptr(), *sizes, *strides, bool(causal), bool(clear),
           dtype_code(q.dtype), _stream(q, stream) or None)
     return out, lse
 
 
 def monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal: bool = True, rest=None,
-                                  stream=None):
+                                  clear: bool = False, stream=None):
     """The gradient of monarch_attn_exact_packed_fwd from its out, lse and rest
     (None: without) and dout = dL/dout, into dq [total, Hq, d], dk and dv [total, Hkv, d]
-    (contiguous; rows of no sequence are left).  Returns (dq, dk, dv)."""
+    (contiguous; rows of no sequence are left, or, with clear, zero).  Returns
+    (dq, dk, dv)."""
     sizes, strides = _check_packed(q, k, v, cu_seqlens)
-    for name, t in (("out", out), ("dout", dout), ("dq", dq)):
-        _check_like(name, t, q.shape, q)
-    for name, t in (("dk", dk), ("dv", dv)):
-        _check_like(name, t, k.shape, q)
+    rows, keys, dtype = q.shape, k.shape, q.dtype
+    _check_each(q, ("out", out, rows, dtype), ("dout", dout, rows, dtype), ("dq", dq, rows, dtype), ("dk", dk, keys, dtype),
+                ("dv", dv, keys, dtype), ("lse", lse, (rows[1], rows[0]), _torch().float32))
     if rest is not None:
-        _check_like("rest", rest, q.shape, q)
-    _check_like("lse", lse, (q.shape[1], q.shape[0]), q, _torch().float32)
+        _check_each(q, ("rest", rest, rows, dtype))
     _call(LIB.monarch_attn_exact_packed_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
           lse.data_ptr(), None if rest is None else rest.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_seqlens.data_ptr(), *sizes,
-          *strides, bool(causal), dtype_code(q.dtype), _stream(q, stream) or None)
+          *strides, bool(causal), bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
     return dq, dk, dv
 
 
@@ -513,11 +550,11 @@ def _packed_function():
             @staticmethod
             def forward(ctx, q, k, v, cu_seqlens, causal):
                 q, k, v = rows(q), rows(k), rows(v)
-                out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
                 lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
                 # (the gradient reads no row of no sequence: rest stays as it is there)
                 rest = torch.empty_like(out) if out.element_size() == 2 else None
-                monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest)
+                monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest, True)
                 ctx.save_for_backward(q, k, v, out, lse, cu_seqlens, *(() if rest is None else (rest,)))
                 ctx.causal = causal
                 return out
@@ -525,9 +562,9 @@ def _packed_function():
             @staticmethod
             def backward(ctx, dout):
                 q, k, v, out, lse, cu_seqlens, *rest = ctx.saved_tensors
-                dq, dk, dv = (torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+                dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
                 monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout.contiguous(), dq, dk, dv, cu_seqlens, ctx.causal,
-                                              *rest)
+                                              *(rest or (None,)), True)
                 return dq, dk, dv, None, None
 
         _PACKED_FN = ExactAttentionPackedFn
@@ -541,14 +578,26 @@ def exact_attention_packed(q, k, v, cu_seqlens, causal: bool = True):
     return _packed_function().apply(q, k, v, cu_seqlens, causal)
 
 
-def _check_cache(k_pages, v_pages):
-    """Sizes (pages, page) of a paged cache [pages, Hkv, page, d]."""
-    rt = _torch()
-    if not isinstance(k_pages, rt.Tensor) or not k_pages.is_cuda:
+def _check_cache(k_pages, v_pages, heads, d, like, like_name):
+    """Raise unless k_pages and v_pages are contiguous [pages, heads, page, d] of the dtype and on the device of
+    `like` (heads None: any number); their shape."""
+    try:
+        shape = k_pages.shape
+        if len(shape) == 4 and v_pages.shape == shape and shape[3] == d and (heads is None or shape[1] == heads) \
+                and k_pages.dtype == v_pages.dtype == like.dtype and k_pages.device == v_pages.device == like.device \
+                and k_pages.is_contiguous() and v_pages.is_contiguous():
+            return shape
+    except AttributeError:
+        pass
+    if not isinstance(k_pages, _torch().Tensor) or not k_pages.is_cuda:
         raise TypeError("k_pages must be a device tensor")
     if k_pages.dim() != 4 or not k_pages.is_contiguous():
         raise ValueError("k_pages must be a contiguous [pages, Hkv, page, d] tensor")
+    if k_pages.shape[3] != d or heads is not None and k_pages.shape[1] != heads or k_pages.dtype != like.dtype \
+            or k_pages.device != like.device:
+        raise ValueError(f"k_pages must match {like_name} in heads, head dimension, dtype and device")
     _check_like("v_pages", v_pages, k_pages.shape, k_pages)
+    return k_pages.shape
 
 
 def monarch_attn_exact_paged_fwd(q, k_pages, v_pages, out, cu_seqlens, kv_lens, block_table, causal: bool = True,
@@ -560,21 +609,22 @@ def monarch_attn_exact_paged_fwd(q, k_pages, v_pages, out, cu_seqlens, kv_lens, 
     the cache, the new ones (its last) among them.  Writes out [total, Hq, d]
     and, if given, lse (float32 [Hq, total]).  Returns (out, lse)."""
     rt = _torch()
-    ldq = _check_rows("q", q, q)
-    _check_cache(k_pages, v_pages)
+    try:
+        ldq = _rows(q, q.dtype, q.device) if q.is_cuda else -1
+    except (AttributeError, ValueError):
+        ldq = -1
+    if ldq < 0:
+        _check_rows("q", q, q)
     total, Hq, d = q.shape
-    pages, Hkv, page, dk = k_pages.shape
-    if dk != d or k_pages.dtype != q.dtype or k_pages.device != q.device:
-        raise ValueError("k_pages must match q in head dimension, dtype and device")
-    _check_like("out", out, q.shape, q)
+    pages, Hkv, page, _ = _check_cache(k_pages, v_pages, None, d, q, "q")
     if not isinstance(block_table, rt.Tensor) or block_table.dim() != 2:
         raise ValueError("block_table must be an int32 tensor [B, blocks]")
     B, blocks = block_table.shape
-    _check_like("block_table", block_table, (B, blocks), q, rt.int32)
-    _check_like("kv_lens", kv_lens, (B,), q, rt.int32)
-    _check_like("cu_seqlens", cu_seqlens, (B + 1,), q, rt.int32)
+    int32 = rt.int32
+    _check_each(q, ("out", out, q.shape, q.dtype), ("block_table", block_table, (B, blocks), int32), ("kv_lens", kv_lens, (B,), int32),
+                ("cu_seqlens", cu_seqlens, (B + 1,), int32))
     if lse is not None:
-        _check_like("lse", lse, (Hq, total), q, rt.float32)
+        _check_each(q, ("lse", lse, (Hq, total), rt.float32))
     _call(LIB.monarch_attn_exact_paged_fwd, q, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
           None if lse is None else lse.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr(),
           B, total, Hq, Hkv, d, ldq, pages, page, blocks, bool(causal), dtype_code(q.dtype), _stream(q, stream) or None)
@@ -590,21 +640,25 @@ def monarch_attn_paged_plan(past, fresh, ring, free_in, block_table, cu_seqlens,
     (int64 [capacity], -1 behind the last), what stays free in free_out [2] and
     0 or PLAN_* bits in status [1].  All int32 device tensors but slots."""
     rt = _torch()
-    for name, t in (("past", past), ("fresh", fresh), ("ring", ring), ("slots", slots), ("block_table", block_table)):
-        if not isinstance(t, rt.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a device tensor")
-        if t.dim() != (2 if name == "block_table" else 1):
-            raise ValueError(f"{name} must have {2 if name == 'block_table' else 1} dimension(s)")
-    B, blocks = past.shape[0], block_table.shape[1]
-    for name, t, shape in (("past", past, (B,)), ("fresh", fresh, (B,)), ("ring", ring, ring.shape),
-                           ("free_in", free_in, (2,)), ("block_table", block_table, (B, blocks)),
-                           ("cu_seqlens", cu_seqlens, (B + 1,)), ("kv_lens", kv_lens, (B,)), ("free_out", free_out, (2,)),
-                           ("status", status, (1,))):
-        _check_like(name, t, shape, past, rt.int32)
-    _check_like("slots", slots, slots.shape, past, rt.int64)
+    int32 = rt.int32
+    try:
+        (B,), (F,), (capacity,), (_, blocks) = past.shape, ring.shape, slots.shape, block_table.shape
+        ok = past.is_cuda
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok:
+        for name, t in (("past", past), ("ring", ring), ("slots", slots), ("block_table", block_table)):
+            if not isinstance(t, rt.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a device tensor")
+            if t.dim() != (2 if name == "block_table" else 1):
+                raise ValueError(f"{name} must have {2 if name == 'block_table' else 1} dimension(s)")
+    _check_each(past, ("past", past, (B,), int32), ("fresh", fresh, (B,), int32), ("ring", ring, (F,), int32),
+                ("free_in", free_in, (2,), int32), ("block_table", block_table, (B, blocks), int32),
+                ("cu_seqlens", cu_seqlens, (B + 1,), int32), ("kv_lens", kv_lens, (B,), int32),
+                ("slots", slots, (capacity,), rt.int64), ("free_out", free_out, (2,), int32), ("status", status, (1,), int32))
     _call(LIB.monarch_attn_paged_plan, past, past.data_ptr(), fresh.data_ptr(), ring.data_ptr(), free_in.data_ptr(),
           block_table.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), free_out.data_ptr(),
-          status.data_ptr(), B, ring.shape[0], blocks, page, slots.shape[0], _stream(past, stream) or None)
+          status.data_ptr(), B, F, blocks, page, capacity, _stream(past, stream) or None)
     return block_table, cu_seqlens, kv_lens, slots, free_out, status
 
 
@@ -612,15 +666,18 @@ def monarch_attn_paged_write(k, v, k_pages, v_pages, slots, stream=None):
     """Rows of k and v [rows, Hkv, d] (may be strided) into the slots (int64
     [rows], all different; -1: nowhere) of k_pages and v_pages
     [pages, Hkv, page, d].  Returns (k_pages, v_pages)."""
-    ldk, ldv = _check_rows("k", k, k, "k"), _check_rows("v", v, k, "k")
-    _check_cache(k_pages, v_pages)
-    rows, Hkv, d = k.shape
-    pages, heads, page, dk = k_pages.shape
-    if v.shape != k.shape:
+    try:
+        ok = k.is_cuda and v.shape == k.shape
+        ldk, ldv = _rows(k, k.dtype, k.device), _rows(v, k.dtype, k.device)
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok or ldk < 0 or ldv < 0:
+        _check_rows("k", k, k, "k")
+        _check_rows("v", v, k, "k")
         raise ValueError("v must match k in shape")
-    if (heads, dk) != (Hkv, d) or k_pages.dtype != k.dtype or k_pages.device != k.device:
-        raise ValueError("k_pages must match k in heads, head dimension, dtype and device")
-    _check_like("slots", slots, (rows,), k, _torch().int64)
+    rows, Hkv, d = k.shape
+    pages, _, page, _ = _check_cache(k_pages, v_pages, Hkv, d, k, "k")
+    _check_each(k, ("slots", slots, (rows,), _torch().int64))
     _call(LIB.monarch_attn_paged_write, k, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
           slots.data_ptr(), rows, Hkv, d, ldk, ldv, pages, page, dtype_code(k.dtype), _stream(k, stream) or None)
     return k_pages, v_pages

@@ -449,15 +449,12 @@ int backward(const void *q, const void *k, const void *v, const void *dout, void
 
 namespace ma_host {
 
-int begin_call(hipStream_t stream, CallScope &c)
-{
-    const int rc = current_device(c.dev, c.num_cus);
-    return rc != MA_OK ? rc : check_capture(stream, c.capturing);
-}
+int begin_call(CallScope &c) { return current_device(c.dev, c.num_cus); }
 
 int call_workspace(hipStream_t stream, size_t need, CallScope &c)
 {
-    return acquire_workspace(c.dev, stream, c.capturing, need, &c.ws, c.hold);
+    const int rc = check_capture(stream, c.capturing);
+    return rc != MA_OK ? rc : acquire_workspace(c.dev, stream, c.capturing, need, &c.ws, c.hold);
 }
 
 int run_launches(hipStream_t stream, int (*f)(Launcher &, void *), void *arg)
@@ -465,8 +462,11 @@ int run_launches(hipStream_t stream, int (*f)(Launcher &, void *), void *arg)
     std::unique_lock<std::mutex> tlock(g_timing_mutex);
     Launcher L{stream, g_timing.enabled};
     if (!L.timed) tlock.unlock();
+    bool capturing = false;
+    int rc = L.timed ? check_capture(stream, capturing) : MA_OK;
+    if (rc != MA_OK) return rc;
     (void)hipGetLastError();  // clear a stale error so the check below is ours
-    const int rc = f(L, arg);
+    rc = f(L, arg);
     if (L.timed) {
         g_timing.nlaunch = L.n;
         g_timing.ready = (rc == MA_OK && L.n > 0);

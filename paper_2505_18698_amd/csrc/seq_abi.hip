@@ -83,8 +83,8 @@ int check_stride(const char *name, int64_t ld, int64_t width, int32_t dtype)
     return MA_OK;
 }
 
-// Row tiles of R packed rows over all sequences, at most (tile0 in seq_tiles.hpp).
-int64_t tiles_of(int64_t total, int64_t rows_a_token, int64_t B, int64_t R) { return total * rows_a_token / R + B; }
+// Row tiles of R packed rows over all sequences, at most (tile0 in seq_tiles.hpp), and one without any.
+int64_t tiles_of(int64_t total, int64_t rows_a_token, int64_t B, int64_t R) { return std::max<int64_t>(1, total * rows_a_token / R + B); }
 
 int check_grid(int64_t units, int64_t Hkv)
 {
@@ -136,7 +136,7 @@ struct BwdLaunch {
 
 int packed_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest, const int32_t *cu, int64_t B,
                int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal,
-               int32_t dtype, hipStream_t stream)
+               int32_t clear, int32_t dtype, hipStream_t stream)
 {
     MA_TRY(check_heads(B, total, Hq, Hkv, d, dtype));
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
@@ -144,7 +144,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
     const int64_t G = Hq / Hkv, tiles = tiles_of(total, G, B, kSeqRows);
     MA_TRY(check_grid(tiles, Hkv));
-    if (B == 0 || total == 0) return MA_OK;  // nothing to compute: no launch, no pointer read
+    if (total == 0 || (B == 0 && !clear)) return MA_OK;  // nothing to compute: no launch, no pointer read
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
                          {"k", k, span_bytes(total, ldk, Hkv * d, dtype)},
                          {"v", v, span_bytes(total, ldv, Hkv * d, dtype)},
@@ -157,15 +157,13 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     if (lse) MA_TRY(check_alignment(outs[1], 4));
     if (rest) MA_TRY(check_alignment(outs[2], 16));
     MA_TRY(check_overlaps(outs, ins));
-    CallScope c;
-    MA_TRY(begin_call(stream, c));
     FwdLaunch x{};
     ma::SeqFwd &p = x.p;
     p.q = q, p.k = k, p.v = v, p.out = out, p.lse = lse, p.rest = rest;
     p.seqs = ma::Seqs{cu, (int)B, (int)total};
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
-    p.c = log2_scale(d), p.causal = causal != 0, p.tiles = (int)tiles;
+    p.c = log2_scale(d), p.causal = causal != 0, p.clear = clear != 0, p.tiles = (int)tiles;
     x.how = SeqPlan{false, false, kSeqRows, tiles};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
@@ -189,7 +187,7 @@ int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
 
 int packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
                const void *dout, void *dq, void *dk, void *dv, const int32_t *cu, int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d,
-               int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal, int32_t dtype, hipStream_t stream)
+               int64_t ldq, int64_t ldk, int64_t ldv, int32_t causal, int32_t clear, int32_t dtype, hipStream_t stream)
 {
     MA_TRY(check_heads(B, total, Hq, Hkv, d, dtype));
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
@@ -197,7 +195,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
     const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, kSeqRows), tiles_k = tiles_of(total, 1, B, kSeqBwdKeys);
     MA_TRY(check_grid(std::max(tiles_q, tiles_k), Hkv));
-    if (B == 0 || total == 0) return MA_OK;
+    if (total == 0 || (B == 0 && !clear)) return MA_OK;
     const size_t qb = span_bytes(total, Hq * d, Hq * d, dtype), kb = span_bytes(total, Hkv * d, Hkv * d, dtype);
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
                          {"k", k, span_bytes(total, ldk, Hkv * d, dtype)},
@@ -214,7 +212,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     for (const Range &r : outs) MA_TRY(check_alignment(r, 16));
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
-    MA_TRY(begin_call(stream, c));
+    MA_TRY(begin_call(c));
     const int64_t pieces = bwd_pieces(tiles_k, Hkv, G, c.num_cus);
     const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq);
     MA_TRY(check_grid(tiles_k * pieces, Hkv));
@@ -226,7 +224,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     p.seqs = ma::Seqs{cu, (int)B, (int)total};
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
-    p.c = log2_scale(d), p.causal = causal != 0;
+    p.c = log2_scale(d), p.causal = causal != 0, p.clear = clear != 0;
     p.tiles_q = (int)tiles_q, p.tiles_k = (int)tiles_k;
     const size_t each = align_up((size_t)(Hq * total) * 4);
     p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each), p.norms = (float2 *)(c.ws + 2 * each);
@@ -309,7 +307,7 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     if (lse) MA_TRY(check_alignment(outs[1], 4));
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
-    MA_TRY(begin_call(stream, c));
+    MA_TRY(begin_call(c));
     const PagedSplit s = paged_split(total, B, G, Hkv, d, blocks * page, c.num_cus, dtype);
     if (s.split) {
         MA_TRY(check_grid(s.units, Hkv));
@@ -352,8 +350,6 @@ int paged_plan(const int32_t *past, const int32_t *fresh, const int32_t *ring, c
     for (const Range &r : outs)
         if (r.bytes) MA_TRY(check_alignment(r, &r == &outs[3] ? 8 : 4));
     MA_TRY(check_overlaps(outs, ins));
-    CallScope c;
-    MA_TRY(begin_call(stream, c));
     ma::PagedPlan p{past, fresh, ring, free_in, table, cu, kv_lens, slots, free_out, status, (int)B, (int)ring_len,
                     (int)blocks, log2_of(page), (int)capacity};
     return run_launches(stream, [](Launcher &L, void *a) { return run_paged_plan(L, *(const ma::PagedPlan *)a); }, &p);
@@ -374,8 +370,6 @@ int paged_write(const void *k, const void *v, void *k_pages, void *v_pages, cons
     for (int i = 0; i < 3; ++i) MA_TRY(check_alignment(ins[i], i < 2 ? 16 : 8));
     for (const Range &r : outs) MA_TRY(check_alignment(r, 16));
     MA_TRY(check_overlaps(outs, ins));
-    CallScope c;
-    MA_TRY(begin_call(stream, c));
     ma::PagedWrite p{k, v, k_pages, v_pages, slots, (int)rows, (int)Hkv, (int)d, log2_of(page), (int)pages,
                      (int)elem_bytes(dtype), ldk, ldv};
     return run_launches(stream, [](Launcher &L, void *a) { return run_paged_write(L, *(const ma::PagedWrite *)a); }, &p);
@@ -387,22 +381,22 @@ extern "C" {
 
 int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
                                   const int32_t *cu_seqlens, int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk,
-                                  int64_t ldv, int32_t causal, int32_t dtype, void *stream)
+                                  int64_t ldv, int32_t causal, int32_t clear, int32_t dtype, void *stream)
 {
     g_err[0] = '\0';
     return guarded([&] {
-        return packed_fwd(q, k, v, out, lse, rest, cu_seqlens, B, total, Hq, Hkv, d, ldq, ldk, ldv, causal, dtype, (hipStream_t)stream);
+        return packed_fwd(q, k, v, out, lse, rest, cu_seqlens, B, total, Hq, Hkv, d, ldq, ldk, ldv, causal, clear, dtype, (hipStream_t)stream);
     });
 }
 
 int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,
                                   const void *rest, const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_seqlens, int64_t B,
                                   int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk, int64_t ldv,
-                                  int32_t causal, int32_t dtype, void *stream)
+                                  int32_t causal, int32_t clear, int32_t dtype, void *stream)
 {
     g_err[0] = '\0';
     return guarded([&] {
-        return packed_bwd(q, k, v, out, lse, rest, dout, dq, dk, dv, cu_seqlens, B, total, Hq, Hkv, d, ldq, ldk, ldv, causal, dtype,
+        return packed_bwd(q, k, v, out, lse, rest, dout, dq, dk, dv, cu_seqlens, B, total, Hq, Hkv, d, ldq, ldk, ldv, causal, clear, dtype,
                           (hipStream_t)stream);
     });
 }

@@ -348,6 +348,8 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             unit = uniform((int64_t)(f.unit0 + f.split) * p.Hkv + kvh);
             if (f.split == 0 && kvh == 0 && tid == 0) p.parts[1 + f.index] = SeqTileParts{seq, tile, f.splits, f.unit0};
         } else {
+            if constexpr (!PAGED)
+                if (p.clear) clear_outside<NTH>(p.seqs, p.out, (int64_t)p.Hkv * p.G * p.d * sizeof(T), blockIdx.x, gridDim.x);
             const int64_t t = p.tiles - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
             seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
             if (seq < 0) return;

@@ -54,6 +54,11 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
 {
     constexpr int V = 16 / (int)sizeof(T);
     const int Hq = p.Hkv * p.G, lane = threadIdx.x & 15;
+    if (p.clear) {
+        clear_outside<256>(p.seqs, p.dq, (int64_t)Hq * p.d * sizeof(T), blockIdx.x, gridDim.x);
+        clear_outside<256>(p.seqs, p.dk, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
+        clear_outside<256>(p.seqs, p.dv, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
+    }
     const int first = p.seqs.start(0), last = p.seqs.start(p.seqs.B);  // (rows of no sequence count for nothing)
     const int64_t step = (int64_t)gridDim.x * 16, own = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     float most_g = 0.f, most_v = 0.f;

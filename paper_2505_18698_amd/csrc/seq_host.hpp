@@ -29,8 +29,8 @@ struct CallScope {
     char *ws = nullptr;
     std::unique_lock<std::mutex> hold;
 };
-// The current device and whether `stream` is under capture.
-int begin_call(hipStream_t stream, CallScope &c);
+// The current device.
+int begin_call(CallScope &c);
 // Its workspace, grown to `need` bytes (acquire_workspace).
 int call_workspace(hipStream_t stream, size_t need, CallScope &c);
 // Run the launches of one call, timed if timing is on, and check for launch errors.

@@ -29,6 +29,7 @@ struct SeqFwd {
     int page_log2, pages, blocks;
     float c;                // s log2(e)
     int causal;
+    int clear;              // packed: write zeros in the rows of no sequence
     int tiles;              // row tiles of one key head (an upper bound)
     // split over the keys: the units' rows, normalised, and their log2-sum-exp,
     // and for every row tile what its units are
@@ -52,6 +53,7 @@ struct SeqBwd {
     int64_t ldq, ldk, ldv;
     float c;                             // s log2(e)
     int causal;
+    int clear;                           // write zeros in the gradients' rows of no sequence
     int tiles_q, tiles_k;                // row and key tiles of one key head (upper bounds)
     float *lse2, *delta;                 // [Hq, total]: lse in log2 units, delta
     float2 *norms;                       // fp16: the largest |dO_i|^2 and |v_j|^2 of every workgroup of seq_stats

@@ -279,6 +279,16 @@ template <int NTH> __device__ inline bool some_thread(bool x, int *shared)
 
 // ---- sequences ----
 
+// Zeros in the rows of no sequence of x, rows of `bytes` bytes (a multiple of
+// 16): the share of workgroup `block` of `blocks`.
+template <int NTH> __device__ inline void clear_outside(const Seqs &q, void *x, int64_t bytes, int64_t block, int64_t blocks)
+{
+    const int first = q.start(0), last = max(first, q.start(q.B));
+    const int64_t before = first * bytes / 16, all = before + (q.total - last) * bytes / 16;
+    for (int64_t i = block * NTH + threadIdx.x; i < all; i += blocks * NTH)
+        reinterpret_cast<u32x4 *>(x)[i < before ? i : i - before + last * bytes / 16] = u32x4{0u, 0u, 0u, 0u};
+}
+
 // Sequence s holds tiles tile0(s) .. tile0(s) + ceil(rows / R) - 1 of R packed
 // rows, tile0(s) = floor(first row / R) + s: with ceil(n / R) <= floor((x + n) / R)
 // - floor(x / R) + 1 the ranges of two sequences never meet, and no prefix sum
@@ -289,6 +299,7 @@ __device__ inline int64_t tile0(const Seqs &q, int s, int G, int R) { return (in
 // or -1 where t is no tile of any.
 __device__ inline int seq_of_tile(const Seqs &q, int64_t t, int G, int R, int lane)
 {
+    if (q.B == 0) return -1;
     int lo = 0, n = q.B;
     while (n > 1) {
         const int step = (n + 63) / 64;

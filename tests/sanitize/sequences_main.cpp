@@ -39,7 +39,7 @@ int main()
     float *L = reinterpret_cast<float *>(O);
     const int64_t big = INT64_MAX;
     auto fwd = [&](int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t ld, int32_t dtype) {
-        return monarch_attn_exact_packed_fwd(F, F, F, O, nullptr, nullptr, I, B, total, Hq, Hkv, d, ld, ld, ld, 1, dtype, nullptr);
+        return monarch_attn_exact_packed_fwd(F, F, F, O, nullptr, nullptr, I, B, total, Hq, Hkv, d, ld, ld, ld, 1, 0, dtype, nullptr);
     };
     expect(fwd(-1, 8, 4, 2, 64, 256, 1), MA_EINVAL, "B < 0");
     expect(fwd(1, 8, 4, 3, 64, 256, 1), MA_EINVAL, "Hq not a multiple of Hkv");
@@ -54,12 +54,12 @@ int main()
     expect(fwd(0, 8, 4, 2, 64, 256, 1), MA_OK, "no sequence");
     expect(fwd(1, 0, 4, 2, 64, 256, 0), MA_OK, "no row");
     expect(fwd(1, 8, 4, 2, 64, 256, 5), MA_EINVAL, "dtype");
-    expect(monarch_attn_exact_packed_fwd(F, F, F, F + 64, nullptr, nullptr, I, 1, 8, 4, 2, 64, 256, 256, 256, 1, 1, nullptr), MA_EINVAL,
+    expect(monarch_attn_exact_packed_fwd(F, F, F, F + 64, nullptr, nullptr, I, 1, 8, 4, 2, 64, 256, 256, 256, 1, 0, 1, nullptr), MA_EINVAL,
            "out overlaps q");
-    expect(monarch_attn_exact_packed_bwd(F, F, F, F, L, nullptr, F, O, O, O, I, 1, 8, 4, 2, 64, 256, 256, 256, 1, 1, nullptr), MA_EINVAL,
+    expect(monarch_attn_exact_packed_bwd(F, F, F, F, L, nullptr, F, O, O, O, I, 1, 8, 4, 2, 64, 256, 256, 256, 1, 0, 1, nullptr), MA_EINVAL,
            "gradients overlap");
     expect(monarch_attn_exact_packed_bwd(nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
-                                         nullptr, 0, 0, 4, 2, 64, 256, 256, 256, 1, 1, nullptr),
+                                         nullptr, 0, 0, 4, 2, 64, 256, 256, 256, 1, 0, 1, nullptr),
            MA_OK, "empty gradient");
     auto paged = [&](int64_t pages, int64_t page, int64_t blocks, int64_t B) {
         return monarch_attn_exact_paged_fwd(F, F, F, F, nullptr, I, I, I, B, 8, 4, 2, 64, 256, pages, page, blocks, 1, 1, nullptr);

@@ -223,6 +223,20 @@ def test_autograd(ma, dtype):
         assert torch.equal(x, got[name])
 
 
+def test_clear(ma):
+    """Rows of no sequence are written as zero on request, without a sequence all rows."""
+    q, k, v, dout, cu = _inputs([40, 0, 9], 4, 2, 64, "bf16", 21, spare=700, first=300)
+    for at in (cu, cu[3:].contiguous()):
+        out, lse = torch.full_like(dout, 7.0), torch.zeros(4, dout.shape[0], device="cuda")
+        grads = [torch.full(t.shape, 7.0, device="cuda", dtype=t.dtype) for t in (q, k, v)]
+        ma.monarch_attn_exact_packed_fwd(q, k, v, out, at, True, lse, clear=True)
+        ma.monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout, *grads, at, True, clear=True)
+        torch.cuda.synchronize()
+        real = torch.zeros(dout.shape[0], dtype=torch.bool, device="cuda")
+        real[300:349] = at is cu
+        assert all(bool((t[~real] == 0).all()) and bool((t[real] != 0).any() == (at is cu)) for t in (out, *grads))
+
+
 def test_empty_calls(ma):
     for lens, rows in (([], 0), ([], 5), ([0, 0, 0], 5)):
         q = torch.randn(rows, 4, 64, device="cuda").bfloat16()

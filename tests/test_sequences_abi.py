@@ -11,14 +11,14 @@ HUGE = 1 << 62
 
 def _packed(**x):
     a = dict(q=A[0], k=A[1], v=A[2], out=A[3], lse=A[4], rest=None, cu=A[5], B=2, total=100, Hq=8, Hkv=2, d=64, ldq=512, ldk=128,
-             ldv=128, causal=1, dtype=1, stream=None)
+             ldv=128, causal=1, clear=0, dtype=1, stream=None)
     a.update(x)
     return ma.LIB.monarch_attn_exact_packed_fwd(*a.values())
 
 
 def _packed_bwd(**x):
     a = dict(q=A[0], k=A[1], v=A[2], out=A[3], lse=A[4], rest=None, dout=A[6], dq=A[7], dk=A[8], dv=A[9], cu=A[5], B=2, total=100,
-             Hq=8, Hkv=2, d=64, ldq=512, ldk=128, ldv=128, causal=1, dtype=1, stream=None)
+             Hq=8, Hkv=2, d=64, ldq=512, ldk=128, ldv=128, causal=1, clear=0, dtype=1, stream=None)
     a.update(x)
     return ma.LIB.monarch_attn_exact_packed_bwd(*a.values())
 
@@ -113,6 +113,8 @@ def test_calls_with_nothing_to_compute():
     for empty in (dict(B=0), dict(total=0)):
         assert _packed(**nothing, **empty) == ma.MA_OK
         assert _packed_bwd(**nothing, dout=None, dq=None, dk=None, dv=None, **empty) == ma.MA_OK
+        if "B" in empty:  # rows of no sequence are cleared all the same: the pointers are needed
+            assert _packed(**nothing, **empty, clear=1) == _packed_bwd(**nothing, dout=None, **empty, clear=1) == ma.MA_EINVAL
         assert _paged(**nothing, kv=None, table=None, **empty) == ma.MA_OK
     assert _write(rows=0, k=None, v=None, kp=None, vp=None, slots=None) == ma.MA_OK
     assert _write(pages=0, k=None, v=None, kp=None, vp=None, slots=None) == ma.MA_OK
