@@ -252,27 +252,26 @@ int log2_of(int64_t page)
 
 // How a paged call runs.  Sequences of few new rows (on average no more than 32
 // packed ones: single tokens) take 32-row tiles, whose waves share the keys.
-// The keys are split into units of equal length, a few times as many as the
-// device holds workgroups (two a compute unit), so that long and short contexts of a
-// batch fill it evenly: the more rows a tile has, the more a unit's partial result costs.  A call
-// with many times as many row tiles is not split, nor is one whose longest possible context is a few key tiles.
+// The work is shared evenly by as many workgroups as the device holds at a time
+// (two a compute unit; find_share in seq_attn.hpp), except where the longest possible context
+// is a few key tiles, or where there are many times as many row tiles: then a row tile is a workgroup's.
 struct PagedSplit {
     int rows;
     bool split;
-    int64_t tiles, target, units;
+    int64_t tiles, units;
     size_t bytes_o, bytes_l, bytes_parts;
 };
 
 PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t max_keys, int64_t num_cus, int32_t dtype)
 {
     const bool few = total * G <= B * kSeqFewRows;
-    PagedSplit s{few ? kSeqFewRows : kSeqRows, false, 0, 0, 0, 0, 0, 0};
+    PagedSplit s{few ? kSeqFewRows : kSeqRows, false, 0, 0, 0, 0, 0};
     s.tiles = s.units = tiles_of(total, G, B, s.rows);
-    s.target = std::max<int64_t>(1, (few ? 8 : 4) * num_cus / Hkv);
-    if (s.tiles >= 4 * s.target || max_keys <= 16 * seq_tile_keys(dtype)) return s;
+    const int64_t shares = std::max<int64_t>(1, 2 * num_cus / Hkv);
+    if (s.tiles >= 16 * shares || max_keys <= 16 * seq_tile_keys(dtype)) return s;
     s.split = true;
-    s.units = s.target + s.tiles;
-    const size_t rows = (size_t)s.units * Hkv * s.rows;
+    s.units = shares;
+    const size_t rows = (size_t)(shares + s.tiles) * Hkv * s.rows;
     s.bytes_o = align_up(rows * tile_d(d) * 4);
     s.bytes_l = align_up(rows * 4);
     s.bytes_parts = align_up((size_t)(s.tiles + 1) * sizeof(ma::SeqTileParts));
@@ -324,7 +323,7 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     p.c = log2_scale(d), p.causal = causal != 0, p.tiles = (int)s.tiles;
     p.part_o = (float *)c.ws, p.part_l = (float *)(c.ws + s.bytes_o);
     p.parts = (ma::SeqTileParts *)(c.ws + s.bytes_o + s.bytes_l);
-    p.target = (int)s.target;
+    p.shares = (int)s.units;
     x.how = SeqPlan{true, s.split, s.rows, s.units};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);

@@ -9,17 +9,26 @@
 
 namespace ma {
 
-// How a split call divides its work: every sequence's row tiles (R rows) times
-// its pieces of `piece` key tiles (BN keys).  All sequences share one piece
-// length, the shortest that gives about `target` units, so that long and short
-// contexts of a batch end together.
-struct Pieces {
-    int seq, tile, split, splits, piece;  // of the unit searched for (seq = -1: none)
-    int index, unit0;                     // number of its tile, and of the tile's first unit
+// How a split call divides its work.  All row tiles of R rows in order, each with
+// the key tiles (BN keys) of its sequence, are one line of `all` steps, which the
+// workgroups share evenly: share w takes the steps from w all / shares on, in segments that
+// lie in one row tile each.  So every workgroup ends at the same time whatever the
+// contexts are, and starts once.  A row tile counts kBegin steps more than it has, for
+// what its first copies, its rows and its masked key tiles take (measured: 8 us to a step's 2 with 128
+// rows, 6 to 2.4 with 32; without, the workgroups of 8 chunks of up to 512 tokens
+// ended between 153 and 257 us).  The segment of share w in row tile i has the
+// number w + i, as both only grow along the line.
+template <int R> constexpr int kBegin = R > 32 ? 4 : 2;
+struct Line {
+    int64_t all;       // steps
+    int shares;        // workgroups that share them, four steps each at least
+    int seq, tile;     // the row tile of the share's first step (seq = -1: none)
+    int index;         // its number
+    int64_t at;        // its first step
 };
 
 template <int R, int BN, int NTH>
-__device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, int max_keys, char *lds)
+__device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char *lds)
 {
     int64_t *sh = reinterpret_cast<int64_t *>(lds);
     constexpr int W = NTH / 64;
@@ -27,29 +36,29 @@ __device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, int max_keys,
     auto shape = [&](int s, int &rt, int &kt) {
         rt = s < p.seqs.B ? (int)(((int64_t)p.seqs.length(s) * p.G + R - 1) / R) : 0;
         const int kv = s < p.seqs.B ? max(0, min(p.kv_lens[s], max_keys)) : 0;
-        kt = max(1, (kv + BN - 1) / BN);
+        kt = kBegin<R> + max(1, (kv + BN - 1) / BN);
     };
-    // all work, in row tiles times key tiles, and all row tiles
-    int64_t sum = 0, all = 0;
+    int64_t sum = 0, tiles = 0;
     for (int s = tid; s < p.seqs.B; s += NTH) {
         int rt, kt;
         shape(s, rt, kt);
-        sum += (int64_t)rt * kt, all += rt;
+        sum += (int64_t)rt * kt, tiles += rt;
     }
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x), all += __shfl_xor(all, x);
-    if (lane == 0) sh[2 * wave] = sum, sh[2 * wave + 1] = all;
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x), tiles += __shfl_xor(tiles, x);
+    if (lane == 0) sh[2 * wave] = sum, sh[2 * wave + 1] = tiles;
     __syncthreads();
-    sum = all = 0;
-    for (int i = 0; i < W; ++i) sum += sh[2 * i], all += sh[2 * i + 1];
+    sum = tiles = 0;
+    for (int i = 0; i < W; ++i) sum += sh[2 * i], tiles += sh[2 * i + 1];
     __syncthreads();
-    if (blockIdx.x == 0 && tid == 0) p.parts[0].splits = (int)all;
-    Pieces r{-1, 0, 0, 1, (int)max((int64_t)2, (sum + p.target - 1) / p.target), 0, 0};
-    int64_t tiles_before = 0, units_before = 0;
+    if (blockIdx.x == 0 && tid == 0) p.parts[0].seq = (int)tiles;
+    Line r{sum, (int)max((int64_t)1, min((int64_t)p.shares, sum / 4)), -1, 0, 0, 0};
+    if (share >= r.shares) return r;
+    const int64_t want = sum * share / r.shares;
+    int64_t steps_before = 0, tiles_before = 0;
     for (int s0 = 0; s0 < p.seqs.B; s0 += NTH) {
         int rt, kt;
         shape(s0 + tid, rt, kt);
-        const int splits = (kt + r.piece - 1) / r.piece;
-        int64_t t = rt, u = (int64_t)rt * splits;  // inclusive sums over the threads
+        int64_t t = rt, u = (int64_t)rt * kt;  // inclusive sums over the threads
         for (int x = 1; x < 64; x <<= 1) {
             const int64_t a = __shfl_up(t, x), b = __shfl_up(u, x);
             if (lane >= x) t += a, u += b;
@@ -62,23 +71,24 @@ __device__ inline Pieces find_piece(const SeqFwd &p, int64_t want, int max_keys,
             at += sh[2 * i], au += sh[2 * i + 1];
         }
         __syncthreads();
-        const int64_t u0 = units_before + u - (int64_t)rt * splits, k = want - u0;
-        const bool mine = k >= 0 && k < (int64_t)rt * splits;  // one thread at most
+        const int64_t u0 = steps_before + u - (int64_t)rt * kt, k = want - u0;
+        const bool mine = k >= 0 && k < (int64_t)rt * kt;  // one thread at most
         if (mine) {
-            const int tile = (int)(k / splits);
-            sh[0] = s0 + tid, sh[1] = tile, sh[2] = k - (int64_t)tile * splits, sh[3] = splits;
-            sh[4] = tiles_before + t - rt + tile, sh[5] = u0 + (int64_t)tile * splits;
+            const int tile = (int)(k / kt);
+            sh[0] = s0 + tid, sh[1] = tile, sh[2] = tiles_before + t - rt + tile, sh[3] = u0 + (int64_t)tile * kt;
         }
         if (some_thread<NTH>(mine, reinterpret_cast<int *>(lds + 64))) {
-            r.seq = (int)sh[0], r.tile = (int)sh[1], r.split = (int)sh[2], r.splits = (int)sh[3];
-            r.index = (int)sh[4], r.unit0 = (int)sh[5];
+            r.seq = (int)sh[0], r.tile = (int)sh[1], r.index = (int)sh[2], r.at = sh[3];
             break;
         }
-        tiles_before += at, units_before += au;
+        steps_before += au, tiles_before += at;
     }
     __syncthreads();
     return r;
 }
+
+// The share that step x of a line belongs to.
+__device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int)(((x + 1) * shares - 1) / all); }
 
 // One workgroup of 4 waves per tile of R = 32 RB WR packed rows (token, head of
 // the group) of one key head: the heads of a group read the same K and V, so
@@ -97,7 +107,11 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     static constexpr int KW = WR == 1 ? BN / 32 : 1;       // waves that share a tile's keys
     static_assert(WR == W || WR == 1, "rows or keys over the waves");
     static constexpr int TILE = BN * S::ROW;
-    static constexpr int LDS_BYTES = 4 * TILE + 16;  // K and V, two of each
+    // Tiles that are there or on their way.  Short contexts of few rows are bound
+    // by the latency of one tile after another: four; two where two workgroups a
+    // compute unit need the room.
+    static constexpr int STAGES = WR == 1 && (D * sizeof(T) <= 128 || !SPLIT) ? 4 : 2;
+    static constexpr int LDS_BYTES = 2 * STAGES * TILE + 16;  // K and V
     using Copy = TileCopy<T, D, BN, W>;
     // A row's weights are taken relative to a reference that follows its running
     // maximum only when that has grown by more than 2^kSlack: the sums stay exact
@@ -259,7 +273,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     __device__ static void join_waves(char *lds, int wave, int lane, State &st)
     {
         constexpr int N = S::ND * 16 + 2;  // a lane's values of a row block
-        static_assert((KW - 1) * RB * N * 256 <= 4 * TILE, "the tiles' room holds them");
+        static_assert((KW - 1) * RB * N * 256 <= 2 * STAGES * TILE, "the tiles' room holds them");
         float *mine = reinterpret_cast<float *>(lds) + (wave - 1) * RB * N * 64 + lane;
         __syncthreads();
         if (wave > 0 && wave < KW) {
@@ -299,28 +313,30 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         const int *table;  // paged: the sequence's pages
         int kv;            // rows from this one on read as zero
         Copy ck, cv;
-        int page[Copy::COPIES];  // paged: of the tile that is copied next
+        int pages, page0;  // paged: lane i holds the sequence's page page0 + i
 
-        // the pages of the tile from key0 on (a tile ahead of their use)
-        __device__ void look(const SeqFwd &p, int key0, int wave)
+        // the pages of the tile from key0 on are among those that the lanes hold
+        __device__ void look(const SeqFwd &p, int key0, int lane)
         {
-#pragma unroll
-            for (int i = 0; i < Copy::COPIES; ++i) {
-                const int key = key0 + Copy::row(i, wave);
-                page[i] = key < kv ? table[key >> p.page_log2] : 0;
-            }
+            const int from = key0 >> p.page_log2, to = (key0 + BN - 1) >> p.page_log2;
+            if (to - page0 < 64) return;
+            page0 = from;
+            pages = from + lane <= (kv - 1) >> p.page_log2 ? table[from + lane] : 0;
         }
         // the tile from key0 on
-        __device__ void copy(const SeqFwd &p, int key0, char *kt, char *vt, int wave)
+        __device__ void copy(const SeqFwd &p, int key0, char *kt, char *vt, int wave, int lane)
         {
             if constexpr (PAGED) {
                 // a page holds the rows of a copy or several copies'
+                look(p, key0, lane);
+                const int ld = p.d * (int)sizeof(T);
+                const int64_t each = (int64_t)(p.Hkv << p.page_log2) * p.d;
 #pragma unroll
                 for (int i = 0; i < Copy::COPIES; ++i) {
-                    const int key = key0 + Copy::row(i, wave), ld = p.d * (int)sizeof(T);
-                    const int pg = uniform(page[i]);
+                    const int key = key0 + Copy::row(i, wave);
+                    const int pg = __builtin_amdgcn_readlane(pages, min((key >> p.page_log2) - page0, 63));
                     const bool ok = (unsigned)pg < (unsigned)p.pages;
-                    const int64_t at = ok ? (((int64_t)pg * p.Hkv << p.page_log2) + (key & ((1 << p.page_log2) - 1))) * p.d : 0;
+                    const int64_t at = ok ? pg * each + (key & ((1 << p.page_log2) - 1)) * p.d : 0;
                     ck.one(ok ? (const void *)(k + at) : &kNanRows, min(kv - key, Copy::RPC), ld, kt, i, wave);
                     ck.one(v + at, ok ? min(kv - key, Copy::RPC) : 0, ld, vt, i, wave);
                 }
@@ -334,27 +350,52 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 
     __device__ static void run(const SeqFwd &p, char *lds)
     {
-        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         const int kvh = uniform((int)(blockIdx.x % p.Hkv));
-        int seq, tile, key_tile0 = 0, key_tiles = 0x7fffffff;
-        int64_t unit = 0;
-        bool parts = false;
         const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0) : 0;
         if constexpr (SPLIT) {
-            const Pieces f = find_piece<R, BN, NTH>(p, blockIdx.x / p.Hkv, max_keys, lds);
-            if (f.seq < 0) return;
-            seq = uniform(f.seq), tile = uniform(f.tile), parts = f.splits > 1;
-            key_tile0 = uniform(f.split * f.piece), key_tiles = uniform(f.piece);
-            unit = uniform((int64_t)(f.unit0 + f.split) * p.Hkv + kvh);
-            if (f.split == 0 && kvh == 0 && tid == 0) p.parts[1 + f.index] = SeqTileParts{seq, tile, f.splits, f.unit0};
+            const int share = uniform((int)(blockIdx.x / p.Hkv));
+            Line f = find_share<R, BN, NTH>(p, share, max_keys, lds);
+            int seq = uniform(f.seq), tile = uniform(f.tile), index = uniform(f.index);
+            if (seq < 0) return;
+            const int shares = uniform(f.shares);
+            const int64_t all = uniform(f.all), end = all * (share + 1) / shares;
+            int64_t at = uniform(f.at), x = all * share / shares;
+            while (x < end) {
+                const int n = uniform(p.seqs.length(seq)), kv = uniform(max(0, min(p.kv_lens[seq], max_keys)));
+                const int tiles = (int)(((int64_t)n * p.G + R - 1) / R), steps = max(1, (kv + BN - 1) / BN);
+                if (tile >= tiles) {  // the next sequence
+                    ++seq, tile = 0;
+                    continue;
+                }
+                const int64_t begin = at + kBegin<R>, from = max(x, begin), stop = min(end, begin + steps);
+                if (from < stop) {
+                    const bool whole = from == begin && stop == begin + steps;
+                    if (from == begin && kvh == 0 && tid == 0) {
+                        const int last = share_of(begin + steps - 1, all, shares);
+                        p.parts[1 + index] = SeqTileParts{seq, tile, share, last - share + 1};
+                    }
+                    segment(p, lds, tid, lane, wave, kvh, seq, tile, (int)(from - begin), (int)(stop - from), !whole,
+                            (int64_t)(share + index) * p.Hkv + kvh, max_keys);
+                    __syncthreads();  // the tiles' room is used again
+                }
+                at += kBegin<R> + steps, x = at, ++tile, ++index;
+            }
         } else {
             if constexpr (!PAGED)
                 if (p.clear) clear_outside<NTH>(p.seqs, p.out, (int64_t)p.Hkv * p.G * p.d * sizeof(T), blockIdx.x, gridDim.x);
             const int64_t t = p.tiles - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
-            seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
+            const int seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
             if (seq < 0) return;
-            tile = uniform((int)(t - tile0(p.seqs, seq, p.G, R)));
+            segment(p, lds, tid, lane, wave, kvh, seq, uniform((int)(t - tile0(p.seqs, seq, p.G, R))), 0, 0x7fffffff, false, 0, max_keys);
         }
+    }
+
+    // Row tile `tile` of a sequence against `key_tiles` key tiles from key_tile0 on.
+    // parts: the rows go to segment `unit` of the partial results.
+    __device__ static __forceinline__ void segment(const SeqFwd &p, char *lds, int tid, int lane, int wave, int kvh, int seq, int tile,
+                                                   int key_tile0, int key_tiles, bool parts, int64_t unit, int max_keys)
+    {
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
         const int kv = PAGED ? uniform(max(0, min(p.kv_lens[seq], max_keys))) : n;
         const int rows = n * p.G, r0 = tile * R;
@@ -396,6 +437,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             src.k = (const T *)p.k + ((int64_t)kvh << p.page_log2) * p.d;
             src.v = (const T *)p.v + ((int64_t)kvh << p.page_log2) * p.d;
             src.table = p.table + (int64_t)seq * p.blocks;
+            src.page0 = -0x10000, src.pages = 0;  // none yet
             src.ck.init(p.d * (int)sizeof(T), p.d, wave, lane);
         } else {
             const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
@@ -412,31 +454,40 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 #pragma unroll
             for (int dt = 0; dt < S::ND; ++dt) st.o[rb][dt] = f32x16{};
         }
-        // The tile from `key0` on arrives while the one before it is computed.  Two
+        // A tile arrives while the one or two before it are computed.  Two
         // loops, the tiles that every row sees whole and the others: one loop
         // with both kinds of step keeps the output registers twice.
         auto bring = [&](int key0, int buf) {
             if (key0 >= last) return;
-            src.copy(p, key0, lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, wave);
-            if constexpr (PAGED) src.look(p, key0 + BN, wave);
+            src.copy(p, key0, lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, wave, lane);
         };
-        if constexpr (PAGED) src.look(p, first, wave);
-        bring(first, 0);
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) bring(first + i * BN, i);
         int key0 = first, buf = 0;
+        auto arrive = [&] {
+            if constexpr (STAGES == 2) {
+                tile_barrier();
+            } else {
+                const int later = min(STAGES - 2, (last - 1 - key0) / BN);  // tiles on their way behind this one
+                if (later >= 2) tile_barrier<4 * Copy::COPIES>();
+                else if (later == 1) tile_barrier<2 * Copy::COPIES>();
+                else tile_barrier();
+            }
+            bring(key0 + (STAGES - 1) * BN, buf == 0 ? STAGES - 1 : buf - 1);
+        };
+        auto next = [&] { key0 += BN, buf = buf == STAGES - 1 ? 0 : buf + 1; };
 #pragma unroll 1
-        for (; key0 + BN <= min(see_all, last); key0 += BN, buf ^= 1) {
-            tile_barrier();
-            bring(key0 + BN, buf ^ 1);
+        for (; key0 + BN <= min(see_all, last); next()) {
+            arrive();
             if (idle) continue;
             step<false>(lds + 2 * TILE * buf + part * 32 * S::ROW, lds + 2 * TILE * buf + TILE + part * 32 * S::ROW, qf, vis,
                         key0 + 32 * part, p.c, p.rest != nullptr, st, lane);
         }
 #pragma unroll 1
-        for (; key0 < last; key0 += BN, buf ^= 1) {
-            tile_barrier();
-            bring(key0 + BN, buf ^ 1);
+        for (; key0 < last; next()) {
+            arrive();
             char *vt = lds + 2 * TILE * buf + TILE;
-            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 4 * TILE)))
+            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 2 * STAGES * TILE)))
                 take_foreign(vt, vis, key0, wave == 0 || WR != 1, st, lane);
             if (key0 + 32 * part < see_most && !idle)
                 step<true>(lds + 2 * TILE * buf + part * 32 * S::ROW, vt + part * 32 * S::ROW, qf, vis, key0 + 32 * part, p.c,
@@ -505,39 +556,64 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 };
 
 template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64) ? 1 : 2) void seq_attention(SeqFwd p)
+__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64) ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
 {
     using U = SeqAttn<T, D, RB, WR, PAGED, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
 }
 
-// The pieces of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x).
-// One workgroup per row tile, key head and `gridDim.y`-th of the tile's rows; it takes a row at a
-// time, 32 threads a piece and 8 pieces at once.
+// The segments of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x).
+// One workgroup per row tile and key head, and, of 128-row tiles, 8 rows, 32
+// threads a row (they have few segments); of 32-row tiles, `gridDim.y`-th of the rows, one
+// at a time, 32 threads a segment and 8 segments at once.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
 {
     constexpr int C = D / 32;  // columns a thread
     __shared__ float sh_o[8][D], sh_l[8];
     const int kvh = blockIdx.x % p.Hkv, tile = blockIdx.x / p.Hkv;
-    if (tile >= p.parts[0].splits) return;
+    if (tile >= p.parts[0].seq) return;
     const SeqTileParts f = p.parts[1 + tile];
-    if (f.splits == 1) return;
+    if (f.count == 1) return;
     const int tid = threadIdx.x, g = tid / 32, c = tid % 32;
     const int row0 = p.seqs.start(f.seq), rows = min(p.seqs.length(f.seq) * p.G - f.tile * R, R);
+    if constexpr (R > 32) {
+        const int r = blockIdx.y * 8 + g;
+        if (r >= rows) return;
+        const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
+        float mx = -INFINITY, sum = 0.f, o[C] = {};
+        for (int x = 0; x < f.count; ++x) mx = max_nan(mx, p.part_l[base + x * each]);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        for (int x = 0; x < f.count; ++x) {
+            const float l = p.part_l[base + x * each], w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);
+            const float *src = p.part_o + (base + x * each) * D + c * C;
+            sum += w;
+#pragma unroll
+            for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);
+        }
+        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
+        const int at = f.tile * R + r, head = kvh * p.G + at % p.G;
+        const int64_t row = row0 + at / p.G;
+        T *out = (T *)p.out + (row * p.Hkv * p.G + head) * p.d + c * C;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (c * C + i < p.d) out[i] = to_elem<T>(o[i] * inv);
+        if (p.lse && c == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+        return;
+    }
     for (int r = blockIdx.y; r < rows; r += gridDim.y) {
-        const int64_t base = ((int64_t)f.unit0 * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
+        const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY;
-        for (int x = c; x < f.splits; x += 32) mx = max_nan(mx, p.part_l[base + x * each]);
+        for (int x = c; x < f.count; x += 32) mx = max_nan(mx, p.part_l[base + x * each]);
 #pragma unroll
         for (int x = 1; x < 32; x <<= 1) mx = max_nan(mx, __shfl_xor(mx, x));
         const float ref = mx == -INFINITY ? 0.f : mx;
         float sum = 0.f, o[C] = {};
 #pragma unroll 4
-        for (int x = g; x < f.splits; x += 8) {
+        for (int x = g; x < f.count; x += 8) {
             const float l = p.part_l[base + x * each];
-            const float w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);  // (a piece of which this row sees nothing is zero)
+            const float w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);  // (a segment of which this row sees nothing is zero)
             const float *src = p.part_o + (base + x * each) * D + c * C;
             sum += w;
 #pragma unroll

@@ -31,16 +31,17 @@ struct SeqFwd {
     int causal;
     int clear;              // packed: write zeros in the rows of no sequence
     int tiles;              // row tiles of one key head (an upper bound)
-    // split over the keys: the units' rows, normalised, and their log2-sum-exp,
-    // and for every row tile what its units are
+    // split over the keys: workgroups of one key head; their segments' rows,
+    // normalised, and their log2-sum-exp; and what every row tile is made of
+    int shares;
     float *part_o, *part_l;
     struct SeqTileParts *parts;
-    int target;             // units of one key head to aim at
 };
 
-// parts[0].splits: how many row tiles there are; parts[1 + i]: of tile i, the first of its units.
+// parts[0].seq: how many row tiles there are; parts[1 + i]: tile i, and the
+// first and the number of the shares that have a segment of it.
 struct SeqTileParts {
-    int seq, tile, splits, unit0;
+    int seq, tile, first, count;
 };
 
 struct SeqBwd {

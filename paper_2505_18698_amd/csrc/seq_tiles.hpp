@@ -253,13 +253,20 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
     }
 };
 
-// Every copy and load of this wave has arrived, and every wave of the workgroup
-// is here.  (The wait is the builtin, not assembly, so that the compiler knows of
-// it: it would wait again in front of the first use of what was loaded before the loop, in
+// All but the last LATER copies of this wave (and all its LDS accesses) are done.
+// (The wait is the builtin, not assembly, so that the compiler knows of it: it
+// would wait again in front of the first use of what was loaded before the loop, in
 // every iteration, and there for copies that it does not know of.)
-__device__ inline void tile_barrier()
+template <int LATER = 0> __device__ inline void copies_arrived()
 {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    static_assert(LATER < 64, "6 bits");
+    __builtin_amdgcn_s_waitcnt((LATER & 15) | 0x70 | (LATER >> 4) << 14);  // vmcnt(LATER) lgkmcnt(0)
+}
+
+// The same, and every wave of the workgroup is here.
+template <int LATER = 0> __device__ inline void tile_barrier()
+{
+    copies_arrived<LATER>();
     asm volatile("s_barrier" ::: "memory");
 }
 
