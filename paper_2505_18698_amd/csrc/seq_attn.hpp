@@ -102,15 +102,15 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
     static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
-    static constexpr int BN = S::kF32 ? 32 : 64;           // keys a tile
+    // keys a tile: of few rows in 16-bit types, where the workgroup has a context alone, 32 a wave
+    static constexpr int BN = S::kF32 ? 32 : WR == 1 && !SPLIT ? 128 : 64;
     static constexpr int KT = WR == 1 ? 1 : BN / 32;       // 32-key parts that a wave takes
     static constexpr int KW = WR == 1 ? BN / 32 : 1;       // waves that share a tile's keys
     static_assert(WR == W || WR == 1, "rows or keys over the waves");
     static constexpr int TILE = BN * S::ROW;
     // Tiles that are there or on their way.  Short contexts of few rows are bound
-    // by the latency of one tile after another: four; two where two workgroups a
-    // compute unit need the room.
-    static constexpr int STAGES = WR == 1 && (D * sizeof(T) <= 128 || !SPLIT) ? 4 : 2;
+    // by the latency of one tile after another: up to four, as the room allows.
+    static constexpr int STAGES = WR != 1 ? 2 : SPLIT ? (D * sizeof(T) <= 128 ? 4 : 2) : S::kF32 ? 4 : D <= 64 ? 3 : 2;
     static constexpr int LDS_BYTES = 2 * STAGES * TILE + 16;  // K and V
     using Copy = TileCopy<T, D, BN, W>;
     // A row's weights are taken relative to a reference that follows its running
@@ -510,43 +510,23 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             if (SPLIT && parts) {
                 const int64_t at = unit * R + wr0 - r0 + 32 * rb;
                 const Span ps(p.part_o + at * D);
-#pragma unroll
-                for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const f32x16 &x = st.o[rb][dt];
-                        ps.store<float>(f32x4{x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv},
-                                        ((lane & 31) * D + 32 * dt + 8 * e + 4 * (lane >> 5)) * 4, real);
-                    }
+                store_row<float, S::ND>(ps, st.o[rb], inv, (lane & 31) * D, D, real, lane);
                 if (real && lane < 32) p.part_l[at + lane] = l2;
                 continue;
             }
             const int at = (tok[rb] * p.Hkv * p.G + head[rb]) * p.d;
-#pragma unroll
-            for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
-                    const f32x16 &x = st.o[rb][dt];
-                    os.store<T>(f32x4{x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv},
-                                (at + col) * (int)sizeof(T), real && col < p.d);
-                }
+            store_row<T, S::ND>(os, st.o[rb], inv, at, p.d, real, lane);
             if constexpr (!S::kF32) {
                 if (p.rest) {
                     const Span es((T *)p.rest + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
 #pragma unroll
                     for (int dt = 0; dt < S::ND; ++dt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
-                            f32x4 x;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                x[i] = st.o[rb][dt][4 * e + i] * inv;
-                                x[i] -= (float)to_elem<T>(x[i]);
-                            }
-                            es.store<T>(x, (at + col) * (int)sizeof(T), real && col < p.d);
+                        for (int r = 0; r < 16; ++r) {
+                            const float x = st.o[rb][dt][r] * inv;
+                            st.o[rb][dt][r] = x - (float)to_elem<T>(x);
                         }
+                    store_row<T, S::ND>(es, st.o[rb], 1.f, at, p.d, real, lane);
                 }
             }
             if (p.lse && real && lane < 32)

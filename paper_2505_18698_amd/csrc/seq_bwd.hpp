@@ -116,20 +116,6 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
     }
 }
 
-// One row (lane % 32) of X^T, held as 32 x 32 results, to row `at` elements behind `base` of a [*, d] tensor.
-template <typename T, int ND>
-__device__ inline void store_transposed(const Span &s, const f32x16 *x, float by, int at, int d, bool real, int lane)
-{
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
-            s.store<T>(f32x4{x[dt][4 * e] * by, x[dt][4 * e + 1] * by, x[dt][4 * e + 2] * by, x[dt][4 * e + 3] * by},
-                       (at + col) * (int)sizeof(T), real && col < d);
-        }
-}
-
 // dQ: the forward's schedule.  S^T = K Q^T and dP^T = V dO^T hold one query row a
 // lane, so lse and delta are lane scalars, and dS^T feeds dQ^T += K^T dS^T from registers.
 template <typename T, int D> struct SeqBwdQ {
@@ -256,7 +242,7 @@ template <typename T, int D> struct SeqBwdQ {
                            delta, sc.ds, dq, lane);
         }
         const Span os((T *)p.dq + (int64_t)(row0 + tok0) * Hq * p.d);
-        store_transposed<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, r0 + wave * 32 + (lane & 31) < rows, lane);
+        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, r0 + wave * 32 + (lane & 31) < rows, lane);
     }
 };
 

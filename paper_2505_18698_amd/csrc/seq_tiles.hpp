@@ -177,6 +177,40 @@ template <int PRODUCTS> __device__ __forceinline__ void sched_step(int reads)
     if (reads == 2) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2, 0);
 }
 
+// One row (lane % 32) of X^T, held as 32 x 32 results, times `by`, to element `at`
+// behind a base: 16 bytes a store.  In 16-bit types a lane holds 8 bytes of every 16, its
+// partner in the other half of the wave the rest; of two such pairs each takes one.
+template <typename O, int ND>
+__device__ inline void store_row(const Span &s, const f32x16 *x, float by, int at, int d, bool real, int lane)
+{
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) {
+        if constexpr (sizeof(O) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = 32 * dt + 8 * e + 4 * (lane >> 5);
+                s.store<O>(f32x4{x[dt][4 * e] * by, x[dt][4 * e + 1] * by, x[dt][4 * e + 2] * by, x[dt][4 * e + 3] * by},
+                           (at + col) * 4, real && col < d);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                uint32_t w[4];  // columns 8 e + 4 h.. and 8 (e + 1) + 4 h.. of the row, two dwords each
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 4 * (e + i / 2) + 2 * (i % 2);
+                    O v[2] = {to_elem<O>(x[dt][r] * by), to_elem<O>(x[dt][r + 1] * by)};
+                    __builtin_memcpy(&w[i], v, 4);
+                }
+                const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+                const auto hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                const int col = 32 * dt + 8 * (e + (lane >> 5));
+                __builtin_amdgcn_raw_buffer_store_b128(u32x4{lo[0], hi[0], lo[1], hi[1]}, s.r, Span::at((at + col) * 2, real && col < d), 0, 0);
+            }
+        }
+    }
+}
+
 // A value that all lanes of the wave share, in a scalar register: the address of a copy has to be there.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ inline int64_t uniform(int64_t x)
