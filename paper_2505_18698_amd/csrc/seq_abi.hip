@@ -142,7 +142,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
     MA_TRY(check_stride("ldk", ldk, Hkv * d, dtype));
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
-    const int64_t G = Hq / Hkv, tiles = tiles_of(total, G, B, kSeqRows);
+    const int64_t G = Hq / Hkv, tiles = tiles_of(total, G, B, seq_rows(dtype));
     MA_TRY(check_grid(tiles, Hkv));
     if (total == 0 || (B == 0 && !clear)) return MA_OK;  // nothing to compute: no launch, no pointer read
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
@@ -164,7 +164,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
     p.c = log2_scale(d), p.causal = causal != 0, p.clear = clear != 0, p.tiles = (int)tiles;
-    x.how = SeqPlan{false, false, kSeqRows, tiles};
+    x.how = SeqPlan{false, false, seq_rows(dtype), tiles};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
 }
@@ -193,7 +193,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
     MA_TRY(check_stride("ldk", ldk, Hkv * d, dtype));
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
-    const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, kSeqRows), tiles_k = tiles_of(total, 1, B, kSeqBwdKeys);
+    const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, seq_rows(dtype)), tiles_k = tiles_of(total, 1, B, kSeqBwdKeys);
     MA_TRY(check_grid(std::max(tiles_q, tiles_k), Hkv));
     if (total == 0 || (B == 0 && !clear)) return MA_OK;
     const size_t qb = span_bytes(total, Hq * d, Hq * d, dtype), kb = span_bytes(total, Hkv * d, Hkv * d, dtype);
@@ -265,7 +265,7 @@ struct PagedSplit {
 PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t max_keys, int64_t num_cus, int32_t dtype)
 {
     const bool few = total * G <= B * kSeqFewRows;
-    PagedSplit s{few ? kSeqFewRows : kSeqRows, false, 0, 0, 0, 0, 0};
+    PagedSplit s{few ? kSeqFewRows : seq_rows(dtype), false, 0, 0, 0, 0, 0};
     s.tiles = s.units = tiles_of(total, G, B, s.rows);
     const int64_t shares = std::max<int64_t>(1, 2 * num_cus / Hkv);
     if (s.tiles >= 16 * shares || max_keys <= 16 * seq_tile_keys(dtype)) return s;

@@ -94,7 +94,9 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // the group) of one key head: the heads of a group read the same K and V, so
 // they share the tile's copies.  With WR = 4 each wave owns 32 RB rows.  With WR = 1, for
 // the few rows of single tokens, all waves copy, every wave takes one of the
-// tile's 32-key parts, and the first joins them at the end.  Scores are formed
+// tile's 32-key parts, and the first joins them at the end.  WR = 2, in fp32: two
+// row blocks by two 32-key parts (128 rows of 1000 keys are 54 us of a compute unit's fp32
+// products, which one long sequence of a call then lasts).  Scores are formed
 // transposed, S^T = K Q^T: a lane holds one query row's scores, so the softmax
 // statistics and the rescaling are lane scalars with one exchange between the
 // two lane halves, and the weights feed O^T = V^T P^T straight from registers.
@@ -103,10 +105,10 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     using frag = typename S::frag;
     static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
     // keys a tile: of few rows in 16-bit types, where the workgroup has a context alone, 32 a wave
-    static constexpr int BN = S::kF32 ? 32 : WR == 1 && !SPLIT ? 128 : 64;
-    static constexpr int KT = WR == 1 ? 1 : BN / 32;       // 32-key parts that a wave takes
-    static constexpr int KW = WR == 1 ? BN / 32 : 1;       // waves that share a tile's keys
-    static_assert(WR == W || WR == 1, "rows or keys over the waves");
+    static constexpr int BN = S::kF32 && WR == 1 ? 32 : WR == 1 && !SPLIT ? 128 : 64;
+    static constexpr int KT = WR == W ? BN / 32 : 1;       // 32-key parts that a wave takes
+    static constexpr int KW = BN / 32 / KT;                // waves that share a tile's keys
+    static_assert(WR * KW <= W, "rows and keys over the waves");
     static constexpr int TILE = BN * S::ROW;
     // Tiles that are there or on their way.  Short contexts of few rows are bound
     // by the latency of one tile after another: up to four, as the room allows.
@@ -273,10 +275,10 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     __device__ static void join_waves(char *lds, int wave, int lane, State &st)
     {
         constexpr int N = S::ND * 16 + 2;  // a lane's values of a row block
-        static_assert((KW - 1) * RB * N * 256 <= 2 * STAGES * TILE, "the tiles' room holds them");
-        float *mine = reinterpret_cast<float *>(lds) + (wave - 1) * RB * N * 64 + lane;
+        static_assert((KW - 1) * WR * RB * N * 256 <= 2 * STAGES * TILE, "the tiles' room holds them");
+        float *mine = reinterpret_cast<float *>(lds) + (wave - WR) * RB * N * 64 + lane;
         __syncthreads();
-        if (wave > 0 && wave < KW) {
+        if (wave >= WR && wave < KW * WR) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 mine[(rb * N + N - 2) * 64] = st.ref[rb], mine[(rb * N + N - 1) * 64] = st.sum[rb];
@@ -287,10 +289,10 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             }
         }
         __syncthreads();
-        if (wave != 0) return;
+        if (wave >= WR) return;
 #pragma unroll
         for (int w = 1; w < KW; ++w) {
-            const float *other = reinterpret_cast<float *>(lds) + (w - 1) * RB * N * 64 + lane;
+            const float *other = reinterpret_cast<float *>(lds) + ((w - 1) * WR + wave) * RB * N * 64 + lane;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const float ref = other[(rb * N + N - 2) * 64], up = fmaxf(ref, st.ref[rb]), base = up == -INFINITY ? 0.f : up;
@@ -403,9 +405,9 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             const int64_t i = (int64_t)min(r, rows - 1) / p.G + (PAGED ? kv - n : 0) + 1;
             return p.causal ? (int)max((int64_t)0, min(i, (int64_t)kv)) : kv;
         };
-        const int wr0 = r0 + (WR == 1 ? 0 : wave) * 32 * RB;
-        const int part = WR == 1 ? min(wave, KW - 1) : 0;  // this wave's keys in a tile, in parts of 32
-        const bool idle = wave >= KW && WR == 1;
+        const int wr0 = r0 + wave % WR * 32 * RB;
+        const int part = min(wave / WR, KW - 1);  // this wave's keys in a tile, in parts of 32
+        const bool idle = wave >= WR * KW;
         const int see_most = uniform(visible(wr0 + 32 * RB - 1));  // keys that some row of the wave sees
         const int see_all = uniform(visible(r0));  // keys that every row of the tile sees
         const int first = key_tile0 * BN;
@@ -488,14 +490,14 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             arrive();
             char *vt = lds + 2 * TILE * buf + TILE;
             if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 2 * STAGES * TILE)))
-                take_foreign(vt, vis, key0, wave == 0 || WR != 1, st, lane);
+                take_foreign(vt, vis, key0, wave < WR, st, lane);
             if (key0 + 32 * part < see_most && !idle)
                 step<true>(lds + 2 * TILE * buf + part * 32 * S::ROW, vt + part * 32 * S::ROW, qf, vis, key0 + 32 * part, p.c,
                            p.rest != nullptr, st, lane);
         }
         if constexpr (KW > 1) {
             join_waves(lds, wave, lane, st);
-            if (wave > 0) return;
+            if (wave >= WR) return;
         }
 
         const Span os((T *)p.out + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);

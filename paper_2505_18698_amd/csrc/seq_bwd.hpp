@@ -121,8 +121,9 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
 template <typename T, int D> struct SeqBwdQ {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int W = 4, NTH = 64 * W, R = 32 * W;
-    static constexpr int BN = S::kF32 ? 32 : 64, KT = BN / 32;
+    static constexpr int W = 4, NTH = 64 * W;
+    static constexpr int WR = S::kF32 ? 2 : W, KW = W / WR, R = 32 * WR;  // row blocks by parts of a tile's keys
+    static constexpr int BN = 64, KT = BN / 32 / KW;
     static constexpr int TILE = BN * S::ROW;
     static constexpr int LDS_BYTES = 4 * TILE;
     using Copy = TileCopy<T, D, BN, W>;
@@ -194,9 +195,10 @@ template <typename T, int D> struct SeqBwdQ {
         const int rows = n * p.G, r0 = tile * R, tok0 = r0 / p.G;
         auto visible = [&](int r) { return p.causal ? min(r, rows - 1) / p.G + 1 : n; };
         const int see_all = uniform(visible(r0)), last = uniform(visible(r0 + R - 1));
-        const int see_most = uniform(visible(r0 + wave * 32 + 31));
+        const int wr0 = r0 + wave % WR * 32, part = wave / WR * 32 * KT;
+        const int see_most = uniform(visible(wr0 + 31));
 
-        const int r = min(r0 + wave * 32 + (lane & 31), rows - 1);
+        const int r = min(wr0 + (lane & 31), rows - 1);
         const int vis = visible(r), tok = r / p.G - tok0, head = kvh * p.G + r % p.G, Hq = p.Hkv * p.G;
         const Span qs((const T *)p.q + (row0 + tok0) * p.ldq), gs((const T *)p.dout + (int64_t)(row0 + tok0) * Hq * p.d);
         frag qf[S::NS], gf[S::NS];
@@ -231,18 +233,32 @@ template <typename T, int D> struct SeqBwdQ {
         for (; key0 + BN <= min(see_all, last); key0 += BN, buf ^= 1) {
             tile_barrier();
             bring(key0 + BN, buf ^ 1);
-            step<false>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, qf, gf, 0, p.c, lse2, delta, sc.ds, dq, lane);
+            step<false>(lds + 2 * TILE * buf + part * S::ROW, lds + 2 * TILE * buf + TILE + part * S::ROW, qf, gf, 0, p.c, lse2, delta, sc.ds, dq, lane);
         }
 #pragma unroll 1
         for (; key0 < last; key0 += BN, buf ^= 1) {
             tile_barrier();
             bring(key0 + BN, buf ^ 1);
-            if (key0 < see_most)
-                step<true>(lds + 2 * TILE * buf, lds + 2 * TILE * buf + TILE, qf, gf, vis - key0 - 4 * (lane >> 5), p.c, lse2,
-                           delta, sc.ds, dq, lane);
+            if (key0 + part < see_most)
+                step<true>(lds + 2 * TILE * buf + part * S::ROW, lds + 2 * TILE * buf + TILE + part * S::ROW, qf, gf,
+                           vis - key0 - part - 4 * (lane >> 5), p.c, lse2, delta, sc.ds, dq, lane);
+        }
+        if constexpr (KW > 1) {  // the waves' sums over their keys, into the first ones'
+            static_assert((KW - 1) * WR * S::ND * 16 * 256 <= LDS_BYTES, "the tiles' room holds them");
+            float *sh = reinterpret_cast<float *>(lds) + lane;
+            __syncthreads();
+            if (wave >= WR)
+#pragma unroll
+                for (int i = 0; i < S::ND * 16; ++i) sh[((wave - WR) * S::ND * 16 + i) * 64] = dq[i / 16][i % 16];
+            __syncthreads();
+            if (wave >= WR) return;
+#pragma unroll
+            for (int w = 1; w < KW; ++w)
+#pragma unroll
+                for (int i = 0; i < S::ND * 16; ++i) dq[i / 16][i % 16] += sh[(((w - 1) * WR + wave) * S::ND * 16 + i) * 64];
         }
         const Span os((T *)p.dq + (int64_t)(row0 + tok0) * Hq * p.d);
-        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, r0 + wave * 32 + (lane & 31) < rows, lane);
+        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, wr0 + (lane & 31) < rows, lane);
     }
 };
 

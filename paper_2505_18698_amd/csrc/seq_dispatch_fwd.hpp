@@ -10,16 +10,17 @@ template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p,
 {
     const dim3 grid((unsigned)(how.units * p.Hkv)), block(256);
     const bool few = how.rows == kSeqFewRows;
+    constexpr int R = kSeqRows<T>, WR = R / 32;
     int rc = L.run(kSeqFwd, [&] {
         return launched([&] {
             if (!how.paged)
-                ma::seq_attention<T, D, 1, 4, false, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, WR, false, false><<<grid, block, 0, L.stream>>>(p);
             else if (!how.split && !few)
-                ma::seq_attention<T, D, 1, 4, true, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, WR, true, false><<<grid, block, 0, L.stream>>>(p);
             else if (!how.split)
                 ma::seq_attention<T, D, 1, 1, true, false><<<grid, block, 0, L.stream>>>(p);
             else if (!few)
-                ma::seq_attention<T, D, 1, 4, true, true><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, WR, true, true><<<grid, block, 0, L.stream>>>(p);
             else
                 ma::seq_attention<T, D, 1, 1, true, true><<<grid, block, 0, L.stream>>>(p);
         });
@@ -31,7 +32,7 @@ template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p,
             if (few)
                 ma::seq_join<T, D, kSeqFewRows><<<dim3(tiles, 8), block, 0, L.stream>>>(p);
             else
-                ma::seq_join<T, D, kSeqRows><<<dim3(tiles, 16), block, 0, L.stream>>>(p);
+                ma::seq_join<T, D, R><<<dim3(tiles, R / 8), block, 0, L.stream>>>(p);
         });
     });
 }

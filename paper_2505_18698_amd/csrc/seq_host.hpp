@@ -45,8 +45,10 @@ struct SeqPlan {
     int64_t units;  // workgroups of one key head
 };
 
-// packed rows a workgroup takes: usually, and where sequences have few; keys a tile
-constexpr int kSeqRows = 128, kSeqFewRows = 32;
+// packed rows a workgroup takes: usually, and where sequences have few
+template <typename T> constexpr int kSeqRows = sizeof(T) == 4 ? 64 : 128;
+constexpr int kSeqFewRows = 32;
+inline int seq_rows(int32_t dtype) { return dtype == MA_F32 ? kSeqRows<float> : kSeqRows<__bf16>; }
 constexpr int kSeqBwdKeys = 64;  // keys a workgroup takes in the gradient
 inline int seq_tile_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }
 
