@@ -104,15 +104,19 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
     static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
-    // keys a tile: of few rows in 16-bit types, where the workgroup has a context alone, 32 a wave
-    static constexpr int BN = S::kF32 && WR == 1 ? 32 : WR == 1 && !SPLIT ? 128 : 64;
+    // Keys a tile.  Of few rows in 16-bit types, where the workgroup has a context
+    // alone, 32 a wave.  Of few rows in fp32, whose products bound them as much as their bytes:
+    // as many waves as the room lets work, four in one workgroup (D = 64: 167 us for the
+    // contexts of 64 requests, 520 MB; 175 two in each of two, 197 one) or, past D = 64, one in
+    // each of two (375 us, 1.04 GB; 432 two in one, 744 one in one).
+    static constexpr int BN = WR != 1 ? 64 : S::kF32 ? (D <= 64 ? 128 : 32) : SPLIT ? 64 : 128;
     static constexpr int KT = WR == W ? BN / 32 : 1;       // 32-key parts that a wave takes
     static constexpr int KW = BN / 32 / KT;                // waves that share a tile's keys
     static_assert(WR * KW <= W, "rows and keys over the waves");
     static constexpr int TILE = BN * S::ROW;
     // Tiles that are there or on their way.  Short contexts of few rows are bound
     // by the latency of one tile after another: up to four, as the room allows.
-    static constexpr int STAGES = WR != 1 ? 2 : SPLIT ? (D * sizeof(T) <= 128 ? 4 : 2) : S::kF32 ? 4 : D <= 64 ? 3 : 2;
+    static constexpr int STAGES = WR != 1 || S::kF32 ? 2 : SPLIT ? (D <= 64 ? 4 : 2) : D <= 64 ? 3 : 2;
     static constexpr int LDS_BYTES = 2 * STAGES * TILE + 16;  // K and V
     using Copy = TileCopy<T, D, BN, W>;
     // A row's weights are taken relative to a reference that follows its running
@@ -538,7 +542,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 };
 
 template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64) ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
+__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64 && WR > 1) ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
 {
     using U = SeqAttn<T, D, RB, WR, PAGED, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
