@@ -540,11 +540,15 @@ def _packed_function():
     if _PACKED_FN is None:
         import torch
 
+        def whole(t):  # contiguous and 16-byte aligned
+            t = t.contiguous()
+            return t if t.data_ptr() % 16 == 0 else t.clone()
+
         def rows(t):  # the kernels' layout: heads of a row adjacent, rows 16-byte aligned
             n = t.element_size()
             fits = t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.stride(0) * n % 16 == 0 \
                 and t.stride(0) >= t.shape[1] * t.shape[2] and t.data_ptr() % 16 == 0
-            return t if fits else t.contiguous()
+            return t if fits else whole(t)
 
         class ExactAttentionPackedFn(torch.autograd.Function):
             @staticmethod
@@ -560,10 +564,11 @@ def _packed_function():
                 return out
 
             @staticmethod
+            @torch.autograd.function.once_differentiable
             def backward(ctx, dout):
                 q, k, v, out, lse, cu_seqlens, *rest = ctx.saved_tensors
                 dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-                monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout.contiguous(), dq, dk, dv, cu_seqlens, ctx.causal,
+                monarch_attn_exact_packed_bwd(q, k, v, out, lse, whole(dout), dq, dk, dv, cu_seqlens, ctx.causal,
                                               *(rest or (None,)), True)
                 return dq, dk, dv, None, None
 
@@ -573,8 +578,14 @@ def _packed_function():
 
 def exact_attention_packed(q, k, v, cu_seqlens, causal: bool = True):
     """Exact attention over packed sequences as a differentiable torch op (see
-    monarch_attn_exact_packed_fwd).  Rows of no sequence get zero output and
-    zero gradients."""
+    monarch_attn_exact_packed_fwd; tensors in other layouts are copied).  Rows
+    of no sequence get zero output and zero gradients.  Differentiable once.
+
+    A backward pass can be captured into a HIP graph together with its forward
+    pass, after one of the same size on the capture stream.  As with every torch
+    op, no autograd graph of the same leaves from outside the capture may be alive then
+    (drop its outputs, or capture with leaves of its own): torch would wait
+    for the stream of that graph, which ends the capture and may end the process."""
     return _packed_function().apply(q, k, v, cu_seqlens, causal)
 
 

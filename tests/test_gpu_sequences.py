@@ -326,3 +326,75 @@ def test_two_streams_at_once(ma):
     torch.cuda.synchronize()
     for w, r in zip(want, got):
         assert all(torch.equal(w[n], r[n]) for n in w)
+
+
+def test_autograd_of_other_layouts(ma):
+    """Leaves and upstream gradients that are not as the kernels need them: off 16 bytes, expanded, heads not adjacent."""
+    lens, Hq, Hkv, d = [70, 3], 4, 2, 64
+    q, k, v, dout, cu = _inputs(lens, Hq, Hkv, d, "bf16", 41, spare=0, first=0)
+    want = _run(ma, q, k, v, dout, cu, True)
+
+    def odd(t):  # contiguous, 2 bytes behind an aligned address
+        flat = torch.empty(t.numel() + 1, device="cuda", dtype=t.dtype)[1:].view(t.shape)
+        return flat.copy_(t)
+
+    leaves = [odd(q).requires_grad_(), k.transpose(0, 1).contiguous().transpose(0, 1).requires_grad_(), odd(v).requires_grad_()]
+    out = ma.exact_attention_packed(*leaves, cu)
+    assert torch.equal(out, want["out"])
+    for g, n in zip(torch.autograd.grad(out, leaves, odd(dout), retain_graph=True), ("dq", "dk", "dv")):
+        assert torch.equal(g, want[n]), n
+    ones = torch.autograd.grad(out.sum(), leaves, retain_graph=True)  # an upstream gradient with strides of zero
+    for g, h in zip(ones, torch.autograd.grad(out, leaves, torch.ones_like(out))):
+        assert torch.equal(g, h)
+
+
+def test_gradient_of_the_gradient_is_refused(ma):
+    q, k, v, _, cu = _inputs([20], 2, 2, 64, "f32", 42, spare=0, first=0)
+    q = q.detach().requires_grad_()
+    (g,) = torch.autograd.grad(ma.exact_attention_packed(q, k, v, cu).square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.sum(), q)
+
+
+def test_captured_autograd(ma):
+    """Forward and backward of the torch op in one graph, replayed with other inputs, against eager passes."""
+    x = _inputs([130, 66], 4, 2, 64, "bf16", 43, spare=0, first=0)
+    leaves, dout, cu = [t.detach().clone().requires_grad_() for t in x[:3]], x[3], x[4]
+    s = torch.cuda.Stream()
+
+    def once():
+        out = ma.exact_attention_packed(*leaves, cu)
+        return (out.detach(), *torch.autograd.grad(out, leaves, dout))
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        once()  # (its autograd graph is gone before the capture)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = once()
+    for i in range(4):
+        y = _inputs([130, 66], 4, 2, 64, "bf16", 44 + i, spare=0, first=0)
+        with torch.no_grad():
+            for dst, src in zip(leaves, y[:3]):
+                dst.copy_(src)
+        dout.copy_(y[3])
+        want = _run(ma, *y, True)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, n in zip(got, ("out", "dq", "dk", "dv")):
+            assert torch.equal(t, want[n]), (i, n)
+
+
+def test_decreasing_row_starts(ma):
+    """Sequences whose ranges overlap: nothing outside the tensors is read or written, in the gradient too."""
+    q, k, v, dout, _ = _inputs([300], 4, 2, 64, "bf16", 45, spare=0, first=0)
+    cu = torch.tensor([0, 300, 0, 300, 0, 300, 100, 250], device="cuda", dtype=torch.int32)
+    around = {n: torch.full((900, h, 64), 7.0, device="cuda", dtype=torch.bfloat16) for n, h in (("out", 4), ("dq", 4), ("dk", 2), ("dv", 2))}
+    mid = {n: t[300:600] for n, t in around.items()}
+    lse = torch.zeros(4, 300, device="cuda")
+    ma.monarch_attn_exact_packed_fwd(q, k, v, mid["out"], cu, True, lse)
+    ma.monarch_attn_exact_packed_bwd(q, k, v, mid["out"], lse, dout, mid["dq"], mid["dk"], mid["dv"], cu)
+    torch.cuda.synchronize()
+    for t in around.values():
+        assert bool((t[:300] == 7).all()) and bool((t[600:] == 7).all())
