@@ -402,9 +402,9 @@ int32_t monarch_attn_timing_read(float *ms, int32_t *kind, int32_t cap);
  * Keys that a row does not see have no effect on its output, whatever they
  * hold (infinities and NaN among them).
  *
- * d: a multiple of 8 (bf16, fp16) or 4 (fp32) up to 128.  Hq * d and the row
- * strides are at most 2^20 elements, total * G and B below 2^31, else
- * MA_EUNSUPPORTED.
+ * d: a multiple of 8 (bf16, fp16) or 4 (fp32) up to 128.  Hq times d rounded
+ * up to 64, 96 or 128, and the row strides, are at most 2^20 elements, total * G
+ * and B below 2^31, else MA_EUNSUPPORTED.
  * Tensors are DEVICE pointers, 16-byte aligned; integers 4- (slots: 8-) byte
  * aligned.  No output overlaps another one or an input (inputs may overlap:
  * q, k and v can be parts of one tensor).  Statistics, sums and gradients are
@@ -447,7 +447,9 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
  * In fp16, dS is formed relative to the largest norms of the rows of dout and
  * v, so gradients of any scale keep their precision.  Values of a sequence
  * that are not finite can reach all gradients of that sequence.
- * Workspace: 8 bytes a row and query head.
+ * Workspace: 8 bytes a row and query head; and where there are few key tiles
+ * for the device (fewer than about 2000 over all key heads) up to four fp32 copies of dk and dv,
+ * which a further launch adds up.
  */
 int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,
                                   const void *rest, const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_seqlens,
@@ -462,7 +464,7 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  * q, out, lse : as in monarch_attn_exact_packed_fwd; sequence i's new tokens
  *               are its rows by cu_seqlens, and are the last of its tokens.
  * kv_lens     : [B] device int32, the tokens of sequence i in the cache, the
- *               new ones among them (clamped to 0..blocks * page).  With
+ *               new ones among them (clamped to 0..blocks * page and 2^31 - 256).  With
  *               causal, new token r of n sees the first kv_lens[i] - n + r + 1
  *               (none where that is not positive); otherwise all kv_lens[i].
  * k_pages,    : [pages, Hkv, page, d], contiguous; page is a power of two from
@@ -471,8 +473,9 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  * block_table : [B, blocks] device int32, contiguous.  Entries past the last
  *               token are not read.  A page number outside 0..pages - 1 leads
  *               to no read: the rows that see a token on it become NaN.
- * Calls with few rows and long contexts are split over the keys and joined by
- * a second launch, from partial results in the workspace.
+ * Calls with long contexts (a table of more than 1024 tokens a sequence, 512 in fp32) are split
+ * over the keys into equal shares, and joined by a second launch, from partial
+ * results in the workspace.
  */
 int monarch_attn_exact_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out, float *lse,
                                  const int32_t *cu_seqlens, const int32_t *kv_lens, const int32_t *block_table,

@@ -66,7 +66,8 @@ int check_heads(int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, in
     const int64_t chunk = 16 / (int64_t)elem_bytes(dtype);
     if (d > 128 || d % chunk)
         return fail(MA_EUNSUPPORTED, "d must be a multiple of %lld up to 128 (got %lld)", (long long)chunk, (long long)d);
-    if (Hq > kMaxWidth / d) return fail(MA_EUNSUPPORTED, "a row of Hq * d elements must not exceed %lld", (long long)kMaxWidth);
+    if (Hq > kMaxWidth / tile_d(d))
+        return fail(MA_EUNSUPPORTED, "Hq times d, rounded up to %d, must not exceed %lld", (int)tile_d(d), (long long)kMaxWidth);
     if (B > 0x7ffffffe || total > 0x7fffff00 || total * (Hq / Hkv) > 0x7fffff00)
         return fail(MA_EUNSUPPORTED, "total * (Hq / Hkv) and B must be below 2^31");
     return MA_OK;

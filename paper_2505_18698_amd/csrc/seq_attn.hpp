@@ -50,7 +50,8 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
     sum = tiles = 0;
     for (int i = 0; i < W; ++i) sum += sh[2 * i], tiles += sh[2 * i + 1];
     __syncthreads();
-    if (blockIdx.x == 0 && tid == 0) p.parts[0].seq = (int)tiles;
+    // (row starts that decrease can make more row tiles than there is room for: those are left out)
+    if (blockIdx.x == 0 && tid == 0) p.parts[0].seq = (int)min(tiles, (int64_t)p.tiles);
     Line r{sum, (int)max((int64_t)1, min((int64_t)p.shares, sum / 4)), -1, 0, 0, 0};
     if (share >= r.shares) return r;
     const int64_t want = sum * share / r.shares;
@@ -78,7 +79,7 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
             sh[0] = s0 + tid, sh[1] = tile, sh[2] = tiles_before + t - rt + tile, sh[3] = u0 + (int64_t)tile * kt;
         }
         if (some_thread<NTH>(mine, reinterpret_cast<int *>(lds + 64))) {
-            r.seq = (int)sh[0], r.tile = (int)sh[1], r.index = (int)sh[2], r.at = sh[3];
+            r.seq = sh[2] < p.tiles ? (int)sh[0] : -1, r.tile = (int)sh[1], r.index = (int)sh[2], r.at = sh[3];
             break;
         }
         steps_before += au, tiles_before += at;
@@ -358,7 +359,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         const int kvh = uniform((int)(blockIdx.x % p.Hkv));
-        const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffc0) : 0;
+        const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffff00) : 0;  // (a tile behind the last one still has a number)
         if constexpr (SPLIT) {
             const int share = uniform((int)(blockIdx.x / p.Hkv));
             Line f = find_share<R, BN, NTH>(p, share, max_keys, lds);
@@ -367,7 +368,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             const int shares = uniform(f.shares);
             const int64_t all = uniform(f.all), end = all * (share + 1) / shares;
             int64_t at = uniform(f.at), x = all * share / shares;
-            while (x < end) {
+            while (x < end && index < p.tiles) {
                 const int n = uniform(p.seqs.length(seq)), kv = uniform(max(0, min(p.kv_lens[seq], max_keys)));
                 const int tiles = (int)(((int64_t)n * p.G + R - 1) / R), steps = max(1, (kv + BN - 1) / BN);
                 if (tile >= tiles) {  // the next sequence

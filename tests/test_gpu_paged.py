@@ -396,3 +396,34 @@ def test_capture_without_workspace_is_refused(ma):
             ma.monarch_attn_exact_paged_fwd(q, kp, vp, out, cu, kv, table)
         out.add_(1)
     assert e.value.status == ma.MA_EUNSUPPORTED and "before capturing" in str(e.value)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_requests_of_odd_lengths(ma, dtype):
+    """Shares of the work that begin and end anywhere in 300 requests, some idle, some without a past."""
+    gen = torch.Generator(device="cuda").manual_seed(71)
+    new = [(0, 1, 1, 7, 40)[i % 5] for i in range(300)]
+    past = [(i * 7919) % 3000 if i % 11 else 0 for i in range(300)]
+    seqs, kp, vp, table, kv = _cache(new, past, 2, 64, 16, dtype, gen)
+    q = torch.randn(sum(new) + 2, 6, 64, generator=gen, device="cuda").to(DTYPES[dtype])
+    cu = starts(new, "cuda")
+    out, lse = _attend(ma, q, kp, vp, cu, kv, table)
+    _check(out, lse, q, cu, seqs, past)
+    again = _attend(ma, q, kp, vp, cu, kv, table)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+def test_decreasing_row_starts(ma):
+    """Row starts that make more row tiles than the tensor's rows: what has no room is left out, and later calls are right."""
+    gen = torch.Generator(device="cuda").manual_seed(72)
+    seqs, kp, vp, table, kv = _cache([200], [2000], 2, 64, 16, "bf16", gen)
+    q = torch.randn(200, 4, 64, generator=gen, device="cuda").bfloat16()
+    cu = starts([200], "cuda")
+    want = _attend(ma, q, kp, vp, cu, kv, table)
+    bad = torch.tensor([0, 200] * 40 + [0], device="cuda", dtype=torch.int32)
+    around = torch.full((600, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    ma.monarch_attn_exact_paged_fwd(q, kp, vp, around[200:400], bad, kv.repeat(80), table.repeat(80, 1))
+    torch.cuda.synchronize()
+    assert bool((around[:200] == 7).all()) and bool((around[400:] == 7).all())
+    got = _attend(ma, q, kp, vp, cu, kv, table)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -211,3 +211,9 @@ def test_rows_may_be_strided(no_library):
         call(**{**tensors, "k": _t(2, 10, 8).transpose(0, 1)})
     with pytest.raises(ValueError, match="out must be"):
         call(**{**tensors, "out": q})
+
+
+def test_heads_wider_than_their_tiles_are_refused():
+    """Offsets within a tile count heads of the tile's width: 32768 heads of 32 columns take 2^21."""
+    assert _paged(Hq=1 << 15, Hkv=1, d=32, ldq=1 << 20) == UNSUPPORTED
+    assert "rounded up" in ma.monarch_attn_last_error()
