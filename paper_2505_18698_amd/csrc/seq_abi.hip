@@ -172,7 +172,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
 
 // Workspace of the gradient: lse in log2 units and delta of every row and head,
 // and the largest norms of the workgroups that form them.
-constexpr int kNormBlocks = 512;
+constexpr int kNormBlocks = 1024;
 size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * total) * 4) + align_up(kNormBlocks * sizeof(float2)); }
 
 // Pieces that the query rows of a key tile are cut into.  The longest walk, of the
@@ -229,7 +229,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     p.tiles_q = (int)tiles_q, p.tiles_k = (int)tiles_k;
     const size_t each = align_up((size_t)(Hq * total) * 4);
     p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each), p.norms = (float2 *)(c.ws + 2 * each);
-    p.norm_blocks = (int)std::min<int64_t>(kNormBlocks, (total * Hq + 15) / 16);
+    p.norm_blocks = (int)std::min<int64_t>(kNormBlocks, (total + 15) / 16 * Hq);
     p.pieces = (int)pieces;
     p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;

@@ -49,7 +49,9 @@ template <typename T> struct BwdScale {
     __device__ static float uniform_float(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 };
 
-// delta and lse in log2 units of every (row, head), 16 lanes a row; in fp16 also the largest norms.
+// delta and lse in log2 units of every (row, head), 16 lanes a row; in fp16 also
+// the largest norms.  A workgroup takes one head of 16 rows at a time, whose lse, delta
+// and lse2 are then 64 bytes together.
 template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
 {
     constexpr int V = 16 / (int)sizeof(T);
@@ -60,9 +62,12 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
         clear_outside<256>(p.seqs, p.dv, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
     }
     const int first = p.seqs.start(0), last = p.seqs.start(p.seqs.B);  // (rows of no sequence count for nothing)
-    const int64_t step = (int64_t)gridDim.x * 16, own = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     float most_g = 0.f, most_v = 0.f;
-    for (int64_t i = (int64_t)first * Hq + own; i < (int64_t)last * Hq; i += step) {
+#pragma unroll 2
+    for (int64_t u = blockIdx.x; u < ((int64_t)last - first + 15) / 16 * Hq; u += gridDim.x) {
+        const int head = (int)(u % Hq), row = first + (int)(u / Hq) * 16 + (int)(threadIdx.x >> 4);
+        if (row >= last) continue;
+        const int64_t i = (int64_t)row * Hq + head;
         float sum = 0.f, norm = 0.f;
         for (int col = lane * V; col < p.d; col += 16 * V) {
             T a[V], b[V];
@@ -86,13 +91,14 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
             if constexpr (BwdScale<T>::kScaled) norm += __shfl_xor(norm, x);
         }
         if (lane == 0) {
-            const int64_t at = i % Hq * p.seqs.total + i / Hq;
+            const int64_t at = (int64_t)head * p.seqs.total + row;
             p.delta[at] = sum;
             p.lse2[at] = p.lse[at] * kLog2e;
         }
         if (norm < INFINITY) most_g = fmaxf(most_g, norm);
     }
     if constexpr (BwdScale<T>::kScaled) {
+        const int64_t step = (int64_t)gridDim.x * 16, own = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
         for (int64_t i = (int64_t)first * p.Hkv + own; i < (int64_t)last * p.Hkv; i += step) {
             float norm = 0.f;
             const T *v = (const T *)p.v + i / p.Hkv * p.ldv + i % p.Hkv * p.d;
