@@ -16,8 +16,8 @@ MA_OK, MA_EINVAL, MA_EUNSUPPORTED, MA_EHIP, MA_ENOMEM = 0, 1, 2, 3, 4
 STATUS_NAMES = {0: "MA_OK", 1: "MA_EINVAL", 2: "MA_EUNSUPPORTED", 3: "MA_EHIP", 4: "MA_ENOMEM"}
 KIND_NAMES = {0: "r_half_step", 1: "l_half_step", 2: "r_half_step_final", 3: "monarch_apply",
               4: "monarch_fused_head", 5: "objective_sum", 6: "exact_attention", 7: "l_bwd", 8: "r_bwd",
-              9: "monarch_fused_group", 10: "seq_attention", 11: "seq_join", 12: "seq_stats", 13: "seq_bwd_k",
-              14: "seq_bwd_q", 15: "paged_plan", 16: "paged_write"}
+              9: "monarch_fused_group", 10: "seq_attention", 11: "seq_join", 12: "seq_stats", 13: "seq_bwd",
+              14: "seq_bwd_join", 15: "paged_plan", 16: "paged_write"}
 PATH_AUTO, PATH_HALF_STEPS, PATH_FUSED, PATH_GROUPED = 0, 1, 2, 3
 
 # Every symbol declared in include/monarch_attn.h.

@@ -183,7 +183,7 @@ size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * 
 int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
 {
     const int64_t want = (8 * num_cus + tiles_k * Hkv - 1) / (tiles_k * Hkv);
-    return std::max<int64_t>(1, std::min<int64_t>({want, 4, G * tiles_k / 8}));
+    return std::max<int64_t>(1, std::min<int64_t>({want, 3, G * tiles_k / 8}));
 }
 
 int packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
@@ -216,7 +216,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(begin_call(c));
     const int64_t pieces = bwd_pieces(tiles_k, Hkv, G, c.num_cus);
     const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq);
-    MA_TRY(check_grid(tiles_k * pieces, Hkv));
+    MA_TRY(check_grid(tiles_k * pieces + tiles_q, Hkv));
     MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
     BwdLaunch x{};
     ma::SeqBwd &p = x.p;

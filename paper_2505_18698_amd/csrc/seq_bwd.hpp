@@ -187,13 +187,13 @@ template <typename T, int D> struct SeqBwdQ {
         }
     }
 
-    __device__ static void run(const SeqBwd &p, char *lds)
+    __device__ static void run(const SeqBwd &p, char *lds, int block)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         BwdScale<T> sc;
         sc.template find<NTH>(p, lds);
-        const int kvh = uniform((int)(blockIdx.x % p.Hkv));
-        const int64_t t = p.tiles_q - 1 - (int)(blockIdx.x / p.Hkv);  // later rows see more keys: they start first
+        const int kvh = uniform(block % p.Hkv);
+        const int64_t t = p.tiles_q - 1 - block / p.Hkv;  // later rows see more keys: they start first
         const int seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
         if (seq < 0) return;
         const int tile = uniform((int)(t - tile0(p.seqs, seq, p.G, R)));
@@ -395,14 +395,14 @@ template <typename T, int D> struct SeqBwdK {
         }
     }
 
-    __device__ static void run(const SeqBwd &p, char *lds)
+    __device__ static void run(const SeqBwd &p, char *lds, int block)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kb = wave % NK, qb = wave / NK;
         BwdScale<T> sc;
         sc.template find<NTH>(p, lds);
-        const int kvh = uniform((int)(blockIdx.x % p.Hkv));
-        const int64_t t = (int)(blockIdx.x / p.Hkv / p.pieces);  // (earlier keys are seen by more rows: they start first)
-        const int piece = uniform((int)(blockIdx.x / p.Hkv % p.pieces));
+        const int kvh = uniform(block % p.Hkv);
+        const int64_t t = block / p.Hkv / p.pieces;  // (earlier keys are seen by more rows: they start first)
+        const int piece = uniform(block / p.Hkv % p.pieces);
         const int seq = uniform(seq_of_tile(p.seqs, t, 1, R, lane));
         if (seq < 0) return;
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
@@ -493,18 +493,19 @@ template <typename T, int D> struct SeqBwdK {
     }
 };
 
-template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd_q(SeqBwd p)
+// Both in one launch, dQ first: its longest walks, over all keys of a long
+// sequence, start at once, and the shorter ones of dK and dV fill what they leave free.
+template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd(SeqBwd p, int blocks_q)
 {
-    using U = SeqBwdQ<T, D>;
-    __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
-    U::run(p, lds);
-}
-
-template <typename T, int D> __global__ __launch_bounds__((SeqBwdK<T, D>::NTH), (sizeof(T) == 4 && D > 64 ? 1 : 2)) void seq_bwd_k(SeqBwd p)
-{
-    using U = SeqBwdK<T, D>;
-    __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
-    U::run(p, lds);
+    using K = SeqBwdK<T, D>;
+    using Q = SeqBwdQ<T, D>;
+    static_assert(K::NTH == 256 && Q::NTH == 256, "one launch");
+    __shared__ __attribute__((aligned(16))) char lds[K::LDS_BYTES > Q::LDS_BYTES ? K::LDS_BYTES : Q::LDS_BYTES];
+    const int block = blockIdx.x;
+    if (block < blocks_q)
+        Q::run(p, lds, block);
+    else
+        K::run(p, lds, block - blocks_q);
 }
 
 // The pieces' sums of dK and dV added up, four columns a thread.

@@ -15,19 +15,14 @@ template <typename T, int D> int run_seq_bwd_d(Launcher &L, const ma::SeqBwd &p)
         return launched([&] { ma::seq_stats<T><<<dim3((unsigned)p.norm_blocks), block, 0, L.stream>>>(p); });
     });
     if (rc != MA_OK) return rc;
-    rc = L.run(kSeqBwdK, [&] {
-        return launched([&] { ma::seq_bwd_k<T, D><<<dim3((unsigned)((int64_t)p.tiles_k * p.pieces * p.Hkv)), dim3(ma::SeqBwdK<T, D>::NTH), 0, L.stream>>>(p); });
+    const int blocks_q = (int)((int64_t)p.tiles_q * p.Hkv), blocks_k = (int)((int64_t)p.tiles_k * p.pieces * p.Hkv);
+    rc = L.run(kSeqBwd, [&] {
+        return launched([&] { ma::seq_bwd<T, D><<<dim3((unsigned)blocks_q + (unsigned)blocks_k), block, 0, L.stream>>>(p, blocks_q); });
     });
-    if (rc != MA_OK) return rc;
-    if (p.pieces > 1) {
-        // two rows' worth of threads at a time, at most 8 workgroups a compute unit
-        const int64_t blocks = std::min<int64_t>(2048, ((int64_t)p.seqs.total * p.Hkv * (D / 4) + 255) / 256);
-        rc = L.run(kSeqJoin, [&] { return launched([&] { ma::seq_bwd_join<T, D><<<dim3((unsigned)blocks), block, 0, L.stream>>>(p); }); });
-        if (rc != MA_OK) return rc;
-    }
-    return L.run(kSeqBwdQ, [&] {
-        return launched([&] { ma::seq_bwd_q<T, D><<<dim3((unsigned)((int64_t)p.tiles_q * p.Hkv)), block, 0, L.stream>>>(p); });
-    });
+    if (rc != MA_OK || p.pieces == 1) return rc;
+    // at most 8 workgroups a compute unit
+    const int64_t blocks = std::min<int64_t>(2048, ((int64_t)p.seqs.total * p.Hkv * (D / 4) + 255) / 256);
+    return L.run(kSeqBwdJoin, [&] { return launched([&] { ma::seq_bwd_join<T, D><<<dim3((unsigned)blocks), block, 0, L.stream>>>(p); }); });
 }
 
 template <typename T> int run_seq_bwd_impl(Launcher &L, const ma::SeqBwd &p)

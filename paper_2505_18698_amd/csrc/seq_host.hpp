@@ -19,7 +19,7 @@ namespace ma_host {
 extern thread_local char g_err[512];  // what monarch_attn_last_error() returns
 
 // Kernel kinds of the timing interface, after those of Kind.
-enum SeqKind { kSeqFwd = 10, kSeqJoin = 11, kSeqStats = 12, kSeqBwdK = 13, kSeqBwdQ = 14, kPagedPlan = 15, kPagedWrite = 16 };
+enum SeqKind { kSeqFwd = 10, kSeqJoin = 11, kSeqStats = 12, kSeqBwd = 13, kSeqBwdJoin = 14, kPagedPlan = 15, kPagedWrite = 16 };
 
 // The device, capture state and workspace of one call; `hold` keeps the
 // workspace until the call's launches are enqueued.
