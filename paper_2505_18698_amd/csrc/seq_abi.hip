@@ -179,7 +179,8 @@ size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * 
 // first keys of one causal sequence that fills the call, is twice the mean one,
 // so 1024 key tiles and heads (two rounds of two workgroups on 256 compute units) end with it; the
 // pieces make it half of the mean work of a compute unit's slot.  A piece of fewer than 8
-// tiles is not worth its sums' way through memory.
+// tiles is not worth its sums' way through memory, nor are more than three pieces (9550 rows, 16 heads on 4 of 128, with the
+// forward: 608 us; 614 with two or four).
 int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
 {
     const int64_t want = (8 * num_cus + tiles_k * Hkv - 1) / (tiles_k * Hkv);
@@ -256,6 +257,9 @@ int log2_of(int64_t page)
 // The work is shared evenly by as many workgroups as the device holds at a time
 // (two a compute unit; find_share in seq_attn.hpp), except where the longest possible context
 // is a few key tiles, or where there are many times as many row tiles: then a row tile is a workgroup's.
+// (64 single tokens over up to 8192: 103 us, in pieces of equal length 122, 128-row tiles 266;
+// 8 chunks of up to 512 over up to 16384: 210 us, in pieces of equal length 241.
+// One token over 501: 9.5 us in one workgroup a head.)
 struct PagedSplit {
     int rows;
     bool split;
