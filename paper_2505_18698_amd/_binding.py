@@ -507,10 +507,14 @@ def monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal: bool = True,
         _check_each(q, ("lse", lse, (q.shape[1], q.shape[0]), _torch().float32))
     if rest is not None:
         _check_each(q, ("rest", rest, q.shape, q.dtype))
-    _call(LIB.monarch_attn_exact_packed_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-          None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(), cu_seqlens.data_ptr(), *sizes, *strides, bool(causal), bool(clear),
-          dtype_code(q.dtype), _stream(q, stream) or None)
+    _packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest, clear, stream, sizes + strides)
     return out, lse
+
+
+def _packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest, clear, stream, dims):
+    _call(LIB.monarch_attn_exact_packed_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+          None if lse is None else lse.data_ptr(), None if rest is None else rest.data_ptr(), cu_seqlens.data_ptr(),
+          *dims, bool(causal), bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
 
 
 def monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal: bool = True, rest=None,
@@ -525,10 +529,15 @@ def monarch_attn_exact_packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlen
                 ("dv", dv, keys, dtype), ("lse", lse, (rows[1], rows[0]), _torch().float32))
     if rest is not None:
         _check_each(q, ("rest", rest, rows, dtype))
-    _call(LIB.monarch_attn_exact_packed_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
-          lse.data_ptr(), None if rest is None else rest.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_seqlens.data_ptr(), *sizes,
-          *strides, bool(causal), bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
+    _packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal, rest, clear, stream, sizes + strides)
     return dq, dk, dv
+
+
+def _packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal, rest, clear, stream, dims):
+    _call(LIB.monarch_attn_exact_packed_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+          lse.data_ptr(), None if rest is None else rest.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(),
+          dv.data_ptr(), cu_seqlens.data_ptr(), *dims, bool(causal), bool(clear), dtype_code(q.dtype),
+          _stream(q, stream) or None)
 
 
 _PACKED_FN = None
@@ -554,22 +563,24 @@ def _packed_function():
             @staticmethod
             def forward(ctx, q, k, v, cu_seqlens, causal):
                 q, k, v = rows(q), rows(k), rows(v)
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-                lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=q.device)
+                sizes, strides = _check_packed(q, k, v, cu_seqlens)
+                out = q.new_empty(q.shape)
+                lse = q.new_empty((sizes[2], sizes[1]), dtype=torch.float32)
                 # (the gradient reads no row of no sequence: rest stays as it is there)
-                rest = torch.empty_like(out) if out.element_size() == 2 else None
-                monarch_attn_exact_packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest, True)
-                ctx.save_for_backward(q, k, v, out, lse, cu_seqlens, *(() if rest is None else (rest,)))
-                ctx.causal = causal
+                rest = q.new_empty(q.shape) if q.element_size() == 2 else None
+                _packed_fwd(q, k, v, out, cu_seqlens, causal, lse, rest, True, None, sizes + strides)
+                ctx.save_for_backward(q, k, v, out, lse, cu_seqlens, rest)
+                ctx.call = causal, sizes + strides
                 return out
 
             @staticmethod
             @torch.autograd.function.once_differentiable
             def backward(ctx, dout):
-                q, k, v, out, lse, cu_seqlens, *rest = ctx.saved_tensors
-                dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-                monarch_attn_exact_packed_bwd(q, k, v, out, lse, whole(dout), dq, dk, dv, cu_seqlens, ctx.causal,
-                                              *(rest or (None,)), True)
+                # (what the forward pass checked or made itself is not checked again: small calls are bound by the host)
+                q, k, v, out, lse, cu_seqlens, rest = ctx.saved_tensors
+                dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
+                causal, dims = ctx.call
+                _packed_bwd(q, k, v, out, lse, whole(dout), dq, dk, dv, cu_seqlens, causal, rest, True, None, dims)
                 return dq, dk, dv, None, None
 
         _PACKED_FN = ExactAttentionPackedFn
