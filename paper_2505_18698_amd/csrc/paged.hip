@@ -8,8 +8,8 @@ namespace ma_host {
 
 int run_paged_plan(Launcher &L, const ma::PagedPlan &p)
 {
-    // one workgroup per 1024 slots; more than 128 repeat the sums for less than they save
-    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(128, (p.capacity + 1023) / 1024));
+    // one slot a thread, up to a workgroup a compute unit
+    const unsigned blocks = (unsigned)std::max<int64_t>(1, std::min<int64_t>(256, (p.capacity + 255) / 256));
     return L.run(kPagedPlan, [&] { return launched([&] { ma::paged_plan<<<dim3(blocks), dim3(256), 0, L.stream>>>(p); }); });
 }
 

@@ -14,7 +14,8 @@ constexpr int kPlanMaxB = MONARCH_ATTN_PLAN_MAX_B;
 // request, microseconds for thousands of them) and then takes its share of the
 // new table entries and of the slots, one a thread, each finding its request by bisection.
 // So the call is one launch without a wait between workgroups: the sums take
-// less than a second launch would.  64 requests: 4.3 us; 512 with 24045 new tokens: 10 us.  What bounds it is latency:
+// less than a second launch would.  64 requests: 4.3 us; 512 with 24045 new tokens: 6.7 us (10 with four
+// slots a thread).  What bounds it is latency:
 // the lengths, the sums, the free pages and the table are each read behind the one before.
 static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
 {
@@ -24,6 +25,7 @@ static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int page = 1 << p.page_log2;
     const int64_t room = min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffffff);  // tokens a request's row of the table holds
+    const int free_first = p.free_in[0], free_count = p.free_in[1];  // (on their way while the sums are formed)
     if (tid == 0) bad = 0;
     __syncthreads();
     // of request s: the tokens before and after the step and the pages they take
@@ -63,8 +65,8 @@ static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
     }
     __syncthreads();
     const int ring_len = max(1, p.ring_len);
-    const int count = max(0, min(p.free_in[1], p.ring_len));
-    int first = p.free_in[0] % ring_len;
+    const int count = max(0, min(free_count, p.ring_len));
+    int first = free_first % ring_len;
     if (first < 0) first += ring_len;
     auto taken_page = [&](int64_t e) { return e < count ? p.ring[(int)((first + e) % ring_len)] : -1; };
     auto request_of = [&](const int *end, int64_t x) {  // the first request whose sum exceeds x
