@@ -117,9 +117,9 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
     // Keys a tile.  Of few rows in 16-bit types, where the workgroup has a context
     // alone, 32 a wave.  Of few rows in fp32, whose products bound them as much as their bytes:
-    // as many waves as the room lets work, four in one workgroup (D = 64: 167 us for the
+    // as many waves as the room lets work, four in one workgroup (D = 64: 161 us for the
     // contexts of 64 requests, 520 MB; 175 two in each of two, 197 one) or, past D = 64, one in
-    // each of two (375 us, 1.04 GB; 432 two in one, 744 one in one).
+    // each of two (364 us, 1.04 GB; 432 two in one, 744 one in one).
     static constexpr int BN = WR != 1 ? 64 : S::kF32 ? (D <= 64 ? 128 : 32) : SPLIT ? 64 : 128;
     static constexpr int KT = WR == W ? BN / 32 : 1;       // 32-key parts that a wave takes
     static constexpr int KW = BN / 32 / KT;                // waves that share a tile's keys
@@ -153,7 +153,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 #pragma unroll
             for (int t = 0; t < KT; ++t) s[rb][t] = f32x16{};
         // (one read of K or V feeds all RB row blocks)
-        constexpr int NK = KT * S::NS, NV = S::kF32 ? KT * 16 * S::ND : KT * 2 * S::ND, AHEAD = 4;
+        constexpr int NK = KT * S::NS, NV = S::kF32 ? KT * 16 * S::ND : KT * 2 * S::ND, AHEAD = S::kF32 ? 2 : 4;
         FragStream<frag, S::kF32 ? NK : NK + NV, AHEAD> stream;
         auto load = [&](int u) {
             if constexpr (!S::kF32)
@@ -344,18 +344,24 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         __device__ void copy(const SeqFwd &p, int key0, char *kt, char *vt, int wave, int lane)
         {
             if constexpr (PAGED) {
-                // a page holds the rows of a copy or several copies'
+                // A page holds the rows of a copy or several copies'.  Lane i finds
+                // where copy i reads (in scalar registers, one copy after another, the
+                // same took 140 instructions a tile, of 400 in all).
                 look(p, key0, lane);
                 const int ld = p.d * (int)sizeof(T);
-                const int64_t each = (int64_t)(p.Hkv << p.page_log2) * p.d;
+                const int64_t each = (int64_t)(p.Hkv << p.page_log2) * ld;
+                const int key = key0 + Copy::row(lane % Copy::COPIES, wave);
+                const int pg = __shfl(pages, min((key >> p.page_log2) - page0, 63));
+                const bool ok = (unsigned)pg < (unsigned)p.pages;
+                const int64_t at = ok ? (int64_t)k + pg * each + (key & ((1 << p.page_log2) - 1)) * ld : (int64_t)&kNanRows;
+                const int size = max(0, min(kv - key, Copy::RPC)) * ld, size_v = ok ? size : 0;
+                const int64_t from_k = uniform((int64_t)v - (int64_t)k);
 #pragma unroll
                 for (int i = 0; i < Copy::COPIES; ++i) {
-                    const int key = key0 + Copy::row(i, wave);
-                    const int pg = __builtin_amdgcn_readlane(pages, min((key >> p.page_log2) - page0, 63));
-                    const bool ok = (unsigned)pg < (unsigned)p.pages;
-                    const int64_t at = ok ? pg * each + (key & ((1 << p.page_log2) - 1)) * p.d : 0;
-                    ck.one(ok ? (const void *)(k + at) : &kNanRows, min(kv - key, Copy::RPC), ld, kt, i, wave);
-                    ck.one(v + at, ok ? min(kv - key, Copy::RPC) : 0, ld, vt, i, wave);
+                    const int64_t a = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), i) << 32 |
+                                                (uint32_t)__builtin_amdgcn_readlane((int)at, i));
+                    ck.one(a, __builtin_amdgcn_readlane(size, i), kt, i, wave);
+                    ck.one(a + from_k, __builtin_amdgcn_readlane(size_v, i), vt, i, wave);
                 }
             } else {
                 const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);

@@ -144,7 +144,7 @@ template <typename T, int D> struct SeqBwdQ {
                                 float delta, float scale, f32x16 *dq, int lane)
     {
         // fragments of a 32-key part: the rows of K, the rows of V, the columns of K
-        constexpr int NA = S::kF32 ? 0 : 2 * S::ND, NP = 2 * S::NS + NA, N = KT * NP, AHEAD = 4;
+        constexpr int NA = S::kF32 ? 0 : 2 * S::ND, NP = 2 * S::NS + NA, N = KT * NP, AHEAD = S::kF32 ? 2 : 4;
         FragStream<frag, N, AHEAD> stream;
         auto load = [&](int u) {
             const int off = u / NP * 32 * S::ROW, i = u % NP;
@@ -305,7 +305,7 @@ template <typename T, int D> struct SeqBwdK {
                                 const char *vt, int ahead, int first, float c, float scale, Grads &x, int lane)
     {
         // fragments: the rows of Q, then of dO (each with V's behind it), then the columns of dO and of Q
-        constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = D > 96 ? 2 : 4;
+        constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = S::kF32 || D > 96 ? 2 : 4;
         FragStream<frag, N, AHEAD> stream;
         auto load = [&](int u) {
             if constexpr (!S::kF32)

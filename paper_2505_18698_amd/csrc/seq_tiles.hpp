@@ -256,7 +256,7 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
     // The copy itself, in assembly: behind the builtin the compiler waits for it
     // before every later LDS read, those of the other tiles among them, so that
     // a tile would not arrive while another is computed.  The instruction writes LDS and
-    // no register; tile_barrier() or wave_arrived() waits for it.
+    // no register; tile_barrier() waits for it.
     // (The compiler does not see into it either: the five wait states are
     // those between a vector write of a scalar register and its use here.)
     __device__ static void copy(u32x4 r, int off, char *tile, int i, int wave)
@@ -265,25 +265,17 @@ template <typename T, int D, int BN, int NW> struct TileCopy {
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                      :: "v"(off), "s"(r), "s"(uniform(to)) : "memory", "m0");
     }
-    // copy i alone, from its own first row
-    __device__ void one(const void *rows, int valid, int ld, char *to, int i, int wave) const
+    // copy i alone, from its own first row, of which `size` bytes can be read
+    __device__ void one(int64_t rows, int size, char *to, int i, int wave) const
     {
-        copy(source(rows, valid, ld), off[i % VAR], to, i, wave);
+        copy(u32x4{(uint32_t)rows, (uint32_t)(rows >> 32) & 0xffffu, (uint32_t)size, (uint32_t)Span::kDefault}, off[i % VAR], to, i, wave);
     }
-    // the whole tile from its first row.  With one wave a tile the addresses that differ from copy to
-    // copy stay in scalar registers (the user of those has no others left), else in the lanes'.
+    // the whole tile from its first row
     __device__ void tile(const void *rows, int valid, int ld, char *to, int wave) const
     {
-        if constexpr (NW == 1) {
-            const int64_t at = uniform((int64_t)rows);
-            valid = uniform(valid);
+        const u32x4 r = source(rows, valid, ld);
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) one((const void *)(at + (int64_t)row(i, 0) * ld), valid - row(i, 0), ld, to, i, 0);
-        } else {
-            const u32x4 r = source(rows, valid, ld);
-#pragma unroll
-            for (int i = 0; i < COPIES; ++i) copy(r, off[i % VAR] + row(i, wave) * ld, to, i, wave);
-        }
+        for (int i = 0; i < COPIES; ++i) copy(r, off[i % VAR] + row(i, wave) * ld, to, i, wave);
     }
 };
 
