@@ -240,11 +240,18 @@ template <typename T, int D> struct SeqBwdQ {
         for (int dt = 0; dt < S::ND; ++dt) dq[dt] = f32x16{};
         bring(0, 0);
         int key0 = 0, buf = 0;
-#pragma unroll 1
-        for (; key0 + BN <= min(see_all, last); key0 += BN, buf ^= 1) {
+        // (a copy of the step for each buffer: its LDS addresses are constants)
+        const int whole = min(see_all, last) - BN;
+        auto unmasked = [&](int b) {
             tile_barrier();
-            bring(key0 + BN, buf ^ 1);
-            step<false>(lds + 2 * TILE * buf + part * S::ROW, lds + 2 * TILE * buf + TILE + part * S::ROW, qf, gf, 0, p.c, lse2, delta, sc.ds, dq, lane);
+            bring(key0 + BN, b ^ 1);
+            step<false>(lds + 2 * TILE * b + part * S::ROW, lds + 2 * TILE * b + TILE + part * S::ROW, qf, gf, 0, p.c, lse2, delta, sc.ds, dq, lane);
+            key0 += BN, buf = b ^ 1;
+        };
+#pragma unroll 1
+        while (key0 <= whole) {
+            unmasked(0);
+            if (key0 <= whole) unmasked(1);
         }
 #pragma unroll 1
         for (; key0 < last; key0 += BN, buf ^= 1) {
