@@ -258,8 +258,8 @@ int log2_of(int64_t page)
 // (two a compute unit; find_share in seq_attn.hpp), except where the longest possible context
 // is a few key tiles, or where there are many times as many row tiles: then a row tile is a workgroup's.
 // (64 single tokens over up to 8192: 103 us, in pieces of equal length 122, 128-row tiles 266;
-// 8 chunks of up to 512 over up to 16384: 210 us, in pieces of equal length 241.
-// One token over 501: 9.5 us in one workgroup a head.)
+// 8 chunks of up to 512 over up to 16384: 213 us, in pieces of equal length 241 (203 since).
+// One token over 501: 9 us in one workgroup a head.)
 struct PagedSplit {
     int rows;
     bool split;

@@ -103,13 +103,13 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // two lane halves, and the weights feed O^T = V^T P^T straight from registers.
 //
 // What bounds it.  Many rows: the products, 4 D operations a pair.  One causal sequence of
-// 16384 tokens, 16 heads on 4 of 128, bf16: 1.02 ms, 1.08 PFLOP/s (a library product
-// of 8192^3 reaches 1.23), the matrix units busy in 60 % of the cycles, at the 1.6 GHz that
+// 16384 tokens, 16 heads on 4 of 128, bf16: 1.01 ms, 1.09 PFLOP/s (a library product
+// of 8192^3 reaches 1.23), the matrix units busy in 61 % of the cycles, at the 1.7 GHz that
 // the card's power leaves.  There a tile's softmax (16 exponentials a lane and 32 x 32 block) runs on one
 // of a SIMD's two waves beside the other's products, and no LDS bank conflict is left.  64 rows
 // and key halves as in fp32 took 1.20 ms, 64 rows a wave (RB = 2) 1.40 ms.
 // Single tokens: the bytes of K and V.  64 requests of up to 8192 tokens, 32 heads on 8 of
-// 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB: 190 us, 5.6 TB/s (a large copy
+// 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB: 190-197 us, 5.5 TB/s (a large copy
 // reads and writes 4.9).
 template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     using S = SeqTile<T, D>;

@@ -15,8 +15,8 @@
 // sum has one owner that adds in a fixed order in fp32 registers, without atomics.
 //
 // On 9550 rows of 7 sequences, 16 heads on 4 of 128, bf16, causal (264 GFLOP in 5 products, 370 in 7):
-// statistics 24 us (118 MB, 4.9 TB/s), dQ, dK and dV 466 us, sums of the pieces 22 us.
-// The matrix units are busy in 44 % of the cycles and the vector units in 33 %: what
+// statistics 23 us (118 MB, 5 TB/s), dQ, dK and dV 435-465 us, sums of the pieces 22 us.
+// The matrix units are busy in 40 to 44 % of the cycles and the vector units in 30 to 33 %: what
 // bounds it is the chain from scores to dS, with two waves a SIMD to cover it.
 #pragma once
 
@@ -507,7 +507,7 @@ template <typename T, int D> struct SeqBwdK {
 
 // Both in one launch, dQ first: its longest walks, over all keys of a long
 // sequence, start at once, and the shorter ones of dK and dV fill what they leave free.  (fp32, 6 sequences of up to 1000
-// tokens, 12 heads of 64: 98 us, two launches 132; the rows above 466 us, two
+// tokens, 12 heads of 64: 98 us, two launches 132 (87 since); the rows above 466 us, two
 // launches 474, dK and dV first 472.)
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd(SeqBwd p, int blocks_q)
 {
