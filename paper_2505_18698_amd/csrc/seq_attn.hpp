@@ -91,9 +91,9 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
 // The share that step x of a line belongs to.
 __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int)(((x + 1) * shares - 1) / all); }
 
-// One workgroup of 4 waves per tile of R = 32 RB WR packed rows (token, head of
+// One workgroup of 4 waves per tile of R = 32 WR packed rows (token, head of
 // the group) of one key head: the heads of a group read the same K and V, so
-// they share the tile's copies.  With WR = 4 each wave owns 32 RB rows.  With WR = 1, for
+// they share the tile's copies.  With WR = 4 each wave owns 32 rows.  With WR = 1, for
 // the few rows of single tokens, all waves copy, every wave takes one of the
 // tile's 32-key parts, and the first joins them at the end.  WR = 2, in fp32: two
 // row blocks by two 32-key parts (128 rows of 1000 keys are 54 us of a compute unit's fp32
@@ -107,14 +107,14 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // of 8192^3 reaches 1.23), the matrix units busy in 61 % of the cycles, at the 1.7 GHz that
 // the card's power leaves.  There a tile's softmax (16 exponentials a lane and 32 x 32 block) runs on one
 // of a SIMD's two waves beside the other's products, and no LDS bank conflict is left.  64 rows
-// and key halves as in fp32 took 1.20 ms, 64 rows a wave (RB = 2) 1.40 ms.
+// and key halves as in fp32 took 1.20 ms, 64 rows a wave 1.40 ms.
 // Single tokens: the bytes of K and V.  64 requests of up to 8192 tokens, 32 heads on 8 of
 // 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB: 190-197 us, 5.5 TB/s (a large copy
 // reads and writes 4.9).
-template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
+template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
-    static constexpr int W = 4, NTH = 64 * W, R = 32 * RB * WR;
+    static constexpr int W = 4, NTH = 64 * W, R = 32 * WR;
     // Keys a tile.  Of few rows in 16-bit types, where the workgroup has a context
     // alone, 32 a wave.  Of few rows in fp32, whose products bound them as much as their bytes:
     // as many waves as the room lets work, four in one workgroup (D = 64: 161 us for the
@@ -136,23 +136,20 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     static constexpr float kSlack = 8.f;
 
     struct State {
-        f32x16 o[RB][S::ND];  // O^T: lane 32 h + c, row c, columns 32 dt + kRow32(r) + 4 h
-        float ref[RB], sum[RB];
+        f32x16 o[S::ND];  // O^T: lane 32 h + c, row c, columns 32 dt + kRow32(r) + 4 h
+        float ref, sum;
     };
 
     // One key tile.  MASK: some row of the wave sees only a part of it.  There
     // `fine` weights take part with twice the bits: rows of few keys, all of which
     // are in such tiles, have outputs as exact as the statistics.
     template <bool MASK>
-    __device__ static void step(const char *kt, const char *vt, const frag (*qf)[S::NS], const int *vis, int key0,
+    __device__ static void step(const char *kt, const char *vt, const frag *qf, int vis, int key0,
                                 float c, bool fine, State &st, int lane)
     {
-        f32x16 s[RB][KT];
+        f32x16 s[KT];
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int t = 0; t < KT; ++t) s[rb][t] = f32x16{};
-        // (one read of K or V feeds all RB row blocks)
+        for (int t = 0; t < KT; ++t) s[t] = f32x16{};
         constexpr int NK = KT * S::NS, NV = S::kF32 ? KT * 16 * S::ND : KT * 2 * S::ND, AHEAD = S::kF32 ? 2 : 4;
         FragStream<frag, S::kF32 ? NK : NK + NV, AHEAD> stream;
         auto load = [&](int u) {
@@ -166,46 +163,42 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
 #pragma unroll
         for (int u = 0; u < NK; ++u) {
             stream.next(u, load, [&](const frag &x) {
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) s[rb][u / S::NS] = S::M::mma(x, qf[rb][u % S::NS], s[rb][u / S::NS]);
+                s[u / S::NS] = S::M::mma(x, qf[u % S::NS], s[u / S::NS]);
             });
-            sched_step<RB * (S::kF32 ? 4 : 1)>(reads(u));
+            sched_step<(S::kF32 ? 4 : 1)>(reads(u));
         }
-        Probs32<T> pf[KT][RB];
+        Probs32<T> pf[KT];
+        const int see = vis - key0 - 4 * (lane >> 5);
+        float mx = -INFINITY;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int see = vis[rb] - key0 - 4 * (lane >> 5);
-            float mx = -INFINITY;
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int t = 0; t < KT; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (MASK && 32 * t + kRow32(r) >= see) s[rb][t][r] = -INFINITY;
-                    mx = max_nan(mx, s[rb][t][r]);
-                }
-            mx = wave_xor_max<32>(mx) * c;
-            if (__any(mx > st.ref[rb] + kSlack)) {
-                const float up = fmaxf(mx, st.ref[rb]);
-                // (a row's first keys: all it has so far is zero, or infinities that take_foreign() added)
-                const float by = st.ref[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref[rb] - up);
-                st.ref[rb] = up;
-                st.sum[rb] *= by;
-#pragma unroll
-                for (int dt = 0; dt < S::ND; ++dt) st.o[rb][dt] *= by;
+            for (int r = 0; r < 16; ++r) {
+                if (MASK && 32 * t + kRow32(r) >= see) s[t][r] = -INFINITY;
+                mx = max_nan(mx, s[t][r]);
             }
-            const float ref = st.ref[rb] == -INFINITY ? 0.f : st.ref[rb];
-            float sum = 0.f;
+        mx = wave_xor_max<32>(mx) * c;
+        if (__any(mx > st.ref + kSlack)) {
+            const float up = fmaxf(mx, st.ref);
+            // (a row's first keys: all it has so far is zero, or infinities that take_foreign() added)
+            const float by = st.ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref - up);
+            st.ref = up;
+            st.sum *= by;
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[rb][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][t][r], c, -ref));
-                    sum += s[rb][t][r];
-                }
-                pf[t][rb].pack(s[rb][t]);
-            }
-            st.sum[rb] += sum;
+            for (int dt = 0; dt < S::ND; ++dt) st.o[dt] *= by;
         }
+        const float ref = st.ref == -INFINITY ? 0.f : st.ref;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r], c, -ref));
+                sum += s[t][r];
+            }
+            pf[t].pack(s[t]);
+        }
+        st.sum += sum;
         if constexpr (S::kF32) {
             add_columns(vt, pf, st, lane);
         } else {
@@ -213,25 +206,23 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             for (int u = NK; u < NK + NV; ++u) {
                 const int ks = (u - NK) / S::ND, dt = (u - NK) % S::ND;
                 stream.next(u, load, [&](const frag &x) {
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = S::M::mma(x, pf[ks / 2][rb].f[ks % 2], st.o[rb][dt]);
+                    st.o[dt] = S::M::mma(x, pf[ks / 2].f[ks % 2], st.o[dt]);
                 });
-                sched_step<RB>(reads(u));
+                sched_step<1>(reads(u));
             }
         }
         if constexpr (MASK && !S::kF32) {
             if (fine) {
 #pragma unroll
                 for (int t = 0; t < KT; ++t)
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) pf[t][rb] = pf[t][rb].rest(s[rb][t]);
+                    pf[t] = pf[t].rest(s[t]);
                 add_columns(vt, pf, st, lane);
             }
         }
     }
 
     // O^T += V^T P^T of a tile.
-    __device__ static void add_columns(const char *vt, const Probs32<T> (*pf)[RB], State &st, int lane)
+    __device__ static void add_columns(const char *vt, const Probs32<T> *pf, State &st, int lane)
     {
 #pragma unroll
         for (int k = 0; k < KT * (S::kF32 ? 16 : 2); ++k)
@@ -239,12 +230,10 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             for (int dt = 0; dt < S::ND; ++dt) {
                 if constexpr (S::kF32) {
                     const float x = S::element(vt, 32 * (k / 16) + kRow32(k % 16) + 4 * (lane >> 5), dt, lane);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, pf[k / 16][rb].s[k % 16], st.o[rb][dt], 0, 0, 0);
+                    st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, pf[k / 16].s[k % 16], st.o[dt], 0, 0, 0);
                 } else {
                     const frag x = S::columns(vt + k * 16 * S::ROW, dt, lane);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt] = S::M::mma(x, pf[k / 2][rb].f[k % 2], st.o[rb][dt]);
+                    st.o[dt] = S::M::mma(x, pf[k / 2].f[k % 2], st.o[dt]);
                 }
             }
     }
@@ -264,7 +253,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         }
         return bad;
     }
-    __device__ static void take_foreign(char *vt, const int *vis, int key0, bool mine, State &st, int lane)
+    __device__ static void take_foreign(char *vt, int vis, int key0, bool mine, State &st, int lane)
     {
 #pragma unroll 1
         for (int key = 0; key < (mine ? BN : 0); ++key) {
@@ -274,8 +263,7 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
                 for (int r = 0; r < 16; ++r) {
                     const int col = 32 * dt + kRow32(r) + 4 * (lane >> 5);
                     const float y = (float)*reinterpret_cast<const T *>(vt + key * S::ROW + (((col / S::V) ^ S::swz(key)) * 16) + col % S::V * (int)sizeof(T));
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) st.o[rb][dt][r] += fabsf(y) < INFINITY || key0 + key >= vis[rb] ? 0.f : y;
+                    st.o[dt][r] += fabsf(y) < INFINITY || key0 + key >= vis ? 0.f : y;
                 }
         }
         __syncthreads();
@@ -290,37 +278,31 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
     __device__ static void join_waves(char *lds, int wave, int lane, State &st)
     {
         constexpr int N = S::ND * 16 + 2;  // a lane's values of a row block
-        static_assert((KW - 1) * WR * RB * N * 256 <= 2 * STAGES * TILE, "the tiles' room holds them");
-        float *mine = reinterpret_cast<float *>(lds) + (wave - WR) * RB * N * 64 + lane;
+        static_assert((KW - 1) * WR * N * 256 <= 2 * STAGES * TILE, "the tiles' room holds them");
+        float *mine = reinterpret_cast<float *>(lds) + (wave - WR) * N * 64 + lane;
         __syncthreads();
         if (wave >= WR && wave < KW * WR) {
+            mine[(N - 2) * 64] = st.ref, mine[(N - 1) * 64] = st.sum;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                mine[(rb * N + N - 2) * 64] = st.ref[rb], mine[(rb * N + N - 1) * 64] = st.sum[rb];
+            for (int dt = 0; dt < S::ND; ++dt)
 #pragma unroll
-                for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) mine[(rb * N + dt * 16 + r) * 64] = st.o[rb][dt][r];
-            }
+                for (int r = 0; r < 16; ++r) mine[(dt * 16 + r) * 64] = st.o[dt][r];
         }
         __syncthreads();
         if (wave >= WR) return;
 #pragma unroll
         for (int w = 1; w < KW; ++w) {
-            const float *other = reinterpret_cast<float *>(lds) + ((w - 1) * WR + wave) * RB * N * 64 + lane;
+            const float *other = reinterpret_cast<float *>(lds) + ((w - 1) * WR + wave) * N * 64 + lane;
+            const float ref = other[(N - 2) * 64], up = fmaxf(ref, st.ref), base = up == -INFINITY ? 0.f : up;
+            // (a part without a key adds zeros, or infinities that take_foreign() added)
+            const float a = st.ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref - base);
+            const float b = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - base);
+            st.ref = up;
+            st.sum = st.sum * a + other[(N - 1) * 64] * b;
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const float ref = other[(rb * N + N - 2) * 64], up = fmaxf(ref, st.ref[rb]), base = up == -INFINITY ? 0.f : up;
-                // (a part without a key adds zeros, or infinities that take_foreign() added)
-                const float a = st.ref[rb] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref[rb] - base);
-                const float b = ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref - base);
-                st.ref[rb] = up;
-                st.sum[rb] = st.sum[rb] * a + other[(rb * N + N - 1) * 64] * b;
+            for (int dt = 0; dt < S::ND; ++dt)
 #pragma unroll
-                for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) st.o[rb][dt][r] = st.o[rb][dt][r] * a + other[(rb * N + dt * 16 + r) * 64] * b;
-            }
+                for (int r = 0; r < 16; ++r) st.o[dt][r] = st.o[dt][r] * a + other[(dt * 16 + r) * 64] * b;
         }
     }
 
@@ -426,10 +408,10 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
             const int64_t i = (int64_t)min(r, rows - 1) / p.G + (PAGED ? kv - n : 0) + 1;
             return p.causal ? (int)max((int64_t)0, min(i, (int64_t)kv)) : kv;
         };
-        const int wr0 = r0 + wave % WR * 32 * RB;
+        const int wr0 = r0 + wave % WR * 32;
         const int part = min(wave / WR, KW - 1);  // this wave's keys in a tile, in parts of 32
         const bool idle = wave >= WR * KW;
-        const int see_most = uniform(visible(wr0 + 32 * RB - 1));  // keys that some row of the wave sees
+        const int see_most = uniform(visible(wr0 + 31));  // keys that some row of the wave sees
         const int see_all = uniform(visible(r0));  // keys that every row of the tile sees
         const int first = key_tile0 * BN;
         const int last = uniform((int)min((int64_t)visible(r0 + R - 1), key_tiles == 0x7fffffff ? (int64_t)0x7fffffff : (int64_t)(key_tile0 + key_tiles) * BN));
@@ -437,21 +419,14 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         // this lane's query rows; offsets of q and out from the tile's first token
         const int tok0 = r0 / p.G;
         const Span qs((const T *)p.q + (row0 + tok0) * p.ldq + (int64_t)kvh * p.G * p.d);
-        int vis[RB], tok[RB], head[RB];
-        frag qf[RB][S::NS];
+        frag qf[S::NS];
+        const int row = wr0 + (lane & 31), r = min(row, rows - 1);
+        const int vis = visible(r), tok = r / p.G - tok0, head = r % p.G;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int r = min(wr0 + 32 * rb + (lane & 31), rows - 1);
-            vis[rb] = visible(r);
-            tok[rb] = r / p.G - tok0;
-            head[rb] = r % p.G;
-            const int at = tok[rb] * (int)p.ldq + head[rb] * p.d;
-#pragma unroll
-            for (int i = 0; i < S::NS; ++i) {
-                const int col = (2 * i + (lane >> 5)) * S::V;
-                const u32x4 x = qs.load16((at + col) * (int)sizeof(T), col < p.d);
-                __builtin_memcpy(&qf[rb][i], &x, 16);
-            }
+        for (int i = 0; i < S::NS; ++i) {
+            const int col = (2 * i + (lane >> 5)) * S::V;
+            const u32x4 x = qs.load16((tok * (int)p.ldq + head * p.d + col) * (int)sizeof(T), col < p.d);
+            __builtin_memcpy(&qf[i], &x, 16);
         }
 
         Rows src;
@@ -471,12 +446,9 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         }
 
         State st;
+        st.ref = -INFINITY, st.sum = 0.f;
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            st.ref[rb] = -INFINITY, st.sum[rb] = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < S::ND; ++dt) st.o[rb][dt] = f32x16{};
-        }
+        for (int dt = 0; dt < S::ND; ++dt) st.o[dt] = f32x16{};
         // A tile arrives while the one or two before it are computed.  Two
         // loops, the tiles that every row sees whole and the others: one loop
         // with both kinds of step keeps the output registers twice.
@@ -531,46 +503,42 @@ template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT> struct SeqA
         }
 
         const Span os((T *)p.out + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int r = wr0 + 32 * rb + (lane & 31);
-            const float sum = wave_xor_sum<32>(st.sum[rb]);
-            const bool none = vis[rb] <= first;  // no key to see
-            const float inv = none ? 0.f : 1.f / sum;
-            const float l2 = none ? -INFINITY : st.ref[rb] + __builtin_amdgcn_logf(sum);
-            const bool real = r < rows;
-            if (SPLIT && parts) {
-                const int64_t at = unit * R + wr0 - r0 + 32 * rb;
-                const Span ps(p.part_o + at * D);
-                store_row<float, S::ND>(ps, st.o[rb], inv, (lane & 31) * D, D, real, lane);
-                if (real && lane < 32) p.part_l[at + lane] = l2;
-                continue;
-            }
-            const int at = (tok[rb] * p.Hkv * p.G + head[rb]) * p.d;
-            store_row<T, S::ND>(os, st.o[rb], inv, at, p.d, real, lane);
-            if constexpr (!S::kF32) {
-                if (p.rest) {
-                    const Span es((T *)p.rest + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
-#pragma unroll
-                    for (int dt = 0; dt < S::ND; ++dt)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const float x = st.o[rb][dt][r] * inv;
-                            st.o[rb][dt][r] = x - (float)to_elem<T>(x);
-                        }
-                    store_row<T, S::ND>(es, st.o[rb], 1.f, at, p.d, real, lane);
-                }
-            }
-            if (p.lse && real && lane < 32)
-                p.lse[(int64_t)(kvh * p.G + head[rb]) * p.seqs.total + row0 + tok0 + tok[rb]] = l2 * kLn2;
+        const float sum = wave_xor_sum<32>(st.sum);
+        const bool none = vis <= first;  // no key to see
+        const float inv = none ? 0.f : 1.f / sum;
+        const float l2 = none ? -INFINITY : st.ref + __builtin_amdgcn_logf(sum);
+        const bool real = row < rows;
+        if (SPLIT && parts) {
+            const int64_t first_row = unit * R + wr0 - r0;
+            const Span ps(p.part_o + first_row * D);
+            store_row<float, S::ND>(ps, st.o, inv, (lane & 31) * D, D, real, lane);
+            if (real && lane < 32) p.part_l[first_row + lane] = l2;
+            return;
         }
+        const int at = (tok * p.Hkv * p.G + head) * p.d;
+        store_row<T, S::ND>(os, st.o, inv, at, p.d, real, lane);
+        if constexpr (!S::kF32) {
+            if (p.rest) {
+                const Span es((T *)p.rest + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
+#pragma unroll
+                for (int dt = 0; dt < S::ND; ++dt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float x = st.o[dt][r] * inv;
+                        st.o[dt][r] = x - (float)to_elem<T>(x);
+                    }
+                store_row<T, S::ND>(es, st.o, 1.f, at, p.d, real, lane);
+            }
+        }
+        if (p.lse && real && lane < 32)
+            p.lse[(int64_t)(kvh * p.G + head) * p.seqs.total + row0 + tok0 + tok] = l2 * kLn2;
     }
 };
 
-template <typename T, int D, int RB, int WR, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(256, RB > 1 || (sizeof(T) == 4 && D > 64 && WR > 1) ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
+template <typename T, int D, int WR, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
 {
-    using U = SeqAttn<T, D, RB, WR, PAGED, SPLIT>;
+    using U = SeqAttn<T, D, WR, PAGED, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
 }

@@ -14,15 +14,15 @@ template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p,
     int rc = L.run(kSeqFwd, [&] {
         return launched([&] {
             if (!how.paged)
-                ma::seq_attention<T, D, 1, WR, false, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, WR, false, false><<<grid, block, 0, L.stream>>>(p);
             else if (!how.split && !few)
-                ma::seq_attention<T, D, 1, WR, true, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, WR, true, false><<<grid, block, 0, L.stream>>>(p);
             else if (!how.split)
-                ma::seq_attention<T, D, 1, 1, true, false><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, true, false><<<grid, block, 0, L.stream>>>(p);
             else if (!few)
-                ma::seq_attention<T, D, 1, WR, true, true><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, WR, true, true><<<grid, block, 0, L.stream>>>(p);
             else
-                ma::seq_attention<T, D, 1, 1, true, true><<<grid, block, 0, L.stream>>>(p);
+                ma::seq_attention<T, D, 1, true, true><<<grid, block, 0, L.stream>>>(p);
         });
     });
     if (rc != MA_OK || !how.split) return rc;
