@@ -473,8 +473,8 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  * block_table : [B, blocks] device int32, contiguous.  Entries past the last
  *               token are not read.  A page number outside 0..pages - 1 leads
  *               to no read: the rows that see a token on it become NaN.
- * Calls with long contexts (a table of more than 1024 tokens a sequence, 512 in fp32) are split
- * over the keys into equal shares, and joined by a second launch, from partial
+ * Calls with long contexts (a table of more tokens a sequence than 128 KB of their keys, 512 tokens
+ * of 128 columns in 16 bits) are split over the keys into equal shares, and joined by a second launch, from partial
  * results in the workspace.
  */
 int monarch_attn_exact_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out, float *lse,

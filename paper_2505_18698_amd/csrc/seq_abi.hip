@@ -255,11 +255,13 @@ int log2_of(int64_t page)
 // How a paged call runs.  Sequences of few new rows (on average no more than 32
 // packed ones: single tokens) take 32-row tiles, whose waves share the keys.
 // The work is shared evenly by as many workgroups as the device holds at a time
-// (two a compute unit; find_share in seq_attn.hpp), except where the longest possible context
-// is a few key tiles, or where there are many times as many row tiles: then a row tile is a workgroup's.
+// (two a compute unit; find_share in seq_attn.hpp), except where the keys of the longest possible context
+// take no more than kWholeBytes, or where there are many times as many row tiles: then a row tile is a workgroup's.
 // (64 single tokens over up to 8192: 103 us, in pieces of equal length 122, 128-row tiles 266;
 // 8 chunks of up to 512 over up to 16384: 213 us, in pieces of equal length 241 (203 since).
 // One token over 501: 9 us in one workgroup a head.)
+// One token over 500 and 1000, 4 heads of 64: 9 and 12 us whole, 14 split; 8 heads of 128: 13 and 18, 15 split.
+constexpr int64_t kWholeBytes = 128 << 10;
 struct PagedSplit {
     int rows;
     bool split;
@@ -273,7 +275,7 @@ PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t
     PagedSplit s{few ? kSeqFewRows : seq_rows(dtype), false, 0, 0, 0, 0, 0};
     s.tiles = s.units = tiles_of(total, G, B, s.rows);
     const int64_t shares = std::max<int64_t>(1, 2 * num_cus / Hkv);
-    if (s.tiles >= 16 * shares || max_keys <= 16 * seq_tile_keys(dtype)) return s;
+    if (s.tiles >= 16 * shares || max_keys * tile_d(d) * (int64_t)elem_bytes(dtype) <= kWholeBytes) return s;
     s.split = true;
     s.units = shares;
     const size_t rows = (size_t)(shares + s.tiles) * Hkv * s.rows;

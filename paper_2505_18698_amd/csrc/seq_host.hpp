@@ -50,7 +50,6 @@ template <typename T> constexpr int kSeqRows = sizeof(T) == 4 ? 64 : 128;
 constexpr int kSeqFewRows = 32;
 inline int seq_rows(int32_t dtype) { return dtype == MA_F32 ? kSeqRows<float> : kSeqRows<__bf16>; }
 constexpr int kSeqBwdKeys = 64;  // keys a workgroup takes in the gradient
-inline int seq_tile_keys(int32_t dtype) { return dtype == MA_F32 ? 32 : 64; }
 
 template <typename T> int run_seq_fwd(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how);
 template <typename T> int run_seq_bwd(Launcher &L, const ma::SeqBwd &p);
