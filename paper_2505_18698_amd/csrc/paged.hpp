@@ -10,13 +10,12 @@ namespace ma {
 
 constexpr int kPlanMaxB = MONARCH_ATTN_PLAN_MAX_B;
 
-// Every workgroup forms the running sums over all requests in LDS (two integers a
-// request, microseconds for thousands of them) and then takes its share of the
-// new table entries and of the slots, one a thread, each finding its request by bisection.
-// So the call is one launch without a wait between workgroups: the sums take
-// less than a second launch would.  64 requests: 4.3 us; 512 with 24045 new tokens: 6.7 us (10 with four
-// slots a thread).  What bounds it is latency:
-// the lengths, the sums, the free pages and the table are each read behind the one before.
+// Every workgroup forms the running sums over all requests in LDS (two integers a request,
+// microseconds for thousands of them) and then takes its share of the new table entries and of the
+// slots, one a thread, each finding its request by bisection. So the call is one launch without a
+// wait between workgroups: the sums take less than a second launch would.  64 requests: 4.3 us; 512
+// with 24045 new tokens: 6.7 us (10 with four slots a thread).  What bounds it is latency: the
+// lengths, the sums, the free pages and the table are each read behind the one before.
 static __global__ __launch_bounds__(256) void paged_plan(PagedPlan p)
 {
     __shared__ int row_end[kPlanMaxB], page_end[kPlanMaxB];  // inclusive sums of new tokens and new pages

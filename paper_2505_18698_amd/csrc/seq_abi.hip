@@ -84,7 +84,8 @@ int check_stride(const char *name, int64_t ld, int64_t width, int32_t dtype)
     return MA_OK;
 }
 
-// Row tiles of R packed rows over all sequences, at most (tile0 in seq_tiles.hpp), and one without any.
+// Row tiles of R packed rows over all sequences, at most (tile0 in seq_tiles.hpp), and one without
+// any.
 int64_t tiles_of(int64_t total, int64_t rows_a_token, int64_t B, int64_t R) { return std::max<int64_t>(1, total * rows_a_token / R + B); }
 
 int check_grid(int64_t units, int64_t Hkv)
@@ -175,12 +176,12 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
 constexpr int kNormBlocks = 1024;
 size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * total) * 4) + align_up(kNormBlocks * sizeof(float2)); }
 
-// Pieces that the query rows of a key tile are cut into.  The longest walk, of the
-// first keys of one causal sequence that fills the call, is twice the mean one,
-// so 1024 key tiles and heads (two rounds of two workgroups on 256 compute units) end with it; the
-// pieces make it half of the mean work of a compute unit's slot.  A piece of fewer than 8
-// tiles is not worth its sums' way through memory, nor are more than three pieces (9550 rows, 16 heads on 4 of 128, with the
-// forward: 608 us; 614 with two or four).
+// Pieces that the query rows of a key tile are cut into.  The longest walk, of the first keys of
+// one causal sequence that fills the call, is twice the mean one, so 1024 key tiles and heads (two
+// rounds of two workgroups on 256 compute units) end with it; the pieces make it half of the mean
+// work of a compute unit's slot.  A piece of fewer than 8 tiles is not worth its sums' way through
+// memory, nor are more than three pieces (9550 rows, 16 heads on 4 of 128, with the forward: 608
+// us; 614 with two or four).
 int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
 {
     const int64_t want = (8 * num_cus + tiles_k * Hkv - 1) / (tiles_k * Hkv);
@@ -252,15 +253,16 @@ int log2_of(int64_t page)
     return x;
 }
 
-// How a paged call runs.  Sequences of few new rows (on average no more than 32
-// packed ones: single tokens) take 32-row tiles, whose waves share the keys.
-// The work is shared evenly by as many workgroups as the device holds at a time
-// (two a compute unit; find_share in seq_attn.hpp), except where the keys of the longest possible context
-// take no more than kWholeBytes, or where there are many times as many row tiles: then a row tile is a workgroup's.
-// (64 single tokens over up to 8192: 103 us, in pieces of equal length 122, 128-row tiles 266;
-// 8 chunks of up to 512 over up to 16384: 213 us, in pieces of equal length 241 (203 since).
-// One token over 501: 9 us in one workgroup a head.)
-// One token over 500 and 1000, 4 heads of 64: 9 and 12 us whole, 14 split; 8 heads of 128: 13 and 18, 15 split.
+// How a paged call runs.  Sequences of few new rows (on average no more than 32 packed ones: single
+// tokens) take 32-row tiles, whose waves share the keys. The work is shared evenly by as many
+// workgroups as the device holds at a time (two a compute unit; find_share in seq_attn.hpp), except
+// where the keys of the longest possible context take no more than kWholeBytes, or where there are
+// many times as many row tiles: then a row tile is a workgroup's. (64 single tokens over up to
+// 8192: 103 us, in pieces of equal length 122, 128-row tiles 266; 8 chunks of up to 512 over up to
+// 16384: 213 us, in pieces of equal length 241 (203 since).)
+//
+// kWholeBytes: one token over 500 and 1000, 4 heads of 64: 9 and 12 us whole, 14 split; 8 heads of
+// 128: 13 and 18 us whole, 15 split.
 constexpr int64_t kWholeBytes = 128 << 10;
 struct PagedSplit {
     int rows;

@@ -9,15 +9,14 @@
 
 namespace ma {
 
-// How a split call divides its work.  All row tiles of R rows in order, each with
-// the key tiles (BN keys) of its sequence, are one line of `all` steps, which the
-// workgroups share evenly: share w takes the steps from w all / shares on, in segments that
-// lie in one row tile each.  So every workgroup ends at the same time whatever the
-// contexts are, and starts once.  A row tile counts kBegin steps more than it has, for
-// what its first copies, its rows and its masked key tiles take (measured: 8 us to a step's 2 with 128
-// rows, 6 to 2.4 with 32; without, the workgroups of 8 chunks of up to 512 tokens
-// ended between 153 and 257 us).  The segment of share w in row tile i has the
-// number w + i, as both only grow along the line.
+// How a split call divides its work.  All row tiles of R rows in order, each with the key tiles (BN
+// keys) of its sequence, are one line of `all` steps, which the workgroups share evenly: share w
+// takes the steps from w all / shares on, in segments that lie in one row tile each.  So every
+// workgroup ends at the same time whatever the contexts are, and starts once.  A row tile counts
+// kBegin steps more than it has, for what its first copies, its rows and its masked key tiles take
+// (measured: 8 us to a step's 2 with 128 rows, 6 to 2.4 with 32; without, the workgroups of 8
+// chunks of up to 512 tokens ended between 153 and 257 us).  The segment of share w in row tile i
+// has the number w + i, as both only grow along the line.
 template <int R> constexpr int kBegin = R > 32 ? 4 : 2;
 struct Line {
     int64_t all;       // steps
@@ -102,15 +101,14 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // statistics and the rescaling are lane scalars with one exchange between the
 // two lane halves, and the weights feed O^T = V^T P^T straight from registers.
 //
-// What bounds it.  Many rows: the products, 4 D operations a pair.  One causal sequence of
-// 16384 tokens, 16 heads on 4 of 128, bf16: 1.01 ms, 1.09 PFLOP/s (a library product
-// of 8192^3 reaches 1.23), the matrix units busy in 61 % of the cycles, at the 1.7 GHz that
-// the card's power leaves.  There a tile's softmax (16 exponentials a lane and 32 x 32 block) runs on one
-// of a SIMD's two waves beside the other's products, and no LDS bank conflict is left.  64 rows
-// and key halves as in fp32 took 1.20 ms, 64 rows a wave 1.40 ms.
-// Single tokens: the bytes of K and V.  64 requests of up to 8192 tokens, 32 heads on 8 of
-// 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB: 190-197 us, 5.5 TB/s (a large copy
-// reads and writes 4.9).
+// What bounds it.  Many rows: the products, 4 D operations a pair.  One causal sequence of 16384
+// tokens, 16 heads on 4 of 128, bf16: 1.01 ms, 1.09 PFLOP/s (a library product of 8192^3 reaches
+// 1.23), the matrix units busy in 61 % of the cycles, at the 1.7 GHz that the card's power leaves.
+// There a tile's softmax (16 exponentials a lane and 32 x 32 block) runs on one of a SIMD's two
+// waves beside the other's products, and no LDS bank conflict is left.  64 rows and key halves as
+// in fp32 took 1.20 ms, 64 rows a wave 1.40 ms. Single tokens: the bytes of K and V.  64 requests
+// of up to 8192 tokens, 32 heads on 8 of 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB:
+// 190-197 us, 5.5 TB/s (a large copy reads and writes 4.9).
 template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
@@ -130,9 +128,9 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     static constexpr int STAGES = WR != 1 || S::kF32 ? 2 : SPLIT ? (D <= 64 ? 4 : 2) : D <= 64 ? 3 : 2;
     static constexpr int LDS_BYTES = 2 * STAGES * TILE + 16;  // K and V
     using Copy = TileCopy<T, D, BN, W>;
-    // A row's weights are taken relative to a reference that follows its running
-    // maximum only when that has grown by more than 2^kSlack: the sums stay exact
-    // to fp32 (weights up to 2^kSlack), and the output is rescaled a few times a row instead of once a tile.
+    // A row's weights are taken relative to a reference that follows its running maximum only when
+    // that has grown by more than 2^kSlack: the sums stay exact to fp32 (weights up to 2^kSlack),
+    // and the output is rescaled a few times a row instead of once a tile.
     static constexpr float kSlack = 8.f;
 
     struct State {
@@ -180,7 +178,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         mx = wave_xor_max<32>(mx) * c;
         if (__any(mx > st.ref + kSlack)) {
             const float up = fmaxf(mx, st.ref);
-            // (a row's first keys: all it has so far is zero, or infinities that take_foreign() added)
+            // (a row's first keys: all it has so far is zero, or infinities that take_foreign()
+            // added)
             const float by = st.ref == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.ref - up);
             st.ref = up;
             st.sum *= by;
@@ -472,7 +471,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         };
         auto next = [&] { key0 += BN, buf = buf == STAGES - 1 ? 0 : buf + 1; };
         // (a copy of the step for each buffer, whose LDS addresses are then constants: 1.01 ms for
-        // 1.03 on the sequence of 16384 tokens; rows of 512 bytes and paged calls leave no registers for it)
+        // 1.03 on the sequence of 16384 tokens; rows of 512 bytes and paged calls leave no
+        // registers for it)
         constexpr int kCopies = !PAGED && D * sizeof(T) <= 256 ? STAGES : 1;
         const int whole = min(see_all, last) - BN;
 #pragma unroll 1
@@ -543,11 +543,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGE
     U::run(p, lds);
 }
 
-// The segments of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x).
-// One workgroup per row tile and key head, and, of tiles of many rows, 8 rows, 32
-// threads a row (they have few segments); of 32-row tiles, `gridDim.y`-th of the rows, one
-// at a time, 32 threads a segment and 8 segments at once.  5 us for single tokens, 13 us for 2786 rows
-// of 32 heads, of which it reads 30 MB of segments.
+// The segments of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x). One
+// workgroup per row tile and key head, and, of tiles of many rows, 8 rows, 32 threads a row (they
+// have few segments); of 32-row tiles, `gridDim.y`-th of the rows, one at a time, 32 threads a
+// segment and 8 segments at once.  5 us for single tokens, 13 us for 2786 rows of 32 heads, of
+// which it reads 30 MB of segments.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
 {

@@ -14,10 +14,10 @@
 // The scores and dP are formed twice (7 products instead of 5), so that each
 // sum has one owner that adds in a fixed order in fp32 registers, without atomics.
 //
-// On 9550 rows of 7 sequences, 16 heads on 4 of 128, bf16, causal (264 GFLOP in 5 products, 370 in 7):
-// statistics 23 us (118 MB, 5 TB/s), dQ, dK and dV 435-465 us, sums of the pieces 22 us.
-// The matrix units are busy in 40 to 44 % of the cycles and the vector units in 30 to 33 %: what
-// bounds it is the chain from scores to dS, with two waves a SIMD to cover it.
+// On 9550 rows of 7 sequences, 16 heads on 4 of 128, bf16, causal (264 GFLOP in 5 products, 370 in
+// 7): statistics 23 us (118 MB, 5 TB/s), dQ, dK and dV 435-465 us, sums of the pieces 22 us. The
+// matrix units are busy in 40 to 44 % of the cycles and the vector units in 30 to 33 %: what bounds
+// it is the chain from scores to dS, with two waves a SIMD to cover it.
 #pragma once
 
 #include "seq_attn.hpp"
@@ -304,14 +304,16 @@ template <typename T, int D> struct SeqBwdK {
         f32x16 dk[S::ND], dv[S::ND];
     };
 
-    // 32 rows of Q and dO (qt, gt); terms: -lse / s, so that P = exp2(c S), and -delta of the rows.  `ahead`: the first of them minus
-    // this lane's key; rows before `first` (row 0, which sees one key) pass no gradient to scores.
-    // vt: the key block's V rows in LDS, where they are there.
+    // 32 rows of Q and dO (qt, gt); terms: -lse / s, so that P = exp2(c S), and -delta of the
+    // rows.  `ahead`: the first of them minus this lane's key; rows before `first` (row 0, which
+    // sees one key) pass no gradient to scores. vt: the key block's V rows in LDS, where they are
+    // there.
     template <bool MASK>
     __device__ static void step(const char *qt, const char *gt, const RowTerms<T> &terms, const frag *kf, const frag *vf,
                                 const char *vt, int ahead, int first, float c, float scale, Grads &x, int lane)
     {
-        // fragments: the rows of Q, then of dO (each with V's behind it), then the columns of dO and of Q
+        // fragments: the rows of Q, then of dO (each with V's behind it), then the columns of dO
+        // and of Q
         constexpr int NV = kVInLds ? 2 : 1, NR = (1 + NV) * S::NS, NA = S::kF32 ? 0 : 2 * S::ND, N = NR + 2 * NA, AHEAD = S::kF32 || D > 96 ? 2 : 4;
         FragStream<frag, N, AHEAD> stream;
         auto load = [&](int u) {
@@ -444,7 +446,8 @@ template <typename T, int D> struct SeqBwdK {
         Copy cq, cg;
         cq.init(ldq, p.d, wave, lane);
         cg.init(ldg, p.d, wave, lane);
-        // The walk: every head's tiles from the first row that sees a key of this workgroup on, this piece's share of them.
+        // The walk: every head's tiles from the first row that sees a key of this workgroup on,
+        // this piece's share of them.
         const int from = p.causal ? k0 : 0, tiles = (n - from + BQ - 1) / BQ;
         const int begin = uniform((int)((int64_t)p.G * tiles * piece / p.pieces)), end = uniform((int)((int64_t)p.G * tiles * (piece + 1) / p.pieces));
         float lse2 = 0.f, delta = 0.f;  // of this lane's row of the tile that is copied
@@ -505,10 +508,10 @@ template <typename T, int D> struct SeqBwdK {
     }
 };
 
-// Both in one launch, dQ first: its longest walks, over all keys of a long
-// sequence, start at once, and the shorter ones of dK and dV fill what they leave free.  (fp32, 6 sequences of up to 1000
-// tokens, 12 heads of 64: 98 us, two launches 132 (87 since); the rows above 466 us, two
-// launches 474, dK and dV first 472.)
+// Both in one launch, dQ first: its longest walks, over all keys of a long sequence, start at once,
+// and the shorter ones of dK and dV fill what they leave free.  (fp32, 6 sequences of up to 1000
+// tokens, 12 heads of 64: 98 us, two launches 132 (87 since); the rows above 466 us, two launches
+// 474, dK and dV first 472.)
 template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd(SeqBwd p, int blocks_q)
 {
     using K = SeqBwdK<T, D>;

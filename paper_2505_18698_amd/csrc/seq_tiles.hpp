@@ -61,7 +61,8 @@ template <typename T, int D> struct SeqTile {
         else return (row & 3) << 2 | ((row >> 2) & 3);
     }
 
-    // Operand fragment of the rows: lane 32 h + c holds chunk 2 st + h of row c of the 32 from `rows` on.
+    // Operand fragment of the rows: lane 32 h + c holds chunk 2 st + h of row c of the 32 from
+    // `rows` on.
     __device__ static frag row_frag(const char *rows, int st, int lane)
     {
         return *reinterpret_cast<const frag *>(rows + (lane & 31) * ROW + ((2 * st) ^ (lane >> 5) ^ swz(lane & 15)) * 16);
@@ -90,10 +91,10 @@ template <typename T, int D> struct SeqTile {
     }
 };
 
-// Two values per row of a 32 x 32 result, each as a product of its own: a lane
-// of the left operand holds its row's x in three slots, as bf16 values whose sum
-// is x to 2^-24, and y in three others; the right operand holds ones in either's.
-// So they reach all results of the row without passing through LDS.  (fp32: x and y in the two slots.)
+// Two values per row of a 32 x 32 result, each as a product of its own: a lane of the left operand
+// holds its row's x in three slots, as bf16 values whose sum is x to 2^-24, and y in three others;
+// the right operand holds ones in either's. So they reach all results of the row without passing
+// through LDS.  (fp32: x and y in the two slots.)
 template <typename T> struct RowTerms {
     bf16x8 a;
     // x and y finite: an infinity would meet itself in the second value
@@ -211,7 +212,8 @@ __device__ inline void store_row(const Span &s, const f32x16 *x, float by, int a
     }
 }
 
-// A value that all lanes of the wave share, in a scalar register: the address of a copy has to be there.
+// A value that all lanes of the wave share, in a scalar register: the address of a copy has to be
+// there.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ inline int64_t uniform(int64_t x)
 {
