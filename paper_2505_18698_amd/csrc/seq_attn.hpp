@@ -38,23 +38,21 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
         kt = kBegin<R> + max(1, (kv + BN - 1) / BN);
     };
     int64_t sum = 0, tiles = 0;
-    for (int s = tid; s < p.seqs.B; s += NTH) {
-        int rt, kt;
-        shape(s, rt, kt);
-        sum += (int64_t)rt * kt, tiles += rt;
+    if (p.seqs.B > NTH) {  // (fewer: the sums below are those of all)
+        for (int s = tid; s < p.seqs.B; s += NTH) {
+            int rt, kt;
+            shape(s, rt, kt);
+            sum += (int64_t)rt * kt, tiles += rt;
+        }
+        for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x), tiles += __shfl_xor(tiles, x);
+        if (lane == 0) sh[2 * wave] = sum, sh[2 * wave + 1] = tiles;
+        __syncthreads();
+        sum = tiles = 0;
+        for (int i = 0; i < W; ++i) sum += sh[2 * i], tiles += sh[2 * i + 1];
+        __syncthreads();
     }
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x), tiles += __shfl_xor(tiles, x);
-    if (lane == 0) sh[2 * wave] = sum, sh[2 * wave + 1] = tiles;
-    __syncthreads();
-    sum = tiles = 0;
-    for (int i = 0; i < W; ++i) sum += sh[2 * i], tiles += sh[2 * i + 1];
-    __syncthreads();
-    // (row starts that decrease can make more row tiles than there is room for: those are left out)
-    if (blockIdx.x == 0 && tid == 0) p.parts[0].seq = (int)min(tiles, (int64_t)p.tiles);
-    Line r{sum, (int)max((int64_t)1, min((int64_t)p.shares, sum / 4)), -1, 0, 0, 0};
-    if (share >= r.shares) return r;
-    const int64_t want = sum * share / r.shares;
-    int64_t steps_before = 0, tiles_before = 0;
+    Line r{0, 0, -1, 0, 0, 0};
+    int64_t want = 0, steps_before = 0, tiles_before = 0;
     for (int s0 = 0; s0 < p.seqs.B; s0 += NTH) {
         int rt, kt;
         shape(s0 + tid, rt, kt);
@@ -71,6 +69,15 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
             at += sh[2 * i], au += sh[2 * i + 1];
         }
         __syncthreads();
+        if (s0 == 0) {
+            if (p.seqs.B <= NTH) sum = au, tiles = at;
+            // (row starts that decrease can make more row tiles than there is room for: those are
+            // left out)
+            if (blockIdx.x == 0 && tid == 0) p.parts[0].count = (int)min(tiles, (int64_t)p.tiles);
+            r.all = sum, r.shares = (int)max((int64_t)1, min((int64_t)p.shares, sum / 4));
+            if (share >= r.shares) return r;
+            want = sum * share / r.shares;
+        }
         const int64_t u0 = steps_before + u - (int64_t)rt * kt, k = want - u0;
         const bool mine = k >= 0 && k < (int64_t)rt * kt;  // one thread at most
         if (mine) {
@@ -377,7 +384,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
                     const bool whole = from == begin && stop == begin + steps;
                     if (from == begin && kvh == 0 && tid == 0) {
                         const int last = share_of(begin + steps - 1, all, shares);
-                        p.parts[1 + index] = SeqTileParts{seq, tile, share, last - share + 1};
+                        p.parts[1 + index] = SeqTileParts{p.seqs.start(seq), tile * R, min(n * p.G - tile * R, R), share, last - share + 1, {}};
                     }
                     segment(p, lds, tid, lane, wave, kvh, seq, tile, (int)(from - begin), (int)(stop - from), !whole,
                             (int64_t)(share + index) * p.Hkv + kvh, max_keys);
@@ -554,14 +561,12 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
     constexpr int C = D / 32;  // columns a thread
     __shared__ float sh_o[8][D], sh_l[8];
     const int kvh = blockIdx.x % p.Hkv, tile = blockIdx.x / p.Hkv;
-    if (tile >= p.parts[0].seq) return;
     const SeqTileParts f = p.parts[1 + tile];
-    if (f.count == 1) return;
+    if (tile >= p.parts[0].count || f.count == 1) return;
     const int tid = threadIdx.x, g = tid / 32, c = tid % 32;
-    const int row0 = p.seqs.start(f.seq), rows = min(p.seqs.length(f.seq) * p.G - f.tile * R, R);
     if constexpr (R > 32) {
         const int r = blockIdx.y * 8 + g;
-        if (r >= rows) return;
+        if (r >= f.rows) return;
         const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY, sum = 0.f, o[C] = {};
         for (int x = 0; x < f.count; ++x) mx = max_nan(mx, p.part_l[base + x * each]);
@@ -574,8 +579,8 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
             for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);
         }
         const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-        const int at = f.tile * R + r, head = kvh * p.G + at % p.G;
-        const int64_t row = row0 + at / p.G;
+        const int at = f.at + r, head = kvh * p.G + at % p.G;
+        const int64_t row = f.row0 + at / p.G;
         T *out = (T *)p.out + (row * p.Hkv * p.G + head) * p.d + c * C;
 #pragma unroll
         for (int i = 0; i < C; ++i)
@@ -583,7 +588,7 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
         if (p.lse && c == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
         return;
     }
-    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    for (int r = blockIdx.y; r < f.rows; r += gridDim.y) {
         const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY;
         for (int x = c; x < f.count; x += 32) mx = max_nan(mx, p.part_l[base + x * each]);
@@ -608,8 +613,8 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
             float all = 0.f, y = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) all += sh_l[i], y += sh_o[i][tid];
-            const int at = f.tile * R + r;
-            const int64_t row = row0 + at / p.G;
+            const int at = f.at + r;
+            const int64_t row = f.row0 + at / p.G;
             const int head = kvh * p.G + at % p.G;
             if (tid < p.d) ((T *)p.out)[(row * p.Hkv * p.G + head) * p.d + tid] = to_elem<T>(mx == -INFINITY ? 0.f : y / all);
             if (p.lse && tid == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(all)) * kLn2;

@@ -38,10 +38,11 @@ struct SeqFwd {
     struct SeqTileParts *parts;
 };
 
-// parts[0].seq: how many row tiles there are; parts[1 + i]: tile i, and the
-// first and the number of the shares that have a segment of it.
+// parts[0].count: how many row tiles there are; parts[1 + i]: of tile i the sequence's first row, the
+// tile's first packed row and their number, and the first and the number of the shares that have a
+// segment of it.
 struct SeqTileParts {
-    int seq, tile, first, count;
+    int row0, at, rows, first, count, unused[3];
 };
 
 struct SeqBwd {
