@@ -554,7 +554,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGE
 // workgroup per row tile and key head, and, of tiles of many rows, 8 rows, 32 threads a row (they
 // have few segments); of 32-row tiles, `gridDim.y`-th of the rows, one at a time, 32 threads a
 // segment and 8 segments at once.  5 us for single tokens, 13 us for 2786 rows of 32 heads, of
-// which it reads 30 MB of segments.
+// which it reads 46 MB of segments.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
 {
