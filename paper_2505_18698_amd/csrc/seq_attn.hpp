@@ -504,10 +504,10 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
                 step<true>(lds + 2 * TILE * buf + part * 32 * S::ROW, vt + part * 32 * S::ROW, qf, vis, key0 + 32 * part, p.c,
                            p.rest != nullptr, st, lane);
         }
-        if constexpr (KW > 1) {
-            join_waves(lds, wave, lane, st);
-            if (wave >= WR) return;
-        }
+        if constexpr (KW > 1) join_waves(lds, wave, lane, st);
+        // (a row has one owner; the waves that only copied tiles, also where no wave shares the
+        // keys, would store what they do not have at the same place)
+        if (wave >= WR) return;
 
         const Span os((T *)p.out + ((row0 + tok0) * (int64_t)p.Hkv + kvh) * p.G * p.d);
         const float sum = wave_xor_sum<32>(st.sum);
