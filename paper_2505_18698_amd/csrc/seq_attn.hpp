@@ -384,7 +384,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
                     const bool whole = from == begin && stop == begin + steps;
                     if (from == begin && kvh == 0 && tid == 0) {
                         const int last = share_of(begin + steps - 1, all, shares);
-                        p.parts[1 + index] = SeqTileParts{p.seqs.start(seq), tile * R, min(n * p.G - tile * R, R), share, last - share + 1, {}};
+                        const int blind = kv == 0 ? n : p.causal ? max(0, n - kv) : 0;  // first tokens that see no key
+                        p.parts[1 + index] = SeqTileParts{p.seqs.start(seq), tile * R, min(n * p.G - tile * R, R), share, last - share + 1, blind * p.G, {}};
                     }
                     segment(p, lds, tid, lane, wave, kvh, seq, tile, (int)(from - begin), (int)(stop - from), !whole,
                             (int64_t)(share + index) * p.Hkv + kvh, max_keys);
@@ -518,7 +519,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         if (SPLIT && parts) {
             const int64_t first_row = unit * R + wr0 - r0;
             const Span ps(p.part_o + first_row * D);
-            store_row<float, S::ND>(ps, st.o, inv, (lane & 31) * D, D, real, lane);
+            // (scores of -infinity alone: a segment without a weight adds zeros to the row)
+            store_row<float, S::ND>(ps, st.o, sum == 0.f ? 0.f : inv, (lane & 31) * D, D, real, lane);
             if (real && lane < 32) p.part_l[first_row + lane] = l2;
             return;
         }
@@ -550,6 +552,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGE
     U::run(p, lds);
 }
 
+// Packed row `at` of a sequence if no segment has a weight of it: zero where it sees no key, else
+// 0 / 0.
+__device__ inline float without_weight(const SeqTileParts &f, int at) { return at < f.blind ? 0.f : NAN; }
+
 // The segments of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x). One
 // workgroup per row tile and key head, and, of tiles of many rows, 8 rows, 32 threads a row (they
 // have few segments); of 32-row tiles, `gridDim.y`-th of the rows, one at a time, 32 threads a
@@ -578,8 +584,9 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
 #pragma unroll
             for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);
         }
-        const float inv = mx == -INFINITY ? 0.f : 1.f / sum;
-        const int at = f.at + r, head = kvh * p.G + at % p.G;
+        const int at = f.at + r;
+        const float inv = mx == -INFINITY ? without_weight(f, at) : 1.f / sum;
+        const int head = kvh * p.G + at % p.G;
         const int64_t row = f.row0 + at / p.G;
         T *out = (T *)p.out + (row * p.Hkv * p.G + head) * p.d + c * C;
 #pragma unroll
@@ -616,7 +623,7 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
             const int at = f.at + r;
             const int64_t row = f.row0 + at / p.G;
             const int head = kvh * p.G + at % p.G;
-            if (tid < p.d) ((T *)p.out)[(row * p.Hkv * p.G + head) * p.d + tid] = to_elem<T>(mx == -INFINITY ? 0.f : y / all);
+            if (tid < p.d) ((T *)p.out)[(row * p.Hkv * p.G + head) * p.d + tid] = to_elem<T>(mx == -INFINITY ? without_weight(f, at) : y / all);
             if (p.lse && tid == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(all)) * kLn2;
         }
         __syncthreads();

@@ -39,10 +39,10 @@ struct SeqFwd {
 };
 
 // parts[0].count: how many row tiles there are; parts[1 + i]: of tile i the sequence's first row, the
-// tile's first packed row and their number, and the first and the number of the shares that have a
-// segment of it.
+// tile's first packed row and their number, the first and the number of the shares that have a
+// segment of it, and how many first packed rows of the sequence see no key.
 struct SeqTileParts {
-    int row0, at, rows, first, count, unused[3];
+    int row0, at, rows, first, count, blind, unused[2];
 };
 
 struct SeqBwd {
