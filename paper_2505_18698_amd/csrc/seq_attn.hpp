@@ -139,6 +139,11 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     // that has grown by more than 2^kSlack: the sums stay exact to fp32 (weights up to 2^kSlack),
     // and the output is rescaled a few times a row instead of once a tile.
     static constexpr float kSlack = 8.f;
+    // fp16 holds 2^-24 to 65504: there all weights are taken times 2^kShift, up to 2^15, so that those
+    // that become zero are below 2^-32 of the reference's (many keys below 2^-25 beside a large one
+    // count in a long context: 2^17 of them were 0.4 % of the row).  The factor is in the sum too, and
+    // leaves with it.
+    static constexpr float kShift = std::is_same<T, _Float16>::value ? 7.f : 0.f;
 
     struct State {
         f32x16 o[S::ND];  // O^T: lane 32 h + c, row c, columns 32 dt + kRow32(r) + 4 h
@@ -193,7 +198,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
 #pragma unroll
             for (int dt = 0; dt < S::ND; ++dt) st.o[dt] *= by;
         }
-        const float ref = st.ref == -INFINITY ? 0.f : st.ref;
+        const float ref = (st.ref == -INFINITY ? 0.f : st.ref) - kShift;
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < KT; ++t) {
@@ -514,7 +519,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         const float sum = wave_xor_sum<32>(st.sum);
         const bool none = vis <= first;  // no key to see
         const float inv = none ? 0.f : 1.f / sum;
-        const float l2 = none ? -INFINITY : st.ref + __builtin_amdgcn_logf(sum);
+        const float l2 = none ? -INFINITY : st.ref + (__builtin_amdgcn_logf(sum) - kShift);
         const bool real = row < rows;
         if (SPLIT && parts) {
             const int64_t first_row = unit * R + wr0 - r0;

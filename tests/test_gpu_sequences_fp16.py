@@ -1,0 +1,40 @@
+"""fp16: weights and gradients far below the largest one."""
+import math
+
+import pytest
+import torch
+
+from sequence_reference import attention, starts, worst
+from test_gpu_sequences import _inputs, _run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ma():
+    assert torch.cuda.is_available(), "no GPU visible"
+    import paper_2505_18698_amd as lib
+
+    return lib
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_small_weights_beside_a_large_one(ma, causal):
+    """The first key has the weight 1, and each of the n = 2^17 - 1 others 2^-25.1, less than half of fp16's smallest
+    number: together they are 0.36 % of the row.
+
+    With |V| = 1 and A the sum of the weights, 1, the row may be off by 2^-11 for its own rounding, 2^-11 for the
+    weights', and the fp32 sums: the products add 16 keys at a time, n / 16 roundings of 2^-24, the weights' sum fewer,
+    and a score's 68 roundings of 2^-24 |s| shift its weight (17.4 = 25.1 ln 2)."""
+    n, d, rows = 1 << 17, 64, slice(-8, None)
+    q, k, v = (torch.zeros(n, 1, d, device="cuda") for _ in range(3))
+    q[..., 0], k[0, 0, 0] = 16.0, 25.1 * math.log(2.0) / 2  # s q.k = 2 k
+    v[:] = torch.where(torch.arange(d, device="cuda") % 3 == 0, -1.0, 1.0)
+    q, k, v = q.half(), k.half(), v.half()
+    out, lse = torch.zeros_like(q), torch.zeros(1, n, device="cuda")
+    ma.monarch_attn_exact_packed_fwd(q, k, v, out, starts([n], "cuda"), causal, lse)
+    torch.cuda.synchronize()
+    ref = attention(q[rows], k, v, causal, n - 8)
+    bound = 2 * 2.0 ** -11 + (n / 16 + 68 * 17.5) * 2.0 ** -24
+    assert float((out[rows].double() - ref["out"][0]).abs().max()) <= bound < 0.0017
+    assert worst(lse[:, rows], *ref["lse"]) <= 1.0
