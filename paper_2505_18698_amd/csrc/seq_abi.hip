@@ -171,10 +171,14 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     return run_launches(stream, FwdLaunch::run, &x);
 }
 
-// Workspace of the gradient: lse in log2 units and delta of every row and head,
-// and the largest norms of the workgroups that form them.
-constexpr int kNormBlocks = 1024;
-size_t bwd_bytes(int64_t total, int64_t Hq) { return 2 * align_up((size_t)(Hq * total) * 4) + align_up(kNormBlocks * sizeof(float2)); }
+// Workspace of the gradient: lse in log2 units and delta of every row and head; in fp16 also the
+// norms of the rows of dout and v.
+constexpr int kStatBlocks = 1024;
+size_t stat_bytes_of(int64_t total, int64_t heads) { return align_up((size_t)(heads * total) * 4); }
+size_t bwd_bytes(int64_t total, int64_t Hq, int64_t Hkv, int32_t dtype)
+{
+    return (dtype == MA_F16 ? 3 : 2) * stat_bytes_of(total, Hq) + (dtype == MA_F16 ? stat_bytes_of(total, Hkv) : 0);
+}
 
 // Pieces that the query rows of a key tile are cut into.  The longest walk, of the first keys of
 // one causal sequence that fills the call, is twice the mean one, so 1024 key tiles and heads (two
@@ -217,7 +221,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     CallScope c;
     MA_TRY(begin_call(c));
     const int64_t pieces = bwd_pieces(tiles_k, Hkv, G, c.num_cus);
-    const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq);
+    const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq, Hkv, dtype);
     MA_TRY(check_grid(tiles_k * pieces + tiles_q, Hkv));
     MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
     BwdLaunch x{};
@@ -229,9 +233,10 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
     p.c = log2_scale(d), p.causal = causal != 0, p.clear = clear != 0;
     p.tiles_q = (int)tiles_q, p.tiles_k = (int)tiles_k;
-    const size_t each = align_up((size_t)(Hq * total) * 4);
-    p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each), p.norms = (float2 *)(c.ws + 2 * each);
-    p.norm_blocks = (int)std::min<int64_t>(kNormBlocks, (total + 15) / 16 * Hq);
+    const size_t each = stat_bytes_of(total, Hq);
+    p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each);
+    if (dtype == MA_F16) p.norm_g = (float *)(c.ws + 2 * each), p.norm_v = (float *)(c.ws + 3 * each);
+    p.stat_blocks = (int)std::min<int64_t>(kStatBlocks, (total + 15) / 16 * Hq);
     p.pieces = (int)pieces;
     p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;

@@ -26,36 +26,57 @@ namespace ma {
 
 // fp16 holds 2^-24 to 65504, and dS is as small as the upstream gradient times
 // a weight: dS is formed times a power of two under which its largest possible
-// value, 2 max|dO_i| max|v_j|, is just below 2^15, and P times 2^14.  Both are
-// taken out of the fp32 sums.  bf16 and fp32 have the range themselves.
+// value, 2 |dO_i| max|v_j| over the keys that row i sees, is just below 2^15, and P times 2^14.
+// Both are taken out of the fp32 sums.  dQ, whose sums are those of a row, has a power of two a row;
+// dK and dV one for the rows that a workgroup walks.  So what a sequence's gradient is depends
+// on no other one's.  bf16 and fp32 have the range themselves.
 template <typename T> struct BwdScale {
     static constexpr bool kScaled = std::is_same<T, _Float16>::value;
     static constexpr float kP = kScaled ? 14.f : 0.f;  // log2
-    float ds = 1.f;                                    // of dS
-    template <int NTH> __device__ void find(const SeqBwd &p, char *lds)
+
+    // The largest of the norms of `count` rows and `heads` heads from `at` on that this thread of
+    // NTH reads: 4 bytes for the 4 D of a row that the walk reads, eight loads on their way at a time.
+    // (9550 rows of 7 sequences, 16 heads on 4 of 128: 470 us for 460 with the largest norms of the
+    // whole call, one sequence of 16384: 2.21 ms for 2.16.)
+    template <int NTH> __device__ static float own_largest(const float *at, int count, int heads, int64_t stride)
     {
-        if constexpr (kScaled) {
-            float a = 0.f, b = 0.f;
-            for (int i = threadIdx.x; i < p.norm_blocks; i += NTH) {
-                const float2 x = p.norms[i];
-                a = fmaxf(a, x.x), b = fmaxf(b, x.y);
+        float a = 0.f;
+        const uint32_t all = (uint32_t)count * (uint32_t)heads;  // (below 2^31)
+        for (uint32_t i = threadIdx.x; i < all; i += 8 * NTH) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const uint32_t j = min(i + u * NTH, all - 1), head = heads == 1 ? 0 : j / (uint32_t)count;
+                x[u] = at[head * stride + (j - head * (uint32_t)count)];
             }
-            for (int x = 1; x < 64; x <<= 1) a = fmaxf(a, __shfl_xor(a, x)), b = fmaxf(b, __shfl_xor(b, x));
-            float *sh = reinterpret_cast<float *>(lds);
-            if (threadIdx.x % 64 == 0) sh[threadIdx.x / 32] = a, sh[threadIdx.x / 32 + 1] = b;
-            __syncthreads();
-            for (int i = 0; i < NTH / 64; ++i) a = fmaxf(a, sh[2 * i]), b = fmaxf(b, sh[2 * i + 1]);
-            __syncthreads();
-            const float most = 2.f * sqrtf(a) * sqrtf(b);
-            const int e = most > 0.f ? 14 - ilogbf(most) : 0;
-            ds = uniform_float(ldexpf(1.f, max(-60, min(e, 60))));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) a = fmaxf(a, x[u]);
         }
+        return a;
     }
-    __device__ static float uniform_float(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+    // The largest a and b of the workgroup.
+    template <int NTH> __device__ static void all_largest(float &a, float &b, char *lds)
+    {
+        for (int x = 1; x < 64; x <<= 1) a = fmaxf(a, __shfl_xor(a, x)), b = fmaxf(b, __shfl_xor(b, x));
+        float *sh = reinterpret_cast<float *>(lds);
+        if (threadIdx.x % 64 == 0) sh[threadIdx.x / 32] = a, sh[threadIdx.x / 32 + 1] = b;
+        __syncthreads();
+        for (int i = 0; i < NTH / 64; ++i) a = fmaxf(a, sh[2 * i]), b = fmaxf(b, sh[2 * i + 1]);
+        __syncthreads();
+        a = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(a)));
+        b = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(b)));
+    }
+    // The power of two for rows of dO and v of at most these norms.
+    __device__ static float of(float norm_g, float norm_v)
+    {
+        const float most = 2.f * sqrtf(norm_g) * sqrtf(norm_v);
+        const int e = most > 0.f ? 14 - ilogbf(most) : 0;
+        return ldexpf(1.f, max(-60, min(e, 60)));
+    }
 };
 
 // delta and lse in log2 units of every (row, head), 16 lanes a row; in fp16 also
-// the largest norms.  A workgroup takes one head of 16 rows at a time, whose lse, delta
+// the norms of dO and v.  A workgroup takes one head of 16 rows at a time, whose lse, delta
 // and lse2 are then 64 bytes together.
 template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
 {
@@ -67,7 +88,6 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
         clear_outside<256>(p.seqs, p.dv, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
     }
     const int first = p.seqs.start(0), last = p.seqs.start(p.seqs.B);  // (rows of no sequence count for nothing)
-    float most_g = 0.f, most_v = 0.f;
 #pragma unroll 2
     for (int64_t u = blockIdx.x; u < ((int64_t)last - first + 15) / 16 * Hq; u += gridDim.x) {
         const int head = (int)(u % Hq), row = first + (int)(u / Hq) * 16 + (int)(threadIdx.x >> 4);
@@ -99,14 +119,15 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
             const int64_t at = (int64_t)head * p.seqs.total + row;
             p.delta[at] = sum;
             p.lse2[at] = p.lse[at] * kLog2e;
+            if constexpr (BwdScale<T>::kScaled) p.norm_g[at] = norm < INFINITY ? norm : 0.f;
         }
-        if (norm < INFINITY) most_g = fmaxf(most_g, norm);
     }
     if constexpr (BwdScale<T>::kScaled) {
-        const int64_t step = (int64_t)gridDim.x * 16, own = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-        for (int64_t i = (int64_t)first * p.Hkv + own; i < (int64_t)last * p.Hkv; i += step) {
+        for (int64_t u = blockIdx.x; u < ((int64_t)last - first + 15) / 16 * p.Hkv; u += gridDim.x) {
+            const int head = (int)(u % p.Hkv), row = first + (int)(u / p.Hkv) * 16 + (int)(threadIdx.x >> 4);
+            if (row >= last) continue;
             float norm = 0.f;
-            const T *v = (const T *)p.v + i / p.Hkv * p.ldv + i % p.Hkv * p.d;
+            const T *v = (const T *)p.v + row * p.ldv + head * p.d;
             for (int col = lane * V; col < p.d; col += 16 * V) {
                 T a[V];
                 __builtin_memcpy(a, v + col, 16);
@@ -115,15 +136,8 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
             }
 #pragma unroll
             for (int x = 1; x < 16; x <<= 1) norm += __shfl_xor(norm, x);
-            if (norm < INFINITY) most_v = fmaxf(most_v, norm);
+            if (lane == 0) p.norm_v[(int64_t)head * p.seqs.total + row] = norm < INFINITY ? norm : 0.f;
         }
-        __shared__ float sh[2][4];
-        for (int x = 16; x < 64; x <<= 1) most_g = fmaxf(most_g, __shfl_xor(most_g, x)), most_v = fmaxf(most_v, __shfl_xor(most_v, x));
-        if (threadIdx.x % 64 == 0) sh[0][threadIdx.x / 64] = most_g, sh[1][threadIdx.x / 64] = most_v;
-        __syncthreads();
-        if (threadIdx.x == 0)
-            p.norms[blockIdx.x] = float2{fmaxf(fmaxf(sh[0][0], sh[0][1]), fmaxf(sh[0][2], sh[0][3])),
-                                         fmaxf(fmaxf(sh[1][0], sh[1][1]), fmaxf(sh[1][2], sh[1][3]))};
     }
 }
 
@@ -195,8 +209,6 @@ template <typename T, int D> struct SeqBwdQ {
     __device__ static void run(const SeqBwd &p, char *lds, int block)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-        BwdScale<T> sc;
-        sc.template find<NTH>(p, lds);
         const int kvh = uniform(block % p.Hkv);
         const int64_t t = p.tiles_q - 1 - block / p.Hkv;  // later rows see more keys: they start first
         const int seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
@@ -223,6 +235,12 @@ template <typename T, int D> struct SeqBwdQ {
         }
         const int64_t at = (int64_t)head * p.seqs.total + row0 + tok0 + tok;
         const float lse2 = p.lse2[at], delta = p.delta[at];
+        float scale = 1.f;  // of this row's dS
+        if constexpr (BwdScale<T>::kScaled) {
+            float most = BwdScale<T>::template own_largest<NTH>(p.norm_v + (int64_t)kvh * p.seqs.total + row0, last, 1, 0), none = 0.f;
+            BwdScale<T>::template all_largest<NTH>(most, none, lds);
+            scale = BwdScale<T>::of(p.norm_g[at], most);
+        }
 
         const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
         const T *k = (const T *)p.k + row0 * p.ldk + kvh * p.d, *v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
@@ -245,7 +263,7 @@ template <typename T, int D> struct SeqBwdQ {
         auto unmasked = [&](int b) {
             tile_barrier();
             bring(key0 + BN, b ^ 1);
-            step<false>(lds + 2 * TILE * b + part * S::ROW, lds + 2 * TILE * b + TILE + part * S::ROW, qf, gf, 0, p.c, lse2, delta, sc.ds, dq, lane);
+            step<false>(lds + 2 * TILE * b + part * S::ROW, lds + 2 * TILE * b + TILE + part * S::ROW, qf, gf, 0, p.c, lse2, delta, scale, dq, lane);
             key0 += BN, buf = b ^ 1;
         };
 #pragma unroll 1
@@ -259,7 +277,7 @@ template <typename T, int D> struct SeqBwdQ {
             bring(key0 + BN, buf ^ 1);
             if (key0 + part < see_most)
                 step<true>(lds + 2 * TILE * buf + part * S::ROW, lds + 2 * TILE * buf + TILE + part * S::ROW, qf, gf,
-                           vis - key0 - part - 4 * (lane >> 5), p.c, lse2, delta, sc.ds, dq, lane);
+                           vis - key0 - part - 4 * (lane >> 5), p.c, lse2, delta, scale, dq, lane);
         }
         if constexpr (KW > 1) {  // the waves' sums over their keys, into the first ones'
             static_assert((KW - 1) * WR * S::ND * 16 * 256 <= LDS_BYTES, "the tiles' room holds them");
@@ -276,7 +294,7 @@ template <typename T, int D> struct SeqBwdQ {
                 for (int i = 0; i < S::ND * 16; ++i) dq[i / 16][i % 16] += sh[(((w - 1) * WR + wave) * S::ND * 16 + i) * 64];
         }
         const Span os((T *)p.dq + (int64_t)(row0 + tok0) * Hq * p.d);
-        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / sc.ds, (tok * Hq + head) * p.d, p.d, wr0 + (lane & 31) < rows, lane);
+        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / scale, (tok * Hq + head) * p.d, p.d, wr0 + (lane & 31) < rows, lane);
     }
 };
 
@@ -412,8 +430,6 @@ template <typename T, int D> struct SeqBwdK {
     __device__ static void run(const SeqBwd &p, char *lds, int block)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kb = wave % NK, qb = wave / NK;
-        BwdScale<T> sc;
-        sc.template find<NTH>(p, lds);
         const int kvh = uniform(block % p.Hkv);
         const int64_t t = block / p.Hkv / p.pieces;  // (earlier keys are seen by more rows: they start first)
         const int piece = uniform(block / p.Hkv % p.pieces);
@@ -421,6 +437,15 @@ template <typename T, int D> struct SeqBwdK {
         if (seq < 0) return;
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
         const int k0 = uniform((int)(t - tile0(p.seqs, seq, 1, R)) * R), Hq = p.Hkv * p.G;
+        const int from = p.causal ? k0 : 0;  // the first row that sees a key of this workgroup
+        float ds = 1.f;                      // the power of two of dS
+        if constexpr (BwdScale<T>::kScaled) {
+            const float *g = p.norm_g + (int64_t)kvh * p.G * p.seqs.total + row0 + from, *v = p.norm_v + (int64_t)kvh * p.seqs.total + row0;
+            float most_g = BwdScale<T>::template own_largest<NTH>(g, n - from, p.G, p.seqs.total);
+            float most_v = BwdScale<T>::template own_largest<NTH>(v, n, 1, 0);
+            BwdScale<T>::template all_largest<NTH>(most_g, most_v, lds);
+            ds = BwdScale<T>::of(most_g, most_v);
+        }
 
         const Span ks((const T *)p.k + (row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d);
         const int ldv = (int)p.ldv * (int)sizeof(T), kc = min(32 * kb + (lane & 31), n - 1 - k0);
@@ -446,9 +471,8 @@ template <typename T, int D> struct SeqBwdK {
         Copy cq, cg;
         cq.init(ldq, p.d, wave, lane);
         cg.init(ldg, p.d, wave, lane);
-        // The walk: every head's tiles from the first row that sees a key of this workgroup on,
-        // this piece's share of them.
-        const int from = p.causal ? k0 : 0, tiles = (n - from + BQ - 1) / BQ;
+        // The walk: every head's tiles from row `from` on, this piece's share of them.
+        const int tiles = (n - from + BQ - 1) / BQ;
         const int begin = uniform((int)((int64_t)p.G * tiles * piece / p.pieces)), end = uniform((int)((int64_t)p.G * tiles * (piece + 1) / p.pieces));
         float lse2 = 0.f, delta = 0.f;  // of this lane's row of the tile that is copied
         auto bring = [&](int i, int g, int q0, int buf) {  // tile i of the walk, at row q0 of head g or the next one's first
@@ -469,7 +493,7 @@ template <typename T, int D> struct SeqBwdK {
         Grads x;
 #pragma unroll
         for (int dt = 0; dt < S::ND; ++dt) x.dk[dt] = x.dv[dt] = f32x16{};
-        const float scale = BwdScale<T>::kScaled ? sc.ds * 0x1p-14f : 1.f;
+        const float scale = BwdScale<T>::kScaled ? ds * 0x1p-14f : 1.f;
         int buf = 0, i = begin, g = begin / tiles;
         int q0 = from + (begin - g * tiles) * BQ;
         bring(i, g, q0, 0);
@@ -495,7 +519,7 @@ template <typename T, int D> struct SeqBwdK {
                     step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, terms, kf, vf, vrows, 0, 0, p.c, scale, x, lane);
             }
         }
-        const float by_k = n == 1 ? 0.f : p.c * kLn2 / sc.ds, by_v = BwdScale<T>::kScaled ? 0x1p-14f : 1.f;
+        const float by_k = n == 1 ? 0.f : p.c * kLn2 / ds, by_v = BwdScale<T>::kScaled ? 0x1p-14f : 1.f;
         if (p.pieces > 1) {
             const int64_t at = (((int64_t)piece * p.seqs.total + row0 + k0) * p.Hkv + kvh) * D;
             add_up<float>(lds, x.dk, Span(p.part_k + at), by_k, p.Hkv * D, D, n - k0, wave, lane);

@@ -12,7 +12,7 @@ template <typename T, int D> int run_seq_bwd_d(Launcher &L, const ma::SeqBwd &p)
 {
     const dim3 block(256);
     int rc = L.run(kSeqStats, [&] {
-        return launched([&] { ma::seq_stats<T><<<dim3((unsigned)p.norm_blocks), block, 0, L.stream>>>(p); });
+        return launched([&] { ma::seq_stats<T><<<dim3((unsigned)p.stat_blocks), block, 0, L.stream>>>(p); });
     });
     if (rc != MA_OK) return rc;
     const int blocks_q = (int)((int64_t)p.tiles_q * p.Hkv), blocks_k = (int)((int64_t)p.tiles_k * p.pieces * p.Hkv);

@@ -58,8 +58,8 @@ struct SeqBwd {
     int clear;                           // write zeros in the gradients' rows of no sequence
     int tiles_q, tiles_k;                // row and key tiles of one key head (upper bounds)
     float *lse2, *delta;                 // [Hq, total]: lse in log2 units, delta
-    float2 *norms;                       // fp16: the largest |dO_i|^2 and |v_j|^2 of every workgroup of seq_stats
-    int norm_blocks;
+    float *norm_g, *norm_v;              // fp16: |dO_i|^2 [Hq, total] and |v_j|^2 [Hkv, total], 0 where not finite
+    int stat_blocks;                     // workgroups of the row statistics
     // pieces that the query rows of a key tile are cut into; with more than one, their sums:
     // dK and dV of every piece, row and key head, in rows of the tile width
     int pieces;

@@ -38,3 +38,32 @@ def test_many_small_weights_beside_a_large_one(ma, causal):
     bound = 2 * 2.0 ** -11 + (n / 16 + 68 * 17.5) * 2.0 ** -24
     assert float((out[rows].double() - ref["out"][0]).abs().max()) <= bound < 0.0017
     assert worst(lse[:, rows], *ref["lse"]) <= 1.0
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("small", [0, 1])
+def test_gradients_of_sequences_of_different_scales(ma, small, causal):
+    """One sequence's upstream gradient is 2^23 times the other's: each gradient is as exact as alone, and its bits do
+    not depend on the other sequence."""
+    q, k, v, dout, cu = _inputs([500, 450], 4, 2, 64, "f16", 51, spare=0, first=0)
+    seqs = slice(0, 500), slice(500, 950)
+    x = dout.clone()
+    x[seqs[small]] *= 2.0 ** -10
+    alone = _run(ma, q, k, v, x, cu, causal)
+    x[seqs[1 - small]] *= 2.0 ** 12
+    r = _run(ma, q, k, v, x, cu, causal)
+    for i, rows in enumerate(seqs):
+        ref = attention(q[rows], k[rows], v[rows], causal, 0, x[rows])
+        for name in ("dq", "dk", "dv"):
+            assert worst(r[name][rows], *ref[name]) <= 1.0, (i, name)
+            assert i != small or torch.equal(r[name][rows], alone[name][rows]), name
+
+
+def test_gradients_of_rows_of_different_scales(ma):
+    """Rows of one sequence whose upstream gradients differ by 2^24: dQ is exact row by row.  (dK and dV sum over the
+    rows, relative to the largest.)"""
+    q, k, v, dout, cu = _inputs([700], 2, 1, 96, "f16", 52, spare=0, first=0)
+    x = dout.clone()
+    x[::2] *= 2.0 ** 12
+    x[1::2] *= 2.0 ** -12
+    assert worst(_run(ma, q, k, v, x, cu, True)["dq"], *attention(q, k, v, True, 0, x)["dq"]) <= 1.0
