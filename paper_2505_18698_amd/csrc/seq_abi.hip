@@ -180,16 +180,22 @@ size_t bwd_bytes(int64_t total, int64_t Hq, int64_t Hkv, int32_t dtype)
     return (dtype == MA_F16 ? 3 : 2) * stat_bytes_of(total, Hq) + (dtype == MA_F16 ? stat_bytes_of(total, Hkv) : 0);
 }
 
-// Pieces that the query rows of a key tile are cut into.  The longest walk, of the first keys of
-// one causal sequence that fills the call, is twice the mean one, so 1024 key tiles and heads (two
-// rounds of two workgroups on 256 compute units) end with it; the pieces make it half of the mean
-// work of a compute unit's slot.  A piece of fewer than 8 tiles is not worth its sums' way through
-// memory, nor are more than three pieces (9550 rows, 16 heads on 4 of 128, with the forward: 608
-// us; 614 with two or four).
-int64_t bwd_pieces(int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
+// Pieces that the query rows of a key tile are cut into, all those of a call alike.  The longest
+// walk, of the first keys of one causal sequence that fills the call, is twice the mean one, so 1024
+// key tiles and heads (two rounds of two workgroups on 256 compute units) end with it; the pieces
+// make it half of the mean work of a compute unit's slot.  More than three are not worth their sums'
+// way through memory (9550 rows, 16 heads on 4 of 128, with the forward: 608 us; 614 with two or
+// four), nor are any where even one sequence of all the call's rows would be a walk of fewer than 16
+// tiles (dQ, dK, dV and the sums of 64 sequences of 10, 4 heads of 64: 9 us, 16 with three pieces).
+//
+// The host knows the rows and not the lengths. So short sequences that are many pay for the pieces
+// that one long one among them would need: 6 of 1 to 1000 tokens, 12 heads of 64 in fp32, take 95 us
+// with three pieces and 112 with one, but 64 of 100, 16 heads on 4 of 128, 87 and 63 us.
+int64_t bwd_pieces(int64_t total, int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
 {
     const int64_t want = (8 * num_cus + tiles_k * Hkv - 1) / (tiles_k * Hkv);
-    return std::max<int64_t>(1, std::min<int64_t>({want, 3, G * tiles_k / 8}));
+    const int64_t longest = G * ((total + kSeqBwdKeys - 1) / kSeqBwdKeys);
+    return std::max<int64_t>(1, std::min<int64_t>({want, 3, longest / 8}));
 }
 
 int packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
@@ -220,7 +226,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
     MA_TRY(begin_call(c));
-    const int64_t pieces = bwd_pieces(tiles_k, Hkv, G, c.num_cus);
+    const int64_t pieces = bwd_pieces(total, tiles_k, Hkv, G, c.num_cus);
     const size_t part = pieces > 1 ? (size_t)(pieces * total * Hkv) * tile_d(d) * 4 : 0, stat_bytes = bwd_bytes(total, Hq, Hkv, dtype);
     MA_TRY(check_grid(tiles_k * pieces + tiles_q, Hkv));
     MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
