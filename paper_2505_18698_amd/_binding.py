@@ -420,6 +420,9 @@ PLAN_NO_PAGES, PLAN_TABLE_FULL, PLAN_BAD_LENGTH, PLAN_NO_SLOTS = 1, 2, 4, 8  # M
 PLAN_MAX_B = 8192  # MONARCH_ATTN_PLAN_MAX_B
 
 
+_MAX_ROW = 1 << 20  # elements between two rows, at most (MA_EUNSUPPORTED beyond)
+
+
 def _rows(t, dtype, device):
     """The row stride of t, [rows, heads, d] of that dtype on that device with
     the heads of a row adjacent, or -1 where it is nothing of the kind."""
@@ -556,7 +559,7 @@ def _packed_function():
         def rows(t):  # the kernels' layout: heads of a row adjacent, rows 16-byte aligned
             n = t.element_size()
             fits = t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.stride(0) * n % 16 == 0 \
-                and t.stride(0) >= t.shape[1] * t.shape[2] and t.data_ptr() % 16 == 0
+                and t.shape[1] * t.shape[2] <= t.stride(0) <= _MAX_ROW and t.data_ptr() % 16 == 0
             return t if fits else whole(t)
 
         class ExactAttentionPackedFn(torch.autograd.Function):

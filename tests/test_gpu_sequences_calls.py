@@ -32,3 +32,18 @@ def test_pieces_of_the_gradient(ma, lens, Hq, Hkv, d, join, causal, dtype):
     _check(r, *x, causal)
     again = _run(ma, *x, causal)
     assert all(torch.equal(r[n], again[n]) for n in r)
+
+
+def test_rows_far_apart_are_copied(ma):
+    """The torch op takes rows further apart than the kernels do."""
+    q, k, v, dout, cu = _inputs([30, 9], 4, 2, 64, "bf16", 62, spare=0, first=0)
+    want = _run(ma, q, k, v, dout, cu, True)
+    buf = torch.zeros(39, (1 << 20) + 8, device="cuda", dtype=torch.bfloat16)
+    leaves = []
+    for i, t in enumerate((q, k, v)):
+        far = buf[:, 256 * i : 256 * i + t.shape[1] * 64].unflatten(1, (-1, 64))
+        leaves.append(far.copy_(t).detach().requires_grad_())
+    out = ma.exact_attention_packed(*leaves, cu)
+    assert torch.equal(out, want["out"])
+    for g, n in zip(torch.autograd.grad(out, leaves, dout), ("dq", "dk", "dv")):
+        assert torch.equal(g, want[n]), n
