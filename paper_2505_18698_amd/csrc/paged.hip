@@ -15,8 +15,7 @@ int run_paged_plan(Launcher &L, const ma::PagedPlan &p)
 
 int run_paged_write(Launcher &L, const ma::PagedWrite &p)
 {
-    // about four 16-byte chunks of K and of V a thread
-    const int chunks = p.Hkv * p.d * p.size / 16, per = std::max(1, 1024 / chunks);
+    const int per = paged_write_rows(p.Hkv * p.d * p.size / 16);
     const unsigned blocks = (unsigned)(((int64_t)p.rows + per - 1) / per);
     return L.run(kPagedWrite, [&] { return launched([&] { ma::paged_write<<<dim3(blocks), dim3(256), 0, L.stream>>>(p, per); }); });
 }

@@ -88,9 +88,10 @@ int check_stride(const char *name, int64_t ld, int64_t width, int32_t dtype)
 // any.
 int64_t tiles_of(int64_t total, int64_t rows_a_token, int64_t B, int64_t R) { return std::max<int64_t>(1, total * rows_a_token / R + B); }
 
+// (HIP launches fewer than 2^32 threads a dimension; every kernel here has kSeqThreads a workgroup.)
 int check_grid(int64_t units, int64_t Hkv)
 {
-    if (units > 0x7fffffff / Hkv) return fail(MA_EUNSUPPORTED, "too many tiles for one grid");
+    if (units > 0xffffffffll / kSeqThreads / Hkv) return fail(MA_EUNSUPPORTED, "too many tiles for one grid");
     return MA_OK;
 }
 
@@ -282,10 +283,12 @@ struct PagedSplit {
     size_t bytes_o, bytes_l, bytes_parts;
 };
 
+// Packed rows a workgroup takes.
+int paged_rows(int64_t total, int64_t B, int64_t G, int32_t dtype) { return total * G <= B * kSeqFewRows ? kSeqFewRows : seq_rows(dtype); }
+
 PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t max_keys, int64_t num_cus, int32_t dtype)
 {
-    const bool few = total * G <= B * kSeqFewRows;
-    PagedSplit s{few ? kSeqFewRows : seq_rows(dtype), false, 0, 0, 0, 0, 0};
+    PagedSplit s{paged_rows(total, B, G, dtype), false, 0, 0, 0, 0, 0};
     s.tiles = s.units = tiles_of(total, G, B, s.rows);
     const int64_t shares = std::max<int64_t>(1, 2 * num_cus / Hkv);
     if (s.tiles >= 16 * shares || max_keys * tile_d(d) * (int64_t)elem_bytes(dtype) <= kWholeBytes) return s;
@@ -307,7 +310,7 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     MA_TRY(check_pages(pages, page));
     if (blocks < 0 || blocks > 0x7fffffff) return fail(MA_EINVAL, "blocks must be in 0..2^31 - 1");
     const int64_t G = Hq / Hkv;
-    MA_TRY(check_grid(tiles_of(total, G, B, kSeqFewRows), Hkv));
+    MA_TRY(check_grid(tiles_of(total, G, B, paged_rows(total, B, G, dtype)), Hkv));
     if (B == 0 || total == 0) return MA_OK;
     const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
@@ -381,6 +384,8 @@ int paged_write(const void *k, const void *v, void *k_pages, void *v_pages, cons
     MA_TRY(check_stride("ldk", ldk, Hkv * d, dtype));
     MA_TRY(check_stride("ldv", ldv, Hkv * d, dtype));
     MA_TRY(check_pages(pages, page));
+    const int64_t per = paged_write_rows(Hkv * d * (int64_t)elem_bytes(dtype) / 16);
+    MA_TRY(check_grid((rows + per - 1) / per, 1));
     if (rows == 0 || pages == 0) return MA_OK;
     const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
     const Range ins[] = {{"k", k, span_bytes(rows, ldk, Hkv * d, dtype)}, {"v", v, span_bytes(rows, ldv, Hkv * d, dtype)},

@@ -48,8 +48,13 @@ struct SeqPlan {
 // packed rows a workgroup takes: usually, and where sequences have few
 template <typename T> constexpr int kSeqRows = sizeof(T) == 4 ? 64 : 128;
 constexpr int kSeqFewRows = 32;
+constexpr int kSeqThreads = 256;  // of a workgroup
 inline int seq_rows(int32_t dtype) { return dtype == MA_F32 ? kSeqRows<float> : kSeqRows<__bf16>; }
 constexpr int kSeqBwdKeys = 64;  // keys a workgroup takes in the gradient
+
+// rows of K and V that a workgroup writes into pages, of `chunks` times 16 bytes: about four chunks
+// of each a thread
+inline int paged_write_rows(int64_t chunks) { return (int)(chunks < 4 * kSeqThreads ? 4 * kSeqThreads / chunks : 1); }
 
 template <typename T> int run_seq_fwd(Launcher &L, const ma::SeqFwd &p, const SeqPlan &how);
 template <typename T> int run_seq_bwd(Launcher &L, const ma::SeqBwd &p);
