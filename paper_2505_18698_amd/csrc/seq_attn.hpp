@@ -250,7 +250,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     }
 
     // A value of V that is not finite meets weights of zero in the rows of a masked
-    // tile that do not see it, where the product would make it NaN.  So such
+    // tile that do not see it, where the product would make it NaN, and in the rows that do what
+    // `fine` adds to their weights, of either sign.  So such
     // values are looked for (`foreign`), added to the rows that see them, and then
     // taken for zero.
     __device__ static bool foreign(const char *vt)
@@ -504,7 +505,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         for (; key0 < last; next()) {
             arrive();
             char *vt = lds + 2 * TILE * buf + TILE;
-            if (p.causal && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 2 * STAGES * TILE)))
+            if ((p.causal || p.rest) && some_thread<NTH>(foreign(vt), reinterpret_cast<int *>(lds + 2 * STAGES * TILE)))
                 take_foreign(vt, vis, key0, wave < WR, st, lane);
             if (key0 + 32 * part < see_most && !idle)
                 step<true>(lds + 2 * TILE * buf + part * 32 * S::ROW, vt + part * 32 * S::ROW, qf, vis, key0 + 32 * part, p.c,

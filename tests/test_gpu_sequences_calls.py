@@ -1,4 +1,6 @@
 """How calls of packed sequences run."""
+import math
+
 import pytest
 import torch
 
@@ -47,3 +49,19 @@ def test_rows_far_apart_are_copied(ma):
     assert torch.equal(out, want["out"])
     for g, n in zip(torch.autograd.grad(out, leaves, dout), ("dq", "dk", "dv")):
         assert torch.equal(g, want[n]), n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_without_a_mask(ma, bad, dtype):
+    """Every weight is positive, so the column of the sequence becomes the value; nothing else changes."""
+    q, k, v, _, cu = _inputs([40, 130, 9], 4, 2, 64, dtype, 63, spare=0, first=0)
+    clean = _run(ma, q, k, v, None, cu, False)["out"]
+    for at, rows in ((10, slice(0, 40)), (45, slice(40, 170)), (168, slice(40, 170)), (175, slice(170, 179))):
+        keep = v[at].clone()
+        v[at, 1, 5] = bad
+        out = _run(ma, q, k, v, None, cu, False)["out"]
+        want = clean.clone()
+        want[rows, 2:, 5] = bad
+        assert torch.equal(out, want) if not math.isnan(bad) else torch.equal(out.nan_to_num(7.0), want.nan_to_num(7.0)), at
+        v[at] = keep
