@@ -294,7 +294,7 @@ PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t
     if (s.tiles >= 16 * shares || max_keys * tile_d(d) * (int64_t)elem_bytes(dtype) <= kWholeBytes) return s;
     s.split = true;
     s.units = shares;
-    const size_t rows = (size_t)(shares + s.tiles) * Hkv * s.rows;
+    const size_t rows = (size_t)(2 * shares) * Hkv * s.rows;  // two segments a share (find_share in seq_attn.hpp)
     s.bytes_o = align_up(rows * tile_d(d) * 4);
     s.bytes_l = align_up(rows * 4);
     s.bytes_parts = align_up((size_t)(s.tiles + 1) * sizeof(ma::SeqTileParts));

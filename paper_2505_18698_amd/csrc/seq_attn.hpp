@@ -15,8 +15,9 @@ namespace ma {
 // workgroup ends at the same time whatever the contexts are, and starts once.  A row tile counts
 // kBegin steps more than it has, for what its first copies, its rows and its masked key tiles take
 // (measured: 8 us to a step's 2 with 128 rows, 6 to 2.4 with 32; without, the workgroups of 8
-// chunks of up to 512 tokens ended between 153 and 257 us).  The segment of share w in row tile i
-// has the number w + i, as both only grow along the line.
+// chunks of up to 512 tokens ended between 153 and 257 us).  Of a share's segments only the first
+// and the last can be parts of a row tile, and go to the partial results: where the share is the row
+// tile's first one it is its last segment, number 2 w + 1 of share w, else its first, 2 w.
 template <int R> constexpr int kBegin = R > 32 ? 4 : 2;
 struct Line {
     int64_t all;       // steps
@@ -394,7 +395,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
                         p.parts[1 + index] = SeqTileParts{p.seqs.start(seq), tile * R, min(n * p.G - tile * R, R), share, last - share + 1, blind * p.G, {}};
                     }
                     segment(p, lds, tid, lane, wave, kvh, seq, tile, (int)(from - begin), (int)(stop - from), !whole,
-                            (int64_t)(share + index) * p.Hkv + kvh, max_keys);
+                            (int64_t)(2 * share + (from == begin)) * p.Hkv + kvh, max_keys);
                     __syncthreads();  // the tiles' room is used again
                 }
                 at += kBegin<R> + steps, x = at, ++tile, ++index;
@@ -576,16 +577,18 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
     const SeqTileParts f = p.parts[1 + tile];
     if (tile >= p.parts[0].count || f.count == 1) return;
     const int tid = threadIdx.x, g = tid / 32, c = tid % 32;
+    // row r of the tile in its segment x (numbers as in find_share)
+    const int64_t share = (int64_t)p.Hkv * R, base = 2 * f.first * share + kvh * R;
+    auto part_row = [&](int x, int r) { return base + (x == 0 ? share : 2 * x * share) + r; };
     if constexpr (R > 32) {
         const int r = blockIdx.y * 8 + g;
         if (r >= f.rows) return;
-        const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY, sum = 0.f, o[C] = {};
-        for (int x = 0; x < f.count; ++x) mx = max_nan(mx, p.part_l[base + x * each]);
+        for (int x = 0; x < f.count; ++x) mx = max_nan(mx, p.part_l[part_row(x, r)]);
         const float ref = mx == -INFINITY ? 0.f : mx;
         for (int x = 0; x < f.count; ++x) {
-            const float l = p.part_l[base + x * each], w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);
-            const float *src = p.part_o + (base + x * each) * D + c * C;
+            const float l = p.part_l[part_row(x, r)], w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);
+            const float *src = p.part_o + part_row(x, r) * D + c * C;
             sum += w;
 #pragma unroll
             for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);
@@ -602,18 +605,17 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
         return;
     }
     for (int r = blockIdx.y; r < f.rows; r += gridDim.y) {
-        const int64_t base = ((int64_t)(f.first + tile) * p.Hkv + kvh) * R + r, each = (int64_t)p.Hkv * R;
         float mx = -INFINITY;
-        for (int x = c; x < f.count; x += 32) mx = max_nan(mx, p.part_l[base + x * each]);
+        for (int x = c; x < f.count; x += 32) mx = max_nan(mx, p.part_l[part_row(x, r)]);
 #pragma unroll
         for (int x = 1; x < 32; x <<= 1) mx = max_nan(mx, __shfl_xor(mx, x));
         const float ref = mx == -INFINITY ? 0.f : mx;
         float sum = 0.f, o[C] = {};
 #pragma unroll 4
         for (int x = g; x < f.count; x += 8) {
-            const float l = p.part_l[base + x * each];
+            const float l = p.part_l[part_row(x, r)];
             const float w = l == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(l - ref);  // (a segment of which this row sees nothing is zero)
-            const float *src = p.part_o + (base + x * each) * D + c * C;
+            const float *src = p.part_o + part_row(x, r) * D + c * C;
             sum += w;
 #pragma unroll
             for (int i = 0; i < C; ++i) o[i] = __builtin_fmaf(w, src[i], o[i]);

@@ -3,7 +3,7 @@ and with many rows a sequence, in one launch and split over the keys."""
 import pytest
 import torch
 
-from sequence_reference import DTYPES, starts
+from sequence_reference import DTYPES, attention, starts, worst
 from test_gpu_paged import _attend, _cache, _check
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,20 @@ def test_each_kernel(ma, dtype, Hq, Hkv, d, rows, split):
     for _ in range(3):
         again = _attend(ma, q, kp, vp, cu, kv, table)
         assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+def test_workspace_of_a_split_call(ma):
+    """900 requests on 8 key heads: two segments of 32 rows a workgroup (17 MB), not one a request more (133 MB)."""
+    gen = torch.Generator(device="cuda").manual_seed(82)
+    seqs, kp, vp, table, kv = _cache([1] * 900, [1000 if i % 300 == 0 else i % 40 for i in range(900)], 8, 128, 16, "bf16", gen)
+    q = torch.randn(900, 32, 128, generator=gen, device="cuda").bfloat16()
+    cu = starts([1] * 900, "cuda")
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    ma.monarch_attn_release_workspace()
+    free = torch.cuda.mem_get_info()[0]
+    ma.monarch_attn_exact_paged_fwd(q, kp, vp, out, cu, kv, table)
+    torch.cuda.synchronize()
+    assert free - torch.cuda.mem_get_info()[0] < 40 << 20
+    for i in (0, 1, 39, 300, 623, 899):
+        assert worst(out[i : i + 1], *attention(q[i : i + 1], *seqs[i], True, len(seqs[i][0]) - 1)["out"]) <= 1.0, i
