@@ -477,8 +477,8 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  *               to no read: the rows that see a token on it become NaN.
  * Calls with long contexts (a table of more tokens a sequence than 128 KB of their keys, 512 tokens
  * of 128 columns in 16 bits) are split over the keys into equal shares, and joined by a second launch, from partial
- * results in the workspace (fp32, two row tiles of 32 to 128 packed rows for each of twice as many workgroups as
- * the device has compute units: 17 to 67 MB at 128 columns).
+ * results in the workspace (fp32, two row tiles of 32 to 128 packed rows for each of one or two workgroups a
+ * compute unit: 17 to 67 MB at 128 columns).
  */
 int monarch_attn_exact_paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out, float *lse,
                                  const int32_t *cu_seqlens, const int32_t *kv_lens, const int32_t *block_table,

@@ -1,6 +1,8 @@
 // Launches of the exact attention forward (included by seq_fwd_*.hip).
 #pragma once
 
+#include <algorithm>
+
 #include "seq_attn.hpp"
 #include "seq_host.hpp"
 
@@ -11,6 +13,10 @@ template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p,
     const dim3 grid((unsigned)(how.units * p.Hkv)), block(256);
     const bool few = how.rows == kSeqFewRows;
     constexpr int R = kSeqRows<T>, WR = R / 32;
+    constexpr int kLds = 160 << 10;
+    static_assert(std::min(2, kLds / ma::SeqAttn<T, D, 1, true, true>::LDS_BYTES) == seq_residents<T>(D, true) &&
+                      std::min(2, kLds / ma::SeqAttn<T, D, WR, true, true>::LDS_BYTES) == seq_residents<T>(D, false),
+                  "the shares of a split call are as many as the device holds");
     int rc = L.run(kSeqFwd, [&] {
         return launched([&] {
             if (!how.paged)

@@ -50,6 +50,10 @@ template <typename T> constexpr int kSeqRows = sizeof(T) == 4 ? 64 : 128;
 constexpr int kSeqFewRows = 32;
 constexpr int kSeqThreads = 256;  // of a workgroup
 inline int seq_rows(int32_t dtype) { return dtype == MA_F32 ? kSeqRows<float> : kSeqRows<__bf16>; }
+// Workgroups of the split kernel that a compute unit holds: one where its K and V tiles take more
+// than half of the LDS, 131 KB of 160 (fp32: few rows up to 64 columns, many rows past 64).
+template <typename T> constexpr int seq_residents(int64_t d, bool few) { return sizeof(T) == 4 && few == (d <= 64) ? 1 : 2; }
+inline int seq_residents(int32_t dtype, int64_t d, bool few) { return dtype == MA_F32 ? seq_residents<float>(d, few) : seq_residents<__bf16>(d, few); }
 constexpr int kSeqBwdKeys = 64;  // keys a workgroup takes in the gradient
 
 // rows of K and V that a workgroup writes into pages, of `chunks` times 16 bytes: about four chunks
