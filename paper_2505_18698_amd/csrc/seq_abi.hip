@@ -268,12 +268,15 @@ int log2_of(int64_t page)
 // How a paged call runs.  Sequences of few new rows (on average no more than 32 packed ones: single
 // tokens) take 32-row tiles, whose waves share the keys. The work is shared evenly by as many
 // workgroups as the device holds at a time (seq_residents; find_share in seq_attn.hpp), except
-// where the keys of the longest possible context take no more than kWholeBytes, or where there are
-// many times as many row tiles: then a row tile is a workgroup's. (64 single tokens over up to
+// where the keys of the longest possible context take no more than kWholeBytes, or where tiles of many
+// rows are 16 times as many: then a row tile is a workgroup's. (64 single tokens over up to
 // 8192: 103 us, in pieces of equal length 122, 128-row tiles 266; 8 chunks of up to 512 over up to
 // 16384, before the copies' addresses were found in lanes: 213 us, in pieces of equal length 241.
 // With two workgroups a compute unit that holds one: 64 tokens over up to 8192, fp32, 32 heads on 8
-// of 64, 292 us for 285; 2 chunks of 100 over 5000, fp32, 16 on 4 of 128, 131 us for 117.)
+// of 64, 292 us for 285; 2 chunks of 100 over 5000, fp32, 16 on 4 of 128, 131 us for 117. Many row
+// tiles, a tile a workgroup and in shares, heads of 128 in bf16: 128 chunks of 512 over 2000 to 4000,
+// 32 heads on 8: 3.0 and 4.7 ms; single tokens of 1100 requests over 300, the same heads: 440 and 289 us,
+// over 1000 and one over 100000: 2.29 and 0.85 ms; of 600 over 500, fp32, 16 heads of 64: 731 and 780 us.)
 //
 // kWholeBytes: one token over 500 and 1000, 4 heads of 64: 9 and 12 us whole, 14 split; 8 heads of
 // 128: 13 and 18 us whole, 15 split.
@@ -292,8 +295,9 @@ PagedSplit paged_split(int64_t total, int64_t B, int64_t G, int64_t Hkv, int64_t
 {
     PagedSplit s{paged_rows(total, B, G, dtype), false, 0, 0, 0, 0, 0};
     s.tiles = s.units = tiles_of(total, G, B, s.rows);
-    const int64_t shares = std::max<int64_t>(1, seq_residents(dtype, d, s.rows == kSeqFewRows) * num_cus / Hkv);
-    if (s.tiles >= 16 * shares || max_keys * tile_d(d) * (int64_t)elem_bytes(dtype) <= kWholeBytes) return s;
+    const bool few = s.rows == kSeqFewRows;
+    const int64_t shares = std::max<int64_t>(1, seq_residents(dtype, d, few) * num_cus / Hkv);
+    if ((!few && s.tiles >= 16 * shares) || max_keys * tile_d(d) * (int64_t)elem_bytes(dtype) <= kWholeBytes) return s;
     s.split = true;
     s.units = shares;
     const size_t rows = (size_t)(2 * shares) * Hkv * s.rows;  // two segments a share (find_share in seq_attn.hpp)

@@ -67,3 +67,18 @@ def test_workspace_of_a_split_call(ma):
     assert free - torch.cuda.mem_get_info()[0] < 40 << 20
     for i in (0, 1, 39, 300, 623, 899):
         assert worst(out[i : i + 1], *attention(q[i : i + 1], *seqs[i], True, len(seqs[i][0]) - 1)["out"]) <= 1.0, i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_long_context_among_many_short_ones(ma, dtype):
+    """However many single tokens there are, the work is shared evenly."""
+    gen = torch.Generator(device="cuda").manual_seed(83)
+    past = [9000 if i == 700 else i % 50 for i in range(1200)]
+    seqs, kp, vp, table, kv = _cache([1] * 1200, past, 8, 64, 16, dtype, gen)
+    q = torch.randn(1200, 16, 64, generator=gen, device="cuda").to(DTYPES[dtype])
+    got = []
+    launches = _launches(ma, lambda: got.extend(_attend(ma, q, kp, vp, starts([1] * 1200, "cuda"), kv, table)))
+    assert "seq_join" in launches
+    for i in (0, 1, 49, 699, 700, 701, 1199):
+        ref = attention(q[i : i + 1], *seqs[i], True, past[i])
+        assert worst(got[0][i : i + 1], *ref["out"]) <= 1.0 and worst(got[1][:, i : i + 1], *ref["lse"]) <= 1.0, i
