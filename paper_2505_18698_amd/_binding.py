@@ -663,7 +663,10 @@ def monarch_attn_paged_plan(past, fresh, ring, free_in, block_table, cu_seqlens,
     free_in = (first, count)) into block_table [B, blocks], row starts
     cu_seqlens [B + 1], kv_lens [B], the slot of every new token in slots
     (int64 [capacity], -1 behind the last), what stays free in free_out [2] and
-    0 or PLAN_* bits in status [1].  All int32 device tensors but slots."""
+    0 or PLAN_* bits in status [1].  All int32 device tensors but slots.
+
+    With bits in status a request did not fit and was cut: attention over these tables is meaningless for it, and
+    its kv_lens, which count tokens without a slot, are not the next step's past."""
     rt = _torch()
     int32 = rt.int32
     try:

@@ -14,8 +14,8 @@ namespace ma {
 // takes the steps from w all / shares on, in segments that lie in one row tile each.  So every
 // workgroup ends at the same time whatever the contexts are, and starts once.  A row tile counts
 // kBegin steps more than it has, for what its first copies, its rows and its masked key tiles take
-// (measured: 8 us to a step's 2 with 128 rows, 6 to 2.4 with 32; without, the workgroups of 8
-// chunks of up to 512 tokens ended between 153 and 257 us).  Of a share's segments only the first
+// (measured in bf16 at 128 columns and used for all: 8 us to a step's 2 with 128 rows, 6 to 2.4
+// with 32; without, the workgroups of 8 chunks of up to 512 tokens ended between 153 and 257 us).  Of a share's segments only the first
 // and the last can be parts of a row tile, and go to the partial results: where the share is the row
 // tile's first one it is its last segment, number 2 w + 1 of share w, else its first, 2 w.
 template <int R> constexpr int kBegin = R > 32 ? 4 : 2;
@@ -110,8 +110,8 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // two lane halves, and the weights feed O^T = V^T P^T straight from registers.
 //
 // What bounds it.  Many rows: the products, 4 D operations a pair.  One causal sequence of 16384
-// tokens, 16 heads on 4 of 128, bf16: 1.01 ms, 1.09 PFLOP/s (a library product of 8192^3 reaches
-// 1.23), the matrix units busy in 61 % of the cycles, at the 1.7 GHz that the card's power leaves.
+// tokens, 16 heads on 4 of 128, bf16: 0.99 ms, 1.11 PFLOP/s (a library product of 8192^3 reaches
+// 1.23), the matrix units busy in 61 % of the cycles, at the 1.76 GHz that the card's power leaves.
 // There a tile's softmax (16 exponentials a lane and 32 x 32 block) runs on one of a SIMD's two
 // waves beside the other's products, and no LDS bank conflict is left.  64 rows and key halves as
 // in fp32 took 1.20 ms, 64 rows a wave 1.40 ms. Single tokens: the bytes of K and V.  64 requests
@@ -123,9 +123,9 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     static constexpr int W = 4, NTH = 64 * W, R = 32 * WR;
     // Keys a tile.  Of few rows in 16-bit types, where the workgroup has a context
     // alone, 32 a wave.  Of few rows in fp32, whose products bound them as much as their bytes:
-    // as many waves as the room lets work, four in one workgroup (D = 64: 161 us for the
+    // as many waves as the room lets work, four in one workgroup (D = 64: 152-162 us for the
     // contexts of 64 requests, 520 MB; 175 two in each of two, 197 one) or, past D = 64, one in
-    // each of two (364 us, 1.04 GB; 432 two in one, 744 one in one).
+    // each of two (375 us, 1.04 GB; 432 two in one, 744 one in one).
     static constexpr int BN = WR != 1 ? 64 : S::kF32 ? (D <= 64 ? 128 : 32) : SPLIT ? 64 : 128;
     static constexpr int KT = WR == W ? BN / 32 : 1;       // 32-key parts that a wave takes
     static constexpr int KW = BN / 32 / KT;                // waves that share a tile's keys
@@ -151,8 +151,8 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         float ref, sum;
     };
 
-    // One key tile.  MASK: some row of the wave sees only a part of it.  There
-    // `fine` weights take part with twice the bits: rows of few keys, all of which
+    // One key tile.  MASK: some row of the tile sees only a part of it.  There
+    // `fine` weights take part with twice the bits: rows of fewer keys than a tile, all of which
     // are in such tiles, have outputs as exact as the statistics.
     template <bool MASK>
     __device__ static void step(const char *kt, const char *vt, const frag *qf, int vis, int key0,

@@ -15,8 +15,8 @@
 // sum has one owner that adds in a fixed order in fp32 registers, without atomics.
 //
 // On 9550 rows of 7 sequences, 16 heads on 4 of 128, bf16, causal (264 GFLOP in 5 products, 370 in
-// 7): statistics 23 us (118 MB, 5 TB/s), dQ, dK and dV 424-465 us, sums of the pieces 22 us. The
-// matrix units are busy in 40 to 44 % of the cycles and the vector units in 30 to 33 %: what bounds
+// 7): statistics 23 us (118 MB, 5 TB/s), dQ, dK and dV 420-440 us, sums of the pieces 22 us. The
+// matrix units are busy in 37 to 40 % of the cycles and the vector units in 26 to 28 %: what bounds
 // it is the chain from scores to dS, with two waves a SIMD to cover it.
 #pragma once
 
