@@ -451,7 +451,7 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
  * In fp16, dS is formed relative to the norms of the rows of dout and v, so
  * gradients of any scale keep their precision: dq row by row; dk and dv, which
  * are sums over rows, relative to the largest rows of their sequence and key head.  No
- * sequence's gradient depends on another one's.  Values of a sequence
+ * sequence's gradient depends on the values of another.  Values of a sequence
  * that are not finite can reach all gradients of that sequence.
  * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a row and key head); and where there are few key tiles
  * for the device (fewer than about 2000 over all key heads) up to three fp32 copies of dk and dv,

@@ -15,9 +15,11 @@ namespace ma {
 // workgroup ends at the same time whatever the contexts are, and starts once.  A row tile counts
 // kBegin steps more than it has, for what its first copies, its rows and its masked key tiles take
 // (measured in bf16 at 128 columns and used for all: 8 us to a step's 2 with 128 rows, 6 to 2.4
-// with 32; without, the workgroups of 8 chunks of up to 512 tokens ended between 153 and 257 us).  Of a share's segments only the first
-// and the last can be parts of a row tile, and go to the partial results: where the share is the row
-// tile's first one it is its last segment, number 2 w + 1 of share w, else its first, 2 w.
+// with 32; without, the workgroups of 8 chunks of up to 512 tokens ended between 153 and 257 us).
+//
+// Of a share's segments only the first and the last can be parts of a row tile, and go to the
+// partial results: where the share is the row tile's first one it is its last segment, number
+// 2 w + 1 of share w, else its first, 2 w.
 template <int R> constexpr int kBegin = R > 32 ? 4 : 2;
 struct Line {
     int64_t all;       // steps
@@ -250,11 +252,10 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
             }
     }
 
-    // A value of V that is not finite meets weights of zero in the rows of a masked
-    // tile that do not see it, where the product would make it NaN, and in the rows that do what
-    // `fine` adds to their weights, of either sign.  So such
-    // values are looked for (`foreign`), added to the rows that see them, and then
-    // taken for zero.
+    // A value of V that is not finite meets weights of zero in the rows of a masked tile that do not
+    // see it, where the product would make it NaN, and in the rows that do what `fine` adds to their
+    // weights, of either sign.  So such values are looked for (`foreign`), added to the rows that see
+    // them, and then taken for zero.
     __device__ static bool foreign(const char *vt)
     {
         bool bad = false;

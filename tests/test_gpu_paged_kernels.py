@@ -82,3 +82,27 @@ def test_a_long_context_among_many_short_ones(ma, dtype):
     for i in (0, 1, 49, 699, 700, 701, 1199):
         ref = attention(q[i : i + 1], *seqs[i], True, past[i])
         assert worst(got[0][i : i + 1], *ref["out"]) <= 1.0 and worst(got[1][:, i : i + 1], *ref["lse"]) <= 1.0, i
+
+
+def test_two_streams_at_once_over_shared_pages(ma):
+    """Split calls on two streams, whose requests share pages of a common prefix: each the bits of a call alone."""
+    gen = torch.Generator(device="cuda").manual_seed(84)
+    _, kp, vp, table, kv = _cache([1, 1, 1, 40], [3000, 2000, 900, 1700], 2, 64, 16, "bf16", gen)
+    table[1:, :50] = table[0, :50]  # 800 tokens
+    cu = starts([1, 1, 1, 40], "cuda")
+    qs = [torch.randn(43, 8, 64, generator=gen, device="cuda").bfloat16() for _ in range(2)]
+    want = [_attend(ma, q, kp, vp, cu, kv, table) for q in qs]
+    got = [(torch.empty_like(o), torch.empty_like(x)) for o, x in want]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q, (out, lse), s in zip(qs, got, streams):
+            ma.monarch_attn_exact_paged_fwd(q, kp, vp, out, cu, kv, table, True, lse, stream=s)
+    torch.cuda.synchronize()
+    for (o, x), (out, lse) in zip(want, got):
+        assert torch.equal(o, out) and torch.equal(x, lse)
+    for row, i in ((0, 0), (1, 1), (2, 2)):
+        n = int(kv[i])
+        pos = torch.arange(n, device="cuda")
+        k, v = (t[table[i, pos // 16].long(), :, pos % 16] for t in (kp, vp))
+        assert worst(want[0][0][row : row + 1], *attention(qs[0][row : row + 1], k, v, True, n - 1)["out"]) <= 1.0, i
