@@ -464,6 +464,42 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
                                   void *stream);
 
 /*
+ * monarch_attn_exact_cross_fwd -- cross attention: the rows of every sequence
+ * over the rows of another tensor (the states of an encoder, projected).
+ *
+ * q, out, lse, : as in monarch_attn_exact_packed_fwd, sequence i the rows cu_q[i] ..
+ * rest           cu_q[i + 1] - 1 of `total`.  So a decoding step of beam search has its beams as
+ *                the rows of one sequence, and reads the encoder's states once for all of them.
+ * k, v         : [total_k, Hkv, d], rows ldk, ldv elements apart: the keys of sequence i
+ *                are in the rows cu_k[i] .. cu_k[i + 1] - 1 (device int32, B + 1 of them, not
+ *                decreasing; each is clamped to 0..total_k).
+ * k_lens       : NULL, or [B] device int32: only the first k_lens[i] of these rows are
+ *                keys (clamped to 0..their number), as in a padded batch.  The others are not read.
+ * Every row sees all keys of its sequence; rows of a sequence without keys get a
+ * zero output and lse -infinity.  The lengths of queries and keys are independent.
+ * Workspace: as in monarch_attn_exact_paged_fwd, where the mean number of keys a sequence is more
+ * than a quarter of the tokens given there.
+ */
+int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
+                                 const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total,
+                                 int64_t total_k, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk, int64_t ldv,
+                                 int32_t clear, int32_t dtype, void *stream);
+
+/*
+ * monarch_attn_exact_cross_bwd -- its gradient, as monarch_attn_exact_packed_bwd.
+ *
+ * out, dout, dq : [total, Hq, d], contiguous; dk, dv: [total_k, Hkv, d], contiguous.
+ * dk and dv are zero in the rows behind k_lens[i] of a sequence, and of sequences without
+ * queries.  Rows of no sequence (by cu_q, by cu_k) are left, or with clear written as zero.
+ * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a key row and key head), and up to three
+ * fp32 copies of dk and dv.
+ */
+int monarch_attn_exact_cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
+                                 const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_q, const int32_t *cu_k,
+                                 const int32_t *k_lens, int64_t B, int64_t total, int64_t total_k, int64_t Hq, int64_t Hkv,
+                                 int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t clear, int32_t dtype, void *stream);
+
+/*
  * monarch_attn_exact_paged_fwd -- the new tokens of every sequence (one, or a
  * chunk) over the keys and values of its pages.
  *

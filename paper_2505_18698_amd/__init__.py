@@ -35,6 +35,7 @@ try:
         MonarchAttnError,
         dtype_code,
         exact_attention_packed,
+        exact_cross_attention,
         fused_applies,
         grouped_applies,
         monarch_attention,
@@ -50,6 +51,8 @@ try:
         monarch_attn_fwd_objective,
         monarch_attn_fwd_prepad,
         monarch_attn_fwd_varlen,
+        monarch_attn_exact_cross_bwd,
+        monarch_attn_exact_cross_fwd,
         monarch_attn_exact_fwd,
         monarch_attn_exact_packed_bwd,
         monarch_attn_exact_packed_fwd,

@@ -42,6 +42,8 @@ EXPORTS = (
     "monarch_attn_fwd_prepad",
     "monarch_attn_exact_packed_fwd",
     "monarch_attn_exact_packed_bwd",
+    "monarch_attn_exact_cross_fwd",
+    "monarch_attn_exact_cross_bwd",
     "monarch_attn_exact_paged_fwd",
     "monarch_attn_paged_plan",
     "monarch_attn_paged_write",
@@ -98,6 +100,8 @@ def _load() -> ctypes.CDLL:
     for name, argtypes in (
         ("monarch_attn_exact_packed_fwd", [vp] * 7 + [i64] * 8 + [i32, i32, i32, vp]),
         ("monarch_attn_exact_packed_bwd", [vp] * 11 + [i64] * 8 + [i32, i32, i32, vp]),
+        ("monarch_attn_exact_cross_fwd", [vp] * 9 + [i64] * 9 + [i32, i32, vp]),
+        ("monarch_attn_exact_cross_bwd", [vp] * 13 + [i64] * 9 + [i32, i32, vp]),
         ("monarch_attn_exact_paged_fwd", [vp] * 8 + [i64] * 9 + [i32, i32, vp]),
         ("monarch_attn_paged_plan", [vp] * 10 + [i64] * 5 + [vp]),
         ("monarch_attn_paged_write", [vp] * 5 + [i64] * 7 + [i32, vp]),
@@ -543,6 +547,20 @@ def _packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal, rest, c
           _stream(q, stream) or None)
 
 
+def _whole(t):
+    """t, contiguous and 16-byte aligned."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def _in_rows(t):
+    """t in the kernels' layout: heads of a row adjacent, rows 16-byte aligned."""
+    n = t.element_size()
+    fits = t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.stride(0) * n % 16 == 0 \
+        and t.shape[1] * t.shape[2] <= t.stride(0) <= _MAX_ROW and t.data_ptr() % 16 == 0
+    return t if fits else _whole(t)
+
+
 _PACKED_FN = None
 
 
@@ -552,20 +570,10 @@ def _packed_function():
     if _PACKED_FN is None:
         import torch
 
-        def whole(t):  # contiguous and 16-byte aligned
-            t = t.contiguous()
-            return t if t.data_ptr() % 16 == 0 else t.clone()
-
-        def rows(t):  # the kernels' layout: heads of a row adjacent, rows 16-byte aligned
-            n = t.element_size()
-            fits = t.dim() == 3 and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.stride(0) * n % 16 == 0 \
-                and t.shape[1] * t.shape[2] <= t.stride(0) <= _MAX_ROW and t.data_ptr() % 16 == 0
-            return t if fits else whole(t)
-
         class ExactAttentionPackedFn(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, v, cu_seqlens, causal):
-                q, k, v = rows(q), rows(k), rows(v)
+                q, k, v = _in_rows(q), _in_rows(k), _in_rows(v)
                 sizes, strides = _check_packed(q, k, v, cu_seqlens)
                 out = q.new_empty(q.shape)
                 lse = q.new_empty((sizes[2], sizes[1]), dtype=torch.float32)
@@ -583,7 +591,7 @@ def _packed_function():
                 q, k, v, out, lse, cu_seqlens, rest = ctx.saved_tensors
                 dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
                 causal, dims = ctx.call
-                _packed_bwd(q, k, v, out, lse, whole(dout), dq, dk, dv, cu_seqlens, causal, rest, True, None, dims)
+                _packed_bwd(q, k, v, out, lse, _whole(dout), dq, dk, dv, cu_seqlens, causal, rest, True, None, dims)
                 return dq, dk, dv, None, None
 
         _PACKED_FN = ExactAttentionPackedFn
@@ -601,6 +609,129 @@ def exact_attention_packed(q, k, v, cu_seqlens, causal: bool = True):
     (drop its outputs, or capture with leaves of its own): torch would wait
     for the stream of that graph, which ends the capture and may end the process."""
     return _packed_function().apply(q, k, v, cu_seqlens, causal)
+
+
+def _check_cross(q, k, v, cu_q, cu_k, k_lens):
+    """Sizes (B, total, total_k, Hq, Hkv, d) and row strides of q [total, Hq, d], k and v [total_k, Hkv, d]."""
+    rt = _torch()
+    try:
+        total, Hq, d = q.shape
+        total_k, Hkv, _ = k.shape
+        (B,) = cu_q.shape
+        dtype, device, int32 = q.dtype, q.device, rt.int32
+        ldq, ldk, ldv = _rows(q, dtype, device), _rows(k, dtype, device), _rows(v, dtype, device)
+        if q.is_cuda and ldq >= 0 and ldk >= 0 and ldv >= 0 and k.shape == v.shape and k.shape[2] == d and B > 0 \
+                and _is(cu_q, (B,), int32, device) and _is(cu_k, (B,), int32, device) \
+                and (k_lens is None or _is(k_lens, (B - 1,), int32, device)):
+            return (B - 1, total, total_k, Hq, Hkv, d), (ldq, ldk, ldv)
+    except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
+        pass
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        _check_rows(name, t, q)
+    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("k and v must be [total_k, Hkv, d] tensors with the head dimension of q")
+    if not isinstance(cu_q, rt.Tensor) or cu_q.dim() != 1 or cu_q.shape[0] < 1:
+        raise ValueError("cu_q must be an int32 tensor [B + 1]")
+    B = cu_q.shape[0]
+    _check_like("cu_q", cu_q, (B,), q, rt.int32)
+    _check_like("cu_k", cu_k, (B,), q, rt.int32)
+    if k_lens is not None:
+        _check_like("k_lens", k_lens, (B - 1,), q, rt.int32)
+    raise ValueError("q, k and v must be device tensors")
+
+
+def monarch_attn_exact_cross_fwd(q, k, v, out, cu_q, cu_k, k_lens=None, lse=None, rest=None, clear: bool = False, stream=None):
+    """Cross attention: q [total, Hq, d] in sequences of rows cu_q[i] to cu_q[i + 1]
+    (int32 device tensor [B + 1]) over all keys of the same sequence in k and v
+    [total_k, Hkv, d], rows cu_k[i] to cu_k[i + 1], of which with k_lens (int32
+    [B]: a padded batch) only the first k_lens[i] are keys.  Rows of all three may
+    be strided.  Writes out [total, Hq, d] and, as monarch_attn_exact_packed_fwd,
+    lse and rest; rows of a sequence without keys become zero, those of no
+    sequence are left, or, with clear, zero.  Returns (out, lse).
+
+    The new tokens of a request's beams are rows of one sequence: its keys are read once for all of them."""
+    sizes, strides = _check_cross(q, k, v, cu_q, cu_k, k_lens)
+    _check_each(q, ("out", out, q.shape, q.dtype))
+    if lse is not None:
+        _check_each(q, ("lse", lse, (q.shape[1], q.shape[0]), _torch().float32))
+    if rest is not None:
+        _check_each(q, ("rest", rest, q.shape, q.dtype))
+    _cross_fwd(q, k, v, out, cu_q, cu_k, k_lens, lse, rest, clear, stream, sizes + strides)
+    return out, lse
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _cross_fwd(q, k, v, out, cu_q, cu_k, k_lens, lse, rest, clear, stream, dims):
+    _call(LIB.monarch_attn_exact_cross_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _address(lse), _address(rest),
+          cu_q.data_ptr(), cu_k.data_ptr(), _address(k_lens), *dims, bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
+
+
+def monarch_attn_exact_cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, k_lens=None, rest=None, clear: bool = False,
+                                 stream=None):
+    """The gradient of monarch_attn_exact_cross_fwd from its out, lse and rest (None:
+    without) and dout = dL/dout, into dq [total, Hq, d], dk and dv
+    [total_k, Hkv, d] (contiguous; padding behind k_lens gets zero, rows of no
+    sequence are left, or, with clear, zero).  Returns (dq, dk, dv)."""
+    sizes, strides = _check_cross(q, k, v, cu_q, cu_k, k_lens)
+    rows, keys, dtype = q.shape, k.shape, q.dtype
+    _check_each(q, ("out", out, rows, dtype), ("dout", dout, rows, dtype), ("dq", dq, rows, dtype), ("dk", dk, keys, dtype),
+                ("dv", dv, keys, dtype), ("lse", lse, (rows[1], rows[0]), _torch().float32))
+    if rest is not None:
+        _check_each(q, ("rest", rest, rows, dtype))
+    _cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, k_lens, rest, clear, stream, sizes + strides)
+    return dq, dk, dv
+
+
+def _cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, k_lens, rest, clear, stream, dims):
+    _call(LIB.monarch_attn_exact_cross_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), _address(rest),
+          dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _address(k_lens), *dims,
+          bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
+
+
+_CROSS_FN = None
+
+
+def _cross_function():
+    """torch.autograd.Function of monarch_attn_exact_cross_fwd and _bwd."""
+    global _CROSS_FN
+    if _CROSS_FN is None:
+        import torch
+
+        class ExactCrossAttentionFn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, cu_q, cu_k, k_lens):
+                q, k, v = _in_rows(q), _in_rows(k), _in_rows(v)
+                sizes, strides = _check_cross(q, k, v, cu_q, cu_k, k_lens)
+                out = q.new_empty(q.shape)
+                lse = q.new_empty((sizes[3], sizes[1]), dtype=torch.float32)
+                rest = q.new_empty(q.shape) if q.element_size() == 2 else None
+                _cross_fwd(q, k, v, out, cu_q, cu_k, k_lens, lse, rest, True, None, sizes + strides)
+                ctx.save_for_backward(q, k, v, out, lse, cu_q, cu_k, k_lens, rest)
+                ctx.dims = sizes + strides
+                return out
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, dout):
+                q, k, v, out, lse, cu_q, cu_k, k_lens, rest = ctx.saved_tensors
+                dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
+                _cross_bwd(q, k, v, out, lse, _whole(dout), dq, dk, dv, cu_q, cu_k, k_lens, rest, True, None, ctx.dims)
+                return dq, dk, dv, None, None, None
+
+        _CROSS_FN = ExactCrossAttentionFn
+    return _CROSS_FN
+
+
+def exact_cross_attention(q, k, v, cu_q, cu_k, k_lens=None):
+    """Cross attention as a differentiable torch op (see
+    monarch_attn_exact_cross_fwd; tensors in other layouts are copied).  Rows of
+    no sequence get zero output and zero gradients, and so do the rows behind
+    k_lens.  Differentiable once; for capture into a HIP graph the same holds as
+    for exact_attention_packed."""
+    return _cross_function().apply(q, k, v, cu_q, cu_k, k_lens)
 
 
 def _check_cache(k_pages, v_pages, heads, d, like, like_name):

@@ -1,112 +1,20 @@
-// C ABI of the exact attention over packed sequences and paged caches
+// C ABI of the exact attention over packed sequences, paged caches and other sequences' rows
 // (include/monarch_attn.h): argument checks, workspaces and how a call runs.
 #include <algorithm>
 #include <cmath>
-#include <exception>
 
-#include "seq_host.hpp"
+#include "seq_checks.hpp"
 #include "seq_params.hpp"
 
 namespace {
 
 using namespace ma_host;
 
-size_t elem_bytes(int32_t dtype) { return dtype == MA_F32 ? 4 : 2; }
-size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
-
-// A C function that cannot let a C++ exception out.
-template <typename F> int guarded(F &&f)
-{
-    try {
-        return f();
-    } catch (const std::exception &e) {
-        return fail(MA_ENOMEM, "out of host resources: %s", e.what());
-    } catch (...) {
-        return fail(MA_ENOMEM, "out of host resources");
-    }
-}
-
-// A device memory range of an argument.
-struct Range {
-    const char *name;
-    const void *p;
-    size_t bytes;
-};
-
-int check_alignment(const Range &r, size_t to)
-{
-    if (!r.p) return fail(MA_EINVAL, "null %s pointer", r.name);
-    if ((uintptr_t)r.p % to) return fail(MA_EINVAL, "%s must be %zu-byte aligned", r.name, to);
-    return MA_OK;
-}
-
-// No output may overlap another one or an input.
-template <size_t NO, size_t NI> int check_overlaps(const Range (&outs)[NO], const Range (&ins)[NI])
-{
-    for (size_t i = 0; i < NO; ++i) {
-        if (!outs[i].p) continue;
-        for (const Range &in : ins)
-            if (in.p && ranges_overlap(outs[i].p, outs[i].bytes, in.p, in.bytes))
-                return fail(MA_EINVAL, "%s must not overlap %s", outs[i].name, in.name);
-        for (size_t j = i + 1; j < NO; ++j)
-            if (outs[j].p && ranges_overlap(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes))
-                return fail(MA_EINVAL, "%s must not overlap %s", outs[i].name, outs[j].name);
-    }
-    return MA_OK;
-}
-
-constexpr int64_t kMaxWidth = int64_t(1) << 20;  // elements of a row: offsets within a tile of rows stay in 32 bits
-
-int check_heads(int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int32_t dtype)
-{
-    if (dtype != MA_F32 && dtype != MA_BF16 && dtype != MA_F16) return fail(MA_EINVAL, "unknown dtype %d", dtype);
-    if (B < 0 || total < 0) return fail(MA_EINVAL, "B and total must be >= 0");
-    if (Hq < 1 || Hkv < 1 || d < 1) return fail(MA_EINVAL, "Hq, Hkv and d must be >= 1");
-    if (Hq % Hkv) return fail(MA_EINVAL, "Hq (%lld) must be a multiple of Hkv (%lld)", (long long)Hq, (long long)Hkv);
-    const int64_t chunk = 16 / (int64_t)elem_bytes(dtype);
-    if (d > 128 || d % chunk)
-        return fail(MA_EUNSUPPORTED, "d must be a multiple of %lld up to 128 (got %lld)", (long long)chunk, (long long)d);
-    if (Hq > kMaxWidth / tile_d(d))
-        return fail(MA_EUNSUPPORTED, "Hq times d, rounded up to %d, must not exceed %lld", (int)tile_d(d), (long long)kMaxWidth);
-    if (B > 0x7ffffffe || total > 0x7fffff00 || total * (Hq / Hkv) > 0x7fffff00)
-        return fail(MA_EUNSUPPORTED, "total * (Hq / Hkv) and B must be below 2^31");
-    return MA_OK;
-}
-
-// Rows of `ld` elements that hold `width`.
-int check_stride(const char *name, int64_t ld, int64_t width, int32_t dtype)
-{
-    const int64_t chunk = 16 / (int64_t)elem_bytes(dtype);
-    if (ld < width || ld % chunk)
-        return fail(MA_EINVAL, "%s (%lld) must be at least %lld and a multiple of %lld", name, (long long)ld, (long long)width,
-                    (long long)chunk);
-    if (ld > kMaxWidth) return fail(MA_EUNSUPPORTED, "%s must not exceed %lld", name, (long long)kMaxWidth);
-    return MA_OK;
-}
-
 // Row tiles of R packed rows over all sequences, at most (tile0 in seq_tiles.hpp), and one without
 // any.
 int64_t tiles_of(int64_t total, int64_t rows_a_token, int64_t B, int64_t R) { return std::max<int64_t>(1, total * rows_a_token / R + B); }
 
-// (HIP launches fewer than 2^32 threads a dimension; every kernel here has kSeqThreads a workgroup.)
-int check_grid(int64_t units, int64_t Hkv)
-{
-    if (units > 0xffffffffll / kSeqThreads / Hkv) return fail(MA_EUNSUPPORTED, "too many tiles for one grid");
-    return MA_OK;
-}
-
 float log2_scale(int64_t d) { return (float)(1.4426950408889634 / std::sqrt((double)d)); }
-
-size_t span_bytes(int64_t rows, int64_t ld, int64_t width, int32_t dtype)
-{
-    return rows == 0 ? 0 : ((size_t)(rows - 1) * ld + width) * elem_bytes(dtype);
-}
-
-#define MA_TRY(x)                    \
-    do {                             \
-        const int rc_ = (x);         \
-        if (rc_ != MA_OK) return rc_; \
-    } while (0)
 
 struct FwdLaunch {
     ma::SeqFwd p;
@@ -167,7 +75,7 @@ int packed_fwd(const void *q, const void *k, const void *v, void *out, float *ls
     p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
     p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
     p.c = log2_scale(d), p.causal = causal != 0, p.clear = clear != 0, p.tiles = (int)tiles;
-    x.how = SeqPlan{false, false, seq_rows(dtype), tiles};
+    x.how = SeqPlan{ma::kSelf, false, seq_rows(dtype), tiles};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
 }
@@ -248,21 +156,6 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;
     return run_launches(stream, BwdLaunch::run, &x);
-}
-
-int check_pages(int64_t pages, int64_t page)
-{
-    if (page < 8 || page > 4096 || (page & (page - 1)))
-        return fail(MA_EUNSUPPORTED, "page must be a power of two from 8 to 4096 (got %lld)", (long long)page);
-    if (pages < 0 || pages > 0x7fffffff) return fail(MA_EINVAL, "pages must be in 0..2^31 - 1");
-    return MA_OK;
-}
-
-int log2_of(int64_t page)
-{
-    int x = 0;
-    while ((int64_t(1) << x) < page) ++x;
-    return x;
 }
 
 // How a paged call runs.  Sequences of few new rows (on average no more than 32 packed ones: single
@@ -353,9 +246,125 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     p.part_o = (float *)c.ws, p.part_l = (float *)(c.ws + s.bytes_o);
     p.parts = (ma::SeqTileParts *)(c.ws + s.bytes_o + s.bytes_l);
     p.shares = (int)s.units;
-    x.how = SeqPlan{true, s.split, s.rows, s.units};
+    x.how = SeqPlan{ma::kPaged, s.split, s.rows, s.units};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
+}
+
+// The split of a cross call: that of a paged one, by the keys that its longest sequence may have. The
+// host knows how many there are in all: the longest one is taken for four times the mean one.
+PagedSplit cross_split(int64_t total, int64_t total_k, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t num_cus, int32_t dtype)
+{
+    const int64_t longest = std::min(total_k, 4 * ((total_k + B - 1) / std::max<int64_t>(1, B)));
+    return paged_split(total, B, G, Hkv, d, longest, num_cus, dtype);
+}
+
+int check_cross(int64_t B, int64_t total, int64_t total_k, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk,
+                int64_t ldv, int32_t dtype)
+{
+    MA_TRY(check_heads(B, total, Hq, Hkv, d, dtype));
+    if (total_k < 0) return fail(MA_EINVAL, "total_k must be >= 0");
+    if (total_k > 0x7fffff00) return fail(MA_EUNSUPPORTED, "total_k must be below 2^31");
+    MA_TRY(check_stride("ldq", ldq, Hq * d, dtype));
+    MA_TRY(check_stride("ldk", ldk, Hkv * d, dtype));
+    return check_stride("ldv", ldv, Hkv * d, dtype);
+}
+
+int cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest, const int32_t *cu_q,
+              const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total, int64_t total_k, int64_t Hq, int64_t Hkv,
+              int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t clear, int32_t dtype, hipStream_t stream)
+{
+    MA_TRY(check_cross(B, total, total_k, Hq, Hkv, d, ldq, ldk, ldv, dtype));
+    const int64_t G = Hq / Hkv;
+    MA_TRY(check_grid(tiles_of(total, G, B, paged_rows(total, B, G, dtype)), Hkv));
+    if (total == 0 || (B == 0 && !clear)) return MA_OK;
+    if (rest && dtype == MA_F32) return fail(MA_EINVAL, "rest is of 16-bit outputs");
+    const size_t ob = span_bytes(total, Hq * d, Hq * d, dtype), starts = (size_t)(B + 1) * 4;
+    const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
+                         {"k", k, span_bytes(total_k, ldk, Hkv * d, dtype)},
+                         {"v", v, span_bytes(total_k, ldv, Hkv * d, dtype)},
+                         {"cu_q", cu_q, starts},
+                         {"cu_k", cu_k, starts},
+                         {"k_lens", k_lens, k_lens ? (size_t)B * 4 : 0}};
+    const Range outs[] = {{"out", out, ob}, {"lse", lse, lse ? (size_t)(Hq * total) * 4 : 0}, {"rest", rest, rest ? ob : 0}};
+    MA_TRY(check_ranges(ins, {16, 16, 16, 4, 4, 4}));
+    MA_TRY(check_ranges(outs, {16, 4, 16}));
+    MA_TRY(check_overlaps(outs, ins));
+    CallScope c;
+    MA_TRY(begin_call(c));
+    PagedSplit s = cross_split(total, total_k, B, G, Hkv, d, c.num_cus, dtype);
+    if (s.split && B > 0) {
+        MA_TRY(check_grid(s.units, Hkv));
+        MA_TRY(call_workspace(stream, s.bytes_o + s.bytes_l + s.bytes_parts, c));
+    } else {
+        s.split = false, s.units = s.tiles;
+    }
+    FwdLaunch x{};
+    ma::SeqFwd &p = x.p;
+    p.q = q, p.k = k, p.v = v, p.out = out, p.lse = lse, p.rest = rest;
+    p.seqs = ma::Seqs{cu_q, (int)B, (int)total};
+    p.keys = ma::KeySeqs{{cu_k, (int)B, (int)total_k}, k_lens};
+    p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
+    p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
+    p.c = log2_scale(d), p.clear = clear != 0, p.tiles = (int)s.tiles;
+    p.part_o = (float *)c.ws, p.part_l = (float *)(c.ws + s.bytes_o);
+    p.parts = (ma::SeqTileParts *)(c.ws + s.bytes_o + s.bytes_l);
+    p.shares = (int)s.units;
+    x.how = SeqPlan{ma::kCross, s.split, s.rows, s.units};
+    x.dtype = dtype;
+    return run_launches(stream, FwdLaunch::run, &x);
+}
+
+int cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest, const void *dout,
+              void *dq, void *dk, void *dv, const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total,
+              int64_t total_k, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t clear, int32_t dtype,
+              hipStream_t stream)
+{
+    MA_TRY(check_cross(B, total, total_k, Hq, Hkv, d, ldq, ldk, ldv, dtype));
+    const int64_t G = Hq / Hkv, tiles_q = tiles_of(total, G, B, seq_rows(dtype)), tiles_k = tiles_of(total_k, 1, B, kSeqBwdKeys);
+    MA_TRY(check_grid(std::max(tiles_q, tiles_k), Hkv));
+    if ((total == 0 && total_k == 0) || (B == 0 && !clear)) return MA_OK;
+    if (rest && dtype == MA_F32) return fail(MA_EINVAL, "rest is of 16-bit outputs");
+    const size_t qb = span_bytes(total, Hq * d, Hq * d, dtype), kb = span_bytes(total_k, Hkv * d, Hkv * d, dtype), starts = (size_t)(B + 1) * 4;
+    const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
+                         {"k", k, span_bytes(total_k, ldk, Hkv * d, dtype)},
+                         {"v", v, span_bytes(total_k, ldv, Hkv * d, dtype)},
+                         {"out", out, qb},
+                         {"dout", dout, qb},
+                         {"lse", lse, (size_t)(Hq * total) * 4},
+                         {"cu_q", cu_q, starts},
+                         {"cu_k", cu_k, starts},
+                         {"k_lens", k_lens, k_lens ? (size_t)B * 4 : 0},
+                         {"rest", rest, rest ? qb : 0}};
+    const Range outs[] = {{"dq", dq, qb}, {"dk", dk, kb}, {"dv", dv, kb}};
+    MA_TRY(check_ranges(ins, {16, 16, 16, 16, 16, 4, 4, 4, 4, 16}));
+    MA_TRY(check_ranges(outs, {16, 16, 16}));
+    MA_TRY(check_overlaps(outs, ins));
+    CallScope c;
+    MA_TRY(begin_call(c));
+    const int64_t pieces = bwd_pieces(total, tiles_k, Hkv, G, c.num_cus);
+    const size_t part = pieces > 1 ? (size_t)(pieces * total_k * Hkv) * tile_d(d) * 4 : 0;
+    const size_t each = stat_bytes_of(total, Hq), norms = dtype == MA_F16 ? each + stat_bytes_of(total_k, Hkv) : 0;
+    const size_t stat_bytes = 2 * each + norms;
+    MA_TRY(check_grid(tiles_k * pieces + tiles_q, Hkv));
+    MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
+    BwdLaunch x{};
+    ma::SeqBwd &p = x.p;
+    p.q = q, p.k = k, p.v = v, p.out = out, p.dout = dout, p.lse = lse, p.rest = rest;
+    p.dq = dq, p.dk = dk, p.dv = dv;
+    p.seqs = ma::Seqs{cu_q, (int)B, (int)total};
+    p.keys = ma::KeySeqs{{cu_k, (int)B, (int)total_k}, k_lens};
+    p.Hkv = (int)Hkv, p.G = (int)G, p.d = (int)d;
+    p.ldq = ldq, p.ldk = ldk, p.ldv = ldv;
+    p.c = log2_scale(d), p.clear = clear != 0;
+    p.tiles_q = (int)tiles_q, p.tiles_k = (int)tiles_k;
+    p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each);
+    if (dtype == MA_F16) p.norm_g = (float *)(c.ws + 2 * each), p.norm_v = (float *)(c.ws + 3 * each);
+    p.stat_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(kStatBlocks, (std::max(total * G, total_k) + 15) / 16 * Hkv));
+    p.pieces = (int)pieces;
+    p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
+    x.dtype = dtype;
+    return run_launches(stream, BwdLaunch::run, &x);
 }
 
 int paged_plan(const int32_t *past, const int32_t *fresh, const int32_t *ring, const int32_t *free_in, int32_t *table,
@@ -428,6 +437,30 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
     return guarded([&] {
         return packed_bwd(q, k, v, out, lse, rest, dout, dq, dk, dv, cu_seqlens, B, total, Hq, Hkv, d, ldq, ldk, ldv, causal, clear, dtype,
                           (hipStream_t)stream);
+    });
+}
+
+int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
+                                 const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total,
+                                 int64_t total_k, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk, int64_t ldv,
+                                 int32_t clear, int32_t dtype, void *stream)
+{
+    g_err[0] = '\0';
+    return guarded([&] {
+        return cross_fwd(q, k, v, out, lse, rest, cu_q, cu_k, k_lens, B, total, total_k, Hq, Hkv, d, ldq, ldk, ldv, clear, dtype,
+                         (hipStream_t)stream);
+    });
+}
+
+int monarch_attn_exact_cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
+                                 const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_q, const int32_t *cu_k,
+                                 const int32_t *k_lens, int64_t B, int64_t total, int64_t total_k, int64_t Hq, int64_t Hkv,
+                                 int64_t d, int64_t ldq, int64_t ldk, int64_t ldv, int32_t clear, int32_t dtype, void *stream)
+{
+    g_err[0] = '\0';
+    return guarded([&] {
+        return cross_bwd(q, k, v, out, lse, rest, dout, dq, dk, dv, cu_q, cu_k, k_lens, B, total, total_k, Hq, Hkv, d, ldq, ldk, ldv,
+                         clear, dtype, (hipStream_t)stream);
     });
 }
 

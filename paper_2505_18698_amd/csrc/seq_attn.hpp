@@ -1,4 +1,5 @@
-// Exact attention over packed sequences and over paged caches.
+// Exact attention over packed sequences, over paged caches and over other sequences' rows (cross
+// attention).
 //
 // For every sequence, key head and group of query heads on it:
 //   O_i = sum_j P_ij v_j,  P_ij = exp(s q_i.k_j - lse_i),  lse_i = log sum_j exp(s q_i.k_j),
@@ -29,7 +30,15 @@ struct Line {
     int64_t at;        // its first step
 };
 
-template <int R, int BN, int NTH>
+// Keys of sequence s (paged: at most max_keys).
+template <Keys KEYS> __device__ inline int keys_of(const SeqFwd &p, int s, int max_keys)
+{
+    if constexpr (KEYS == kPaged) return max(0, min(p.kv_lens[s], max_keys));
+    if constexpr (KEYS == kCross) return p.keys.count(s);
+    return p.seqs.length(s);
+}
+
+template <Keys KEYS, int R, int BN, int NTH>
 __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char *lds)
 {
     int64_t *sh = reinterpret_cast<int64_t *>(lds);
@@ -37,7 +46,7 @@ __device__ inline Line find_share(const SeqFwd &p, int share, int max_keys, char
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     auto shape = [&](int s, int &rt, int &kt) {
         rt = s < p.seqs.B ? (int)(((int64_t)p.seqs.length(s) * p.G + R - 1) / R) : 0;
-        const int kv = s < p.seqs.B ? max(0, min(p.kv_lens[s], max_keys)) : 0;
+        const int kv = s < p.seqs.B ? keys_of<KEYS>(p, s, max_keys) : 0;
         kt = kBegin<R> + max(1, (kv + BN - 1) / BN);
     };
     int64_t sum = 0, tiles = 0;
@@ -119,7 +128,8 @@ __device__ inline int share_of(int64_t x, int64_t all, int shares) { return (int
 // in fp32 took 1.20 ms, 64 rows a wave 1.40 ms. Single tokens: the bytes of K and V.  64 requests
 // of up to 8192 tokens, 32 heads on 8 of 128, bf16, 521 MB: 103 us, 5.1 TB/s; 2 of 131000, 1.07 GB:
 // 190-197 us, 5.5 TB/s (a large copy reads and writes 4.9).
-template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
+template <typename T, int D, int WR, Keys KEYS, bool SPLIT> struct SeqAttn {
+    static constexpr bool PAGED = KEYS == kPaged;
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
     static constexpr int W = 4, NTH = 64 * W, R = 32 * WR;
@@ -322,7 +332,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
 
     // The K and V rows that a wave copies.
     struct Rows {
-        const T *k, *v;    // packed: the sequence's rows; paged: the key head's part of page 0
+        const T *k, *v;    // the sequence's rows; paged: the key head's part of page 0
         const int *table;  // paged: the sequence's pages
         int kv;            // rows from this one on read as zero
         Copy ck, cv;
@@ -374,14 +384,16 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
         const int max_keys = PAGED ? (int)min((int64_t)p.blocks << p.page_log2, (int64_t)0x7fffff00) : 0;  // (a tile behind the last one still has a number)
         if constexpr (SPLIT) {
             const int share = uniform((int)(blockIdx.x / p.Hkv));
-            Line f = find_share<R, BN, NTH>(p, share, max_keys, lds);
+            if constexpr (!PAGED)
+                if (p.clear) clear_outside<NTH>(p.seqs, p.out, (int64_t)p.Hkv * p.G * p.d * sizeof(T), blockIdx.x, gridDim.x);
+            Line f = find_share<KEYS, R, BN, NTH>(p, share, max_keys, lds);
             int seq = uniform(f.seq), tile = uniform(f.tile), index = uniform(f.index);
             if (seq < 0) return;
             const int shares = uniform(f.shares);
             const int64_t all = uniform(f.all), end = all * (share + 1) / shares;
             int64_t at = uniform(f.at), x = all * share / shares;
             while (x < end && index < p.tiles) {
-                const int n = uniform(p.seqs.length(seq)), kv = uniform(max(0, min(p.kv_lens[seq], max_keys)));
+                const int n = uniform(p.seqs.length(seq)), kv = uniform(keys_of<KEYS>(p, seq, max_keys));
                 const int tiles = (int)(((int64_t)n * p.G + R - 1) / R), steps = max(1, (kv + BN - 1) / BN);
                 if (tile >= tiles) {  // the next sequence
                     ++seq, tile = 0;
@@ -417,7 +429,7 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
                                                    int key_tile0, int key_tiles, bool parts, int64_t unit, int max_keys)
     {
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
-        const int kv = PAGED ? uniform(max(0, min(p.kv_lens[seq], max_keys))) : n;
+        const int kv = KEYS == kSelf ? n : uniform(keys_of<KEYS>(p, seq, max_keys));
         const int rows = n * p.G, r0 = tile * R;
         auto visible = [&](int r) {  // keys that packed row r sees (the last row stands for those behind it)
             const int64_t i = (int64_t)min(r, rows - 1) / p.G + (PAGED ? kv - n : 0) + 1;
@@ -454,8 +466,9 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
             src.ck.init(p.d * (int)sizeof(T), p.d, wave, lane);
         } else {
             const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
-            src.k = (const T *)p.k + row0 * p.ldk + kvh * p.d;
-            src.v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
+            const int64_t key_row0 = KEYS == kSelf ? row0 : uniform(p.keys.start(seq));
+            src.k = (const T *)p.k + key_row0 * p.ldk + kvh * p.d;
+            src.v = (const T *)p.v + key_row0 * p.ldv + kvh * p.d;
             src.ck.init(ldk, p.d, wave, lane);
             src.cv.init(ldv, p.d, wave, lane);
         }
@@ -554,10 +567,10 @@ template <typename T, int D, int WR, bool PAGED, bool SPLIT> struct SeqAttn {
     }
 };
 
-template <typename T, int D, int WR, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGED && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
+template <typename T, int D, int WR, Keys KEYS, bool SPLIT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : KEYS == kSelf && D * sizeof(T) <= 128 ? 3 : 2) void seq_attention(SeqFwd p)
 {
-    using U = SeqAttn<T, D, WR, PAGED, SPLIT>;
+    using U = SeqAttn<T, D, WR, KEYS, SPLIT>;
     __shared__ __attribute__((aligned(16))) char lds[U::LDS_BYTES];
     U::run(p, lds);
 }
@@ -565,6 +578,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 && WR > 1 ? 1 : !PAGE
 // Packed row `at` of a sequence if no segment has a weight of it: zero where it sees no key, else
 // 0 / 0.
 __device__ inline float without_weight(const SeqTileParts &f, int at) { return at < f.blind ? 0.f : NAN; }
+
+// Element `at` of out, and what its rounding leaves.
+template <typename T> __device__ inline void store_joined(const SeqFwd &p, int64_t at, float x)
+{
+    const T y = to_elem<T>(x);
+    ((T *)p.out)[at] = y;
+    if constexpr (sizeof(T) == 2)
+        if (p.rest) ((T *)p.rest)[at] = to_elem<T>(x - (float)y);
+}
 
 // The segments of a split call's rows joined: O = sum_x w_x O_x / sum_x w_x, w_x = exp(lse_x). One
 // workgroup per row tile and key head, and, of tiles of many rows, 8 rows, 32 threads a row (they
@@ -600,10 +622,10 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
         const float inv = mx == -INFINITY ? without_weight(f, at) : 1.f / sum;
         const int head = kvh * p.G + at % p.G;
         const int64_t row = f.row0 + at / p.G;
-        T *out = (T *)p.out + (row * p.Hkv * p.G + head) * p.d + c * C;
+        const int64_t to = (row * p.Hkv * p.G + head) * p.d + c * C;
 #pragma unroll
         for (int i = 0; i < C; ++i)
-            if (c * C + i < p.d) out[i] = to_elem<T>(o[i] * inv);
+            if (c * C + i < p.d) store_joined<T>(p, to + i, o[i] * inv);
         if (p.lse && c == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
         return;
     }
@@ -634,7 +656,7 @@ __global__ __launch_bounds__(256) void seq_join(SeqFwd p)
             const int at = f.at + r;
             const int64_t row = f.row0 + at / p.G;
             const int head = kvh * p.G + at % p.G;
-            if (tid < p.d) ((T *)p.out)[(row * p.Hkv * p.G + head) * p.d + tid] = to_elem<T>(mx == -INFINITY ? without_weight(f, at) : y / all);
+            if (tid < p.d) store_joined<T>(p, (row * p.Hkv * p.G + head) * p.d + tid, mx == -INFINITY ? without_weight(f, at) : y / all);
             if (p.lse && tid == 0) p.lse[(int64_t)head * p.seqs.total + row] = mx == -INFINITY ? mx : (ref + __builtin_amdgcn_logf(all)) * kLn2;
         }
         __syncthreads();

@@ -1,4 +1,4 @@
-// The gradient of exact attention over packed sequences.
+// The gradient of exact attention over packed sequences, and of cross attention to the rows of others.
 //
 // With P = exp(s Q K^T - lse) and the upstream gradient dO:
 //   delta_i = sum_c dO_ic O_ic (= sum_j P_ij dP_ij),  dP = dO V^T,
@@ -78,14 +78,15 @@ template <typename T> struct BwdScale {
 // delta and lse in log2 units of every (row, head), 16 lanes a row; in fp16 also
 // the norms of dO and v.  A workgroup takes one head of 16 rows at a time, whose lse, delta
 // and lse2 are then 64 bytes together.
-template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
+template <typename T, Keys KEYS> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
 {
+    const Seqs &keys = KEYS == kCross ? p.keys : p.seqs;
     constexpr int V = 16 / (int)sizeof(T);
     const int Hq = p.Hkv * p.G, lane = threadIdx.x & 15;
     if (p.clear) {
         clear_outside<256>(p.seqs, p.dq, (int64_t)Hq * p.d * sizeof(T), blockIdx.x, gridDim.x);
-        clear_outside<256>(p.seqs, p.dk, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
-        clear_outside<256>(p.seqs, p.dv, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
+        clear_outside<256>(keys, p.dk, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
+        clear_outside<256>(keys, p.dv, (int64_t)p.Hkv * p.d * sizeof(T), blockIdx.x, gridDim.x);
     }
     const int first = p.seqs.start(0), last = p.seqs.start(p.seqs.B);  // (rows of no sequence count for nothing)
 #pragma unroll 2
@@ -123,9 +124,10 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
         }
     }
     if constexpr (BwdScale<T>::kScaled) {
-        for (int64_t u = blockIdx.x; u < ((int64_t)last - first + 15) / 16 * p.Hkv; u += gridDim.x) {
-            const int head = (int)(u % p.Hkv), row = first + (int)(u / p.Hkv) * 16 + (int)(threadIdx.x >> 4);
-            if (row >= last) continue;
+        const int first_k = keys.start(0), last_k = keys.start(keys.B);
+        for (int64_t u = blockIdx.x; u < ((int64_t)last_k - first_k + 15) / 16 * p.Hkv; u += gridDim.x) {
+            const int head = (int)(u % p.Hkv), row = first_k + (int)(u / p.Hkv) * 16 + (int)(threadIdx.x >> 4);
+            if (row >= last_k) continue;
             float norm = 0.f;
             const T *v = (const T *)p.v + row * p.ldv + head * p.d;
             for (int col = lane * V; col < p.d; col += 16 * V) {
@@ -136,14 +138,14 @@ template <typename T> __global__ __launch_bounds__(256) void seq_stats(SeqBwd p)
             }
 #pragma unroll
             for (int x = 1; x < 16; x <<= 1) norm += __shfl_xor(norm, x);
-            if (lane == 0) p.norm_v[(int64_t)head * p.seqs.total + row] = norm < INFINITY ? norm : 0.f;
+            if (lane == 0) p.norm_v[(int64_t)head * keys.total + row] = norm < INFINITY ? norm : 0.f;
         }
     }
 }
 
 // dQ: the forward's schedule.  S^T = K Q^T and dP^T = V dO^T hold one query row a
 // lane, so lse and delta are lane scalars, and dS^T feeds dQ^T += K^T dS^T from registers.
-template <typename T, int D> struct SeqBwdQ {
+template <typename T, int D, Keys KEYS> struct SeqBwdQ {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
     static constexpr int W = 4, NTH = 64 * W;
@@ -215,8 +217,9 @@ template <typename T, int D> struct SeqBwdQ {
         if (seq < 0) return;
         const int tile = uniform((int)(t - tile0(p.seqs, seq, p.G, R)));
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
+        const int key_row0 = KEYS == kCross ? uniform(p.keys.start(seq)) : row0, keys = KEYS == kCross ? uniform(p.keys.count(seq)) : n;
         const int rows = n * p.G, r0 = tile * R, tok0 = r0 / p.G;
-        auto visible = [&](int r) { return p.causal ? min(r, rows - 1) / p.G + 1 : n; };
+        auto visible = [&](int r) { return p.causal ? min(r, rows - 1) / p.G + 1 : keys; };
         const int see_all = uniform(visible(r0)), last = uniform(visible(r0 + R - 1));
         const int wr0 = r0 + wave % WR * 32, part = wave / WR * 32 * KT;
         const int see_most = uniform(visible(wr0 + 31));
@@ -237,20 +240,20 @@ template <typename T, int D> struct SeqBwdQ {
         const float lse2 = p.lse2[at], delta = p.delta[at];
         float scale = 1.f;  // of this row's dS
         if constexpr (BwdScale<T>::kScaled) {
-            float most = BwdScale<T>::template own_largest<NTH>(p.norm_v + (int64_t)kvh * p.seqs.total + row0, last, 1, 0), none = 0.f;
+            float most = BwdScale<T>::template own_largest<NTH>(p.norm_v + (int64_t)kvh * (KEYS == kCross ? p.keys : p.seqs).total + key_row0, last, 1, 0), none = 0.f;
             BwdScale<T>::template all_largest<NTH>(most, none, lds);
             scale = BwdScale<T>::of(p.norm_g[at], most);
         }
 
         const int ldk = (int)p.ldk * (int)sizeof(T), ldv = (int)p.ldv * (int)sizeof(T);
-        const T *k = (const T *)p.k + row0 * p.ldk + kvh * p.d, *v = (const T *)p.v + row0 * p.ldv + kvh * p.d;
+        const T *k = (const T *)p.k + key_row0 * p.ldk + kvh * p.d, *v = (const T *)p.v + key_row0 * p.ldv + kvh * p.d;
         Copy ck, cv;
         ck.init(ldk, p.d, wave, lane);
         cv.init(ldv, p.d, wave, lane);
         auto bring = [&](int key0, int buf) {
             if (key0 >= last) return;
-            ck.tile(k + key0 * p.ldk, n - key0, ldk, lds + 2 * TILE * buf, wave);
-            cv.tile(v + key0 * p.ldv, n - key0, ldv, lds + 2 * TILE * buf + TILE, wave);
+            ck.tile(k + key0 * p.ldk, keys - key0, ldk, lds + 2 * TILE * buf, wave);
+            cv.tile(v + key0 * p.ldv, keys - key0, ldv, lds + 2 * TILE * buf + TILE, wave);
         };
 
         f32x16 dq[S::ND];
@@ -309,7 +312,7 @@ template <typename T, int D> struct SeqBwdQ {
 // what does not fit goes through memory (530 us on the rows above; 288 us so, as a launch of
 // its own).  Few keys and many rows a workgroup, because the
 // longest walk, that of a long sequence's first keys, bounds the call.
-template <typename T, int D> struct SeqBwdK {
+template <typename T, int D, Keys KEYS> struct SeqBwdK {
     using S = SeqTile<T, D>;
     using frag = typename S::frag;
     static constexpr int NK = 2, NQ = 2, W = NK * NQ, NTH = 64 * W, R = 32 * NK;
@@ -400,9 +403,9 @@ template <typename T, int D> struct SeqBwdK {
         }
     }
 
-    // The waves' sums of one gradient, scaled, to the keys' rows of `out`.
+    // The waves' sums of one gradient, scaled, to the keys' rows of `out`; zero in the `padding` rows behind them.
     template <typename O>
-    __device__ static void add_up(char *lds, const f32x16 *x, const Span &out, float by, int ld, int d, int keys, int wave, int lane)
+    __device__ static void add_up(char *lds, const f32x16 *x, const Span &out, float by, int ld, int d, int keys, int padding, int wave, int lane)
     {
         constexpr int N = S::ND * 4 * 64;  // a wave's sums, in 4 values
         static_assert(W * N * 16 <= 4 * TILE, "the tiles' room holds them");
@@ -422,7 +425,9 @@ template <typename T, int D> struct SeqBwdK {
 #pragma unroll
                 for (int q = 1; q < NQ; ++q) sum += src[q * NK * N + e * 64];
                 const int key = 32 * kb + (lane & 31), col = 32 * dt + 8 * e + 4 * (lane >> 5);
-                out.store<O>(sum * by, (key * ld + col) * (int)sizeof(O), key < keys && col < d);
+                if constexpr (KEYS == kCross)
+                    if (key >= keys) sum = f32x4{0.f, 0.f, 0.f, 0.f};
+                out.store<O>(sum * by, (key * ld + col) * (int)sizeof(O), key < keys + padding && col < d);
             }
         }
     }
@@ -433,28 +438,32 @@ template <typename T, int D> struct SeqBwdK {
         const int kvh = uniform(block % p.Hkv);
         const int64_t t = block / p.Hkv / p.pieces;  // (earlier keys are seen by more rows: they start first)
         const int piece = uniform(block / p.Hkv % p.pieces);
-        const int seq = uniform(seq_of_tile(p.seqs, t, 1, R, lane));
+        const Seqs &key_seqs = KEYS == kCross ? p.keys : p.seqs;
+        const int seq = uniform(seq_of_tile(key_seqs, t, 1, R, lane));
         if (seq < 0) return;
         const int row0 = uniform(p.seqs.start(seq)), n = uniform(p.seqs.length(seq));
-        const int k0 = uniform((int)(t - tile0(p.seqs, seq, 1, R)) * R), Hq = p.Hkv * p.G;
+        // keys: of the sequence; behind them come `padding` rows, whose gradients are zero
+        const int key_row0 = KEYS == kCross ? uniform(p.keys.start(seq)) : row0, keys = KEYS == kCross ? uniform(p.keys.count(seq)) : n;
+        const int k0 = uniform((int)(t - tile0(key_seqs, seq, 1, R)) * R), Hq = p.Hkv * p.G;
+        const int padding = KEYS == kCross ? uniform(p.keys.length(seq)) - max(keys, k0) : 0;
         const int from = p.causal ? k0 : 0;  // the first row that sees a key of this workgroup
         float ds = 1.f;                      // the power of two of dS
         if constexpr (BwdScale<T>::kScaled) {
-            const float *g = p.norm_g + (int64_t)kvh * p.G * p.seqs.total + row0 + from, *v = p.norm_v + (int64_t)kvh * p.seqs.total + row0;
+            const float *g = p.norm_g + (int64_t)kvh * p.G * p.seqs.total + row0 + from, *v = p.norm_v + (int64_t)kvh * key_seqs.total + key_row0;
             float most_g = BwdScale<T>::template own_largest<NTH>(g, n - from, p.G, p.seqs.total);
-            float most_v = BwdScale<T>::template own_largest<NTH>(v, n, 1, 0);
+            float most_v = BwdScale<T>::template own_largest<NTH>(v, keys, 1, 0);
             BwdScale<T>::template all_largest<NTH>(most_g, most_v, lds);
             ds = BwdScale<T>::of(most_g, most_v);
         }
 
-        const Span ks((const T *)p.k + (row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d);
-        const int ldv = (int)p.ldv * (int)sizeof(T), kc = min(32 * kb + (lane & 31), n - 1 - k0);
+        const Span ks((const T *)p.k + (key_row0 + k0) * p.ldk + kvh * p.d), vs((const T *)p.v + (key_row0 + k0) * p.ldv + kvh * p.d);
+        const int ldv = (int)p.ldv * (int)sizeof(T), kc = max(0, min(32 * kb + (lane & 31), keys - 1 - k0));
         char *vt = lds + 4 * TILE;
         frag kf[S::NS], vf[kVInLds ? 1 : S::NS];
         if constexpr (kVInLds) {
             TileCopy<T, D, R, W> cv;
             cv.init(ldv, p.d, wave, lane);
-            cv.tile((const T *)p.v + (row0 + k0) * p.ldv + kvh * p.d, n - k0, ldv, vt, wave);
+            cv.tile((const T *)p.v + (key_row0 + k0) * p.ldv + kvh * p.d, keys - k0, ldv, vt, wave);
         }
 #pragma unroll
         for (int i = 0; i < S::NS; ++i) {
@@ -472,7 +481,7 @@ template <typename T, int D> struct SeqBwdK {
         cq.init(ldq, p.d, wave, lane);
         cg.init(ldg, p.d, wave, lane);
         // The walk: every head's tiles from row `from` on, this piece's share of them.
-        const int tiles = (n - from + BQ - 1) / BQ;
+        const int tiles = KEYS == kCross && keys <= k0 ? 0 : (n - from + BQ - 1) / BQ;
         const int begin = uniform((int)((int64_t)p.G * tiles * piece / p.pieces)), end = uniform((int)((int64_t)p.G * tiles * (piece + 1) / p.pieces));
         float lse2 = 0.f, delta = 0.f;  // of this lane's row of the tile that is copied
         auto bring = [&](int i, int g, int q0, int buf) {  // tile i of the walk, at row q0 of head g or the next one's first
@@ -494,7 +503,7 @@ template <typename T, int D> struct SeqBwdK {
 #pragma unroll
         for (int dt = 0; dt < S::ND; ++dt) x.dk[dt] = x.dv[dt] = f32x16{};
         const float scale = BwdScale<T>::kScaled ? ds * 0x1p-14f : 1.f;
-        int buf = 0, i = begin, g = begin / tiles;
+        int buf = 0, i = begin, g = KEYS == kCross && tiles == 0 ? 0 : begin / tiles;
         int q0 = from + (begin - g * tiles) * BQ;
         bring(i, g, q0, 0);
         const char *own = lds + 32 * qb * S::ROW, *vrows = vt + 32 * kb * S::ROW;
@@ -519,16 +528,16 @@ template <typename T, int D> struct SeqBwdK {
                     step<false>(own + 2 * TILE * buf, own + 2 * TILE * buf + TILE, terms, kf, vf, vrows, 0, 0, p.c, scale, x, lane);
             }
         }
-        const float by_k = n == 1 ? 0.f : p.c * kLn2 / ds, by_v = BwdScale<T>::kScaled ? 0x1p-14f : 1.f;
+        const float by_k = keys == 1 ? 0.f : p.c * kLn2 / ds, by_v = BwdScale<T>::kScaled ? 0x1p-14f : 1.f;
         if (p.pieces > 1) {
-            const int64_t at = (((int64_t)piece * p.seqs.total + row0 + k0) * p.Hkv + kvh) * D;
-            add_up<float>(lds, x.dk, Span(p.part_k + at), by_k, p.Hkv * D, D, n - k0, wave, lane);
-            add_up<float>(lds, x.dv, Span(p.part_v + at), by_v, p.Hkv * D, D, n - k0, wave, lane);
+            const int64_t at = (((int64_t)piece * key_seqs.total + key_row0 + k0) * p.Hkv + kvh) * D;
+            add_up<float>(lds, x.dk, Span(p.part_k + at), by_k, p.Hkv * D, D, max(0, keys - k0), padding, wave, lane);
+            add_up<float>(lds, x.dv, Span(p.part_v + at), by_v, p.Hkv * D, D, max(0, keys - k0), padding, wave, lane);
             return;
         }
-        const int64_t out0 = ((int64_t)(row0 + k0) * p.Hkv + kvh) * p.d;
-        add_up<T>(lds, x.dk, Span((T *)p.dk + out0), by_k, p.Hkv * p.d, p.d, n - k0, wave, lane);
-        add_up<T>(lds, x.dv, Span((T *)p.dv + out0), by_v, p.Hkv * p.d, p.d, n - k0, wave, lane);
+        const int64_t out0 = ((int64_t)(key_row0 + k0) * p.Hkv + kvh) * p.d;
+        add_up<T>(lds, x.dk, Span((T *)p.dk + out0), by_k, p.Hkv * p.d, p.d, max(0, keys - k0), padding, wave, lane);
+        add_up<T>(lds, x.dv, Span((T *)p.dv + out0), by_v, p.Hkv * p.d, p.d, max(0, keys - k0), padding, wave, lane);
     }
 };
 
@@ -536,10 +545,10 @@ template <typename T, int D> struct SeqBwdK {
 // and the shorter ones of dK and dV fill what they leave free.  (fp32, 6 sequences of up to 1000
 // tokens, 12 heads of 64: 98 us, two launches 132 (87 since); the rows above 466 us, two launches
 // 474, dK and dV first 472.)
-template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd(SeqBwd p, int blocks_q)
+template <typename T, int D, Keys KEYS> __global__ __launch_bounds__(256, sizeof(T) == 4 && D > 64 ? 1 : 2) void seq_bwd(SeqBwd p, int blocks_q)
 {
-    using K = SeqBwdK<T, D>;
-    using Q = SeqBwdQ<T, D>;
+    using K = SeqBwdK<T, D, KEYS>;
+    using Q = SeqBwdQ<T, D, KEYS>;
     static_assert(K::NTH == 256 && Q::NTH == 256, "one launch");
     __shared__ __attribute__((aligned(16))) char lds[K::LDS_BYTES > Q::LDS_BYTES ? K::LDS_BYTES : Q::LDS_BYTES];
     const int block = blockIdx.x;
@@ -550,11 +559,12 @@ template <typename T, int D> __global__ __launch_bounds__(256, sizeof(T) == 4 &&
 }
 
 // The pieces' sums of dK and dV added up, four columns a thread.
-template <typename T, int D> __global__ __launch_bounds__(256) void seq_bwd_join(SeqBwd p)
+template <typename T, int D, Keys KEYS> __global__ __launch_bounds__(256) void seq_bwd_join(SeqBwd p)
 {
     constexpr int C = D / 4;
-    const int64_t first = (int64_t)p.seqs.start(0) * p.Hkv, rows = (int64_t)p.seqs.start(p.seqs.B) * p.Hkv - first;
-    const int64_t each = (int64_t)p.seqs.total * p.Hkv * D;
+    const Seqs &keys = KEYS == kCross ? p.keys : p.seqs;
+    const int64_t first = (int64_t)keys.start(0) * p.Hkv, rows = (int64_t)keys.start(keys.B) * p.Hkv - first;
+    const int64_t each = (int64_t)keys.total * p.Hkv * D;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * C; i += (int64_t)gridDim.x * 256) {
         const int64_t row = first + i / C;
         const int col = (int)(i % C) * 4;

@@ -14,21 +14,29 @@ template <typename T, int D> int run_seq_fwd_d(Launcher &L, const ma::SeqFwd &p,
     const bool few = how.rows == kSeqFewRows;
     constexpr int R = kSeqRows<T>, WR = R / 32;
     constexpr int kLds = 160 << 10;
-    static_assert(std::min(2, kLds / ma::SeqAttn<T, D, 1, true, true>::LDS_BYTES) == seq_residents<T>(D, true) &&
-                      std::min(2, kLds / ma::SeqAttn<T, D, WR, true, true>::LDS_BYTES) == seq_residents<T>(D, false),
+    using ma::kCross, ma::kPaged, ma::kSelf;
+    static_assert(std::min(2, kLds / ma::SeqAttn<T, D, 1, kPaged, true>::LDS_BYTES) == seq_residents<T>(D, true) &&
+                      std::min(2, kLds / ma::SeqAttn<T, D, WR, kPaged, true>::LDS_BYTES) == seq_residents<T>(D, false),
                   "the shares of a split call are as many as the device holds");
     int rc = L.run(kSeqFwd, [&] {
         return launched([&] {
-            if (!how.paged)
-                ma::seq_attention<T, D, WR, false, false><<<grid, block, 0, L.stream>>>(p);
-            else if (!how.split && !few)
-                ma::seq_attention<T, D, WR, true, false><<<grid, block, 0, L.stream>>>(p);
-            else if (!how.split)
-                ma::seq_attention<T, D, 1, true, false><<<grid, block, 0, L.stream>>>(p);
-            else if (!few)
-                ma::seq_attention<T, D, WR, true, true><<<grid, block, 0, L.stream>>>(p);
+            auto by_rows = [&](auto keys) {
+                constexpr ma::Keys K = decltype(keys)::value;
+                if (!how.split && !few)
+                    ma::seq_attention<T, D, WR, K, false><<<grid, block, 0, L.stream>>>(p);
+                else if (!how.split)
+                    ma::seq_attention<T, D, 1, K, false><<<grid, block, 0, L.stream>>>(p);
+                else if (!few)
+                    ma::seq_attention<T, D, WR, K, true><<<grid, block, 0, L.stream>>>(p);
+                else
+                    ma::seq_attention<T, D, 1, K, true><<<grid, block, 0, L.stream>>>(p);
+            };
+            if (how.keys == kSelf)
+                ma::seq_attention<T, D, WR, kSelf, false><<<grid, block, 0, L.stream>>>(p);
+            else if (how.keys == kPaged)
+                by_rows(std::integral_constant<ma::Keys, kPaged>{});
             else
-                ma::seq_attention<T, D, 1, true, true><<<grid, block, 0, L.stream>>>(p);
+                by_rows(std::integral_constant<ma::Keys, kCross>{});
         });
     });
     if (rc != MA_OK || !how.split) return rc;

@@ -40,7 +40,8 @@ bool ranges_overlap(const void *a, size_t na, const void *b, size_t nb);
 
 // How a forward call runs.
 struct SeqPlan {
-    bool paged, split;
+    int keys;  // an ma::Keys
+    bool split;
     int rows;       // packed rows a workgroup takes
     int64_t units;  // workgroups of one key head
 };

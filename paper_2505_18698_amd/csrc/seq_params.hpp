@@ -16,12 +16,28 @@ struct Seqs {
     __device__ inline int length(int s) const { return max(0, start(s + 1) - start(s)); }
 };
 
+// Where the keys of the query rows are: in the same rows; in pages; or, for cross attention, in rows
+// of their own.
+enum Keys { kSelf, kPaged, kCross };
+
+// The key rows of cross attention: the ranges of packed sequences, of which the first lens[s] rows
+// are keys (null: all of them) and the others padding.
+struct KeySeqs : Seqs {
+    const int *lens;
+    __device__ inline int count(int s) const
+    {
+        const int n = length(s);
+        return lens ? max(0, min(lens[s], n)) : n;
+    }
+};
+
 struct SeqFwd {
-    const void *q, *k, *v;  // packed: rows of ldq, ldk, ldv elements; paged: k, v are [pages, Hkv, page, d]
+    const void *q, *k, *v;  // packed, cross: rows of ldq, ldk, ldv elements; paged: k, v are [pages, Hkv, page, d]
     void *out;              // [total, Hq, d]
     float *lse;             // [Hq, total] or null
     void *rest;             // as out, or null: what rounding out to 16 bits leaves
     Seqs seqs;              // the query rows
+    KeySeqs keys;           // cross: the key rows
     const int *kv_lens;     // paged: keys of every sequence
     const int *table;       // paged: [B, blocks] page numbers
     int Hkv, G, d;          // Hq = Hkv G
@@ -29,7 +45,7 @@ struct SeqFwd {
     int page_log2, pages, blocks;
     float c;                // s log2(e)
     int causal;
-    int clear;              // packed: write zeros in the rows of no sequence
+    int clear;              // packed, cross: write zeros in the rows of no sequence
     int tiles;              // row tiles of one key head (an upper bound)
     // split over the keys: workgroups of one key head; their segments' rows,
     // normalised, and their log2-sum-exp; and what every row tile is made of
@@ -47,10 +63,11 @@ struct SeqTileParts {
 
 struct SeqBwd {
     const void *q, *k, *v, *out, *dout;  // q, k, v: rows of ldq, ldk, ldv elements
-    const float *lse;                    // [Hq, total]
+    const float *lse;                    // [Hq, total]; total: of the query rows, total_k of the key rows (self: the same)
     const void *rest;                    // as out, or null
     void *dq, *dk, *dv;
     Seqs seqs;
+    KeySeqs keys;                        // cross: the key rows
     int Hkv, G, d;
     int64_t ldq, ldk, ldv;
     float c;                             // s log2(e)
@@ -58,7 +75,7 @@ struct SeqBwd {
     int clear;                           // write zeros in the gradients' rows of no sequence
     int tiles_q, tiles_k;                // row and key tiles of one key head (upper bounds)
     float *lse2, *delta;                 // [Hq, total]: lse in log2 units, delta
-    float *norm_g, *norm_v;              // fp16: |dO_i|^2 [Hq, total] and |v_j|^2 [Hkv, total], 0 where not finite
+    float *norm_g, *norm_v;              // fp16: |dO_i|^2 [Hq, total] and |v_j|^2 [Hkv, total_k], 0 where not finite
     int stat_blocks;                     // workgroups of the row statistics
     // pieces that the query rows of a key tile are cut into; with more than one, their sums:
     // dK and dV of every piece, row and key head, in rows of the tile width
