@@ -584,6 +584,96 @@ int monarch_attn_paged_write(const void *k, const void *v, void *k_pages, void *
                              int64_t rows, int64_t Hkv, int64_t d, int64_t ldk, int64_t ldv, int64_t pages,
                              int64_t page, int32_t dtype, void *stream);
 
+/*
+ * ---- A decoder's positions and beams ----
+ *
+ * Types, alignment, errors, asynchrony and graph capture as above.
+ */
+
+/*
+ * monarch_attn_rotate -- rotary positions: the rows of q and k, turned.  Pair i
+ * of a head, (a, b), of a token at position t becomes
+ *   (a cos w - b sin w, a sin w + b cos w),  w = t inv_freq[i],
+ * with inverse != 0 the same of -w, which is also the gradient.  The angle is
+ * formed in 64 bits, the turn in fp32.
+ *
+ * q, k        : [total, Hq, d] and [total, Hk, d], rows ldq, ldk elements apart; Hk may be 0 (then
+ *               k and k_out are not read or written).
+ * q_out, k_out: the same, contiguous.  Not overlapping the inputs.
+ * inv_freq    : [rot / 2] device floats, radians a token.
+ * rot         : columns that turn, a multiple of 8 up to d; those behind are copied.
+ *               Pairs are the columns i and rot / 2 + i, with interleaved != 0 2 i and 2 i + 1.
+ * cu_seqlens  : row starts, as in monarch_attn_exact_packed_fwd.  Rows of no sequence
+ *               are left, or with clear != 0 written as zero.
+ * kv_lens     : NULL: a row's position is its number in its sequence.  Else [B] device int32: the
+ *               rows of sequence i are the last of its kv_lens[i] tokens, as in
+ *               monarch_attn_exact_paged_fwd (a position before the first token is negative).
+ */
+int monarch_attn_rotate(const void *q, const void *k, void *q_out, void *k_out, const float *inv_freq, const int32_t *cu_seqlens,
+                        const int32_t *kv_lens, int64_t B, int64_t total, int64_t Hq, int64_t Hk, int64_t d, int64_t rot,
+                        int64_t ldq, int64_t ldk, int32_t interleaved, int32_t inverse, int32_t clear, int32_t dtype, void *stream);
+
+/*
+ * monarch_attn_paged_append -- monarch_attn_rotate and monarch_attn_paged_write in one
+ * pass: the rows of q turned into q_out, those of k turned into their slots of k_pages, those of v
+ * into v_pages.  cu_seqlens and kv_lens (not NULL) as monarch_attn_paged_plan makes them.
+ * Rows of no sequence are not written anywhere, rows without a slot not into pages.
+ */
+int monarch_attn_paged_append(const void *q, const void *k, const void *v, void *q_out, void *k_pages, void *v_pages,
+                              const float *inv_freq, const int32_t *cu_seqlens, const int32_t *kv_lens, const int64_t *slots,
+                              int64_t B, int64_t total, int64_t Hq, int64_t Hkv, int64_t d, int64_t rot, int64_t ldq, int64_t ldk,
+                              int64_t ldv, int64_t pages, int64_t page, int32_t interleaved, int32_t dtype, void *stream);
+
+#define MONARCH_ATTN_BEAM_MAX 32            /* beams of a request, and candidates taken  */
+#define MONARCH_ATTN_BEAM_MAX_VOCAB 524288  /* tokens to choose from                    */
+
+/*
+ * monarch_attn_beam_select -- a step of beam search: of all candidates (beam k, token t) of a
+ * request, with the value
+ *   scores[k] + logits[k, t] - log sum_u exp(logits[k, u]),
+ * the M largest in descending order; equal ones by the lowest k V + t.
+ *
+ * logits    : [B, K, V], rows ld elements apart (any ld >= V; aligned to their element only).
+ *             -infinity: a token that is not allowed.
+ * scores    : [B, K] device floats, the beams' sums so far; -infinity: a beam that is not in
+ *             use (as all but the first are at the start).
+ * done      : NULL, or [B, K] bytes: a beam that has ended offers the token eos, at its own
+ *             score, and nothing else.
+ * scores_out, tokens, parents : [B, M], written: value, token and beam.
+ * done_out  : NULL, or [B, M] bytes, written: whether the beam is done or the token eos.
+ * eos       : a token, needed with done or done_out (else anything).
+ *
+ * A candidate whose value is not a number counts as -infinity, so do those of a beam with a logit of NaN or
+ * +infinity or without any allowed token.  Where fewer than M candidates are larger, -infinities fill up, the
+ * lowest k V + t first.  Values are formed in 64 bits from sums of fp32 exponentials.  Within a beam
+ * the order is that of the logits, also where its score is too large for the sums to differ.
+ * K and M up to MONARCH_ATTN_BEAM_MAX, M <= K V, V up to MONARCH_ATTN_BEAM_MAX_VOCAB.
+ * Workspace: 8 M + 8 bytes for every 8192 tokens of a beam.
+ */
+int monarch_attn_beam_select(const void *logits, const float *scores, const uint8_t *done, float *scores_out, int32_t *tokens,
+                             int32_t *parents, uint8_t *done_out, int64_t B, int64_t K, int64_t V, int64_t M, int64_t ld, int32_t eos,
+                             int32_t dtype, void *stream);
+
+/*
+ * monarch_attn_paged_reorder -- the cache of K beams a request as that of their
+ * parents, in place.  Beam c of request b is sequence b K + c of the paged cache.
+ *
+ * parents    : [B, K] device int32: beam c goes on from beam parents[b, c] (out of range: from itself).
+ * lens       : [B K] device int32, tokens in the cache; the beams of a request have the same number
+ *              (that of its first beam counts).
+ * block_table: [B K, blocks] device int32.  With n tokens, the entries of the n / page full
+ *              pages become the parent's (move_table != 0), so beams share full pages. The started page, if
+ *              any, stays each beam's own and gets the rows of the parent's.
+ * k_pages, v_pages : [pages, Hkv, page, d].  The started pages of different beams must be different
+ *              ones, as monarch_attn_paged_plan gives them.
+ * One call a layer, of which only one moves the table that the layers share.  A
+ * page keeps being that of the sequence for which the plan took it: give the pages of a request back when all of
+ * its beams have ended.
+ */
+int monarch_attn_paged_reorder(void *k_pages, void *v_pages, int32_t *block_table, const int32_t *parents, const int32_t *lens,
+                               int64_t B, int64_t K, int64_t Hkv, int64_t d, int64_t pages, int64_t page, int64_t blocks,
+                               int32_t move_table, int32_t dtype, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

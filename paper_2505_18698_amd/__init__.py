@@ -8,6 +8,8 @@ raises the ImportError: there is no fallback path.
 """
 try:
     from ._binding import (  # noqa: F401
+        BEAM_MAX,
+        BEAM_MAX_VOCAB,
         EXPORTS,
         KIND_NAMES,
         LIB,
@@ -40,6 +42,7 @@ try:
         grouped_applies,
         monarch_attention,
         monarch_attention_autograd,
+        monarch_attn_beam_select,
         monarch_attn_bwd,
         monarch_attn_bwd_varlen,
         monarch_attn_bwd_check,
@@ -59,13 +62,17 @@ try:
         monarch_attn_exact_paged_fwd,
         monarch_attn_fwd_raw,
         monarch_attn_last_error,
+        monarch_attn_paged_append,
         monarch_attn_paged_plan,
+        monarch_attn_paged_reorder,
         monarch_attn_paged_write,
         monarch_attn_release_workspace,
+        monarch_attn_rotate,
         monarch_attn_set_path,
         monarch_attn_timing_enable,
         monarch_attn_timing_read,
         monarch_attn_workspace_bytes,
+        rotate_packed,
     )
 except ImportError as _err:  # library not built
     _missing = _err

@@ -17,7 +17,8 @@ STATUS_NAMES = {0: "MA_OK", 1: "MA_EINVAL", 2: "MA_EUNSUPPORTED", 3: "MA_EHIP", 
 KIND_NAMES = {0: "r_half_step", 1: "l_half_step", 2: "r_half_step_final", 3: "monarch_apply",
               4: "monarch_fused_head", 5: "objective_sum", 6: "exact_attention", 7: "l_bwd", 8: "r_bwd",
               9: "monarch_fused_group", 10: "seq_attention", 11: "seq_join", 12: "seq_stats", 13: "seq_bwd",
-              14: "seq_bwd_join", 15: "paged_plan", 16: "paged_write"}
+              14: "seq_bwd_join", 15: "paged_plan", 16: "paged_write", 17: "rotate", 18: "beam_parts", 19: "beam_join",
+              20: "paged_reorder"}
 PATH_AUTO, PATH_HALF_STEPS, PATH_FUSED, PATH_GROUPED = 0, 1, 2, 3
 
 # Every symbol declared in include/monarch_attn.h.
@@ -47,6 +48,10 @@ EXPORTS = (
     "monarch_attn_exact_paged_fwd",
     "monarch_attn_paged_plan",
     "monarch_attn_paged_write",
+    "monarch_attn_rotate",
+    "monarch_attn_paged_append",
+    "monarch_attn_beam_select",
+    "monarch_attn_paged_reorder",
 )
 
 
@@ -105,6 +110,10 @@ def _load() -> ctypes.CDLL:
         ("monarch_attn_exact_paged_fwd", [vp] * 8 + [i64] * 9 + [i32, i32, vp]),
         ("monarch_attn_paged_plan", [vp] * 10 + [i64] * 5 + [vp]),
         ("monarch_attn_paged_write", [vp] * 5 + [i64] * 7 + [i32, vp]),
+        ("monarch_attn_rotate", [vp] * 7 + [i64] * 8 + [i32] * 4 + [vp]),
+        ("monarch_attn_paged_append", [vp] * 10 + [i64] * 11 + [i32, i32, vp]),
+        ("monarch_attn_beam_select", [vp] * 7 + [i64] * 5 + [i32, i32, vp]),
+        ("monarch_attn_paged_reorder", [vp] * 5 + [i64] * 7 + [i32, i32, vp]),
     ):
         getattr(lib, name).argtypes = argtypes
         getattr(lib, name).restype = ctypes.c_int
@@ -167,7 +176,7 @@ class _Torch:
         import torch
 
         self.Tensor = torch.Tensor
-        self.int32, self.int64, self.float32 = torch.int32, torch.int64, torch.float32
+        self.int32, self.int64, self.float32, self.bool = torch.int32, torch.int64, torch.float32, torch.bool
         self.codes = {torch.float32: MA_F32, torch.bfloat16: MA_BF16, torch.float16: MA_F16}
         self.device = torch.cuda.device
         self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -840,6 +849,208 @@ def monarch_attn_paged_write(k, v, k_pages, v_pages, slots, stream=None):
     _call(LIB.monarch_attn_paged_write, k, k.data_ptr(), v.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
           slots.data_ptr(), rows, Hkv, d, ldk, ldv, pages, page, dtype_code(k.dtype), _stream(k, stream) or None)
     return k_pages, v_pages
+
+
+# ---- a decoder's positions and beams ----
+
+BEAM_MAX = 32  # MONARCH_ATTN_BEAM_MAX
+BEAM_MAX_VOCAB = 524288  # MONARCH_ATTN_BEAM_MAX_VOCAB
+
+
+def _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens):
+    """Sizes (B, total, Hq, Hk, d, rot) and row strides of q [total, Hq, d] and k [total, Hk, d] or None."""
+    rt = _torch()
+    try:
+        total, Hq, d = q.shape
+        Hk = 0 if k is None else k.shape[1]
+        (B,), (pairs,) = cu_seqlens.shape, inv_freq.shape
+        dtype, device, int32 = q.dtype, q.device, rt.int32
+        ldq, ldk = _rows(q, dtype, device), 0 if k is None else _rows(k, dtype, device)
+        if q.is_cuda and ldq >= 0 and ldk >= 0 and (k is None or k.shape == (total, Hk, d)) and B > 0 \
+                and _is(cu_seqlens, (B,), int32, device) and _is(inv_freq, (pairs,), rt.float32, device) \
+                and (kv_lens is None or _is(kv_lens, (B - 1,), int32, device)):
+            return (B - 1, total, Hq, Hk, d, 2 * pairs), (ldq, ldk)
+    except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
+        pass
+    _check_rows("q", q, q)
+    if k is not None:
+        _check_rows("k", k, q)
+        if k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+            raise ValueError("k must have the rows and head dimension of q")
+    for name, t in (("inv_freq", inv_freq), ("cu_seqlens", cu_seqlens)):
+        if not isinstance(t, rt.Tensor) or t.dim() != 1 or name == "cu_seqlens" and t.shape[0] < 1:
+            raise ValueError(f"{name} must be a tensor of one dimension")
+    _check_like("inv_freq", inv_freq, inv_freq.shape, q, rt.float32)
+    _check_like("cu_seqlens", cu_seqlens, cu_seqlens.shape, q, rt.int32)
+    if kv_lens is not None:
+        _check_like("kv_lens", kv_lens, (cu_seqlens.shape[0] - 1,), q, rt.int32)
+    raise ValueError("q and k must be device tensors")
+
+
+def monarch_attn_rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, kv_lens=None, interleaved: bool = False, inverse: bool = False,
+                        clear: bool = False, stream=None):
+    """Rotary positions: q [total, Hq, d] and k [total, Hk, d] (rows may be strided; k
+    and k_out may be None), sequences by cu_seqlens (int32 [B + 1]), turned by
+    position times inv_freq (float32 [pairs], 2 pairs a multiple of 8 up to d),
+    with `inverse` backwards, into the contiguous q_out and k_out.  Pairs are the
+    columns i and pairs + i, or, interleaved, 2 i and 2 i + 1.  A row's position is
+    its number in its sequence, or, with kv_lens (int32 [B]), the rows are the last
+    of so many tokens.  Rows of no sequence are left, or, with clear, zero.
+    Returns (q_out, k_out)."""
+    sizes, strides = _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens)
+    _check_each(q, ("q_out", q_out, q.shape, q.dtype))
+    if k is not None:
+        _check_each(q, ("k_out", k_out, k.shape, q.dtype))
+    _rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, kv_lens, interleaved, inverse, clear, stream, sizes + strides)
+    return q_out, k_out
+
+
+def _rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, kv_lens, interleaved, inverse, clear, stream, dims):
+    _call(LIB.monarch_attn_rotate, q, q.data_ptr(), _address(k), q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+          inv_freq.data_ptr(), cu_seqlens.data_ptr(), _address(kv_lens), *dims, bool(interleaved), bool(inverse), bool(clear),
+          dtype_code(q.dtype), _stream(q, stream) or None)
+
+
+_ROTATE_FN = None
+
+
+def _rotate_function():
+    """torch.autograd.Function of monarch_attn_rotate."""
+    global _ROTATE_FN
+    if _ROTATE_FN is None:
+        import torch
+
+        class RotatePackedFn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, inv_freq, cu_seqlens, interleaved):
+                q, k = _in_rows(q), _in_rows(k)
+                sizes, strides = _check_rotation(q, k, inv_freq, cu_seqlens, None)
+                q_out, k_out = q.new_empty(q.shape), k.new_empty(k.shape)
+                _rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, None, interleaved, False, True, None, sizes + strides)
+                ctx.save_for_backward(inv_freq, cu_seqlens)
+                ctx.call = interleaved, sizes
+                return q_out, k_out
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, dq_out, dk_out):
+                (inv_freq, cu_seqlens), (interleaved, sizes) = ctx.saved_tensors, ctx.call
+                g, h = _in_rows(dq_out), _in_rows(dk_out)
+                dq, dk = g.new_empty(g.shape), h.new_empty(h.shape)
+                strides = _rows(g, g.dtype, g.device), _rows(h, g.dtype, g.device)
+                _rotate(g, h, dq, dk, inv_freq, cu_seqlens, None, interleaved, True, True, None, sizes + strides)
+                return dq, dk, None, None, None
+
+        _ROTATE_FN = RotatePackedFn
+    return _ROTATE_FN
+
+
+def rotate_packed(q, k, inv_freq, cu_seqlens, interleaved: bool = False):
+    """Rotary positions of packed sequences as a differentiable torch op (see
+    monarch_attn_rotate; tensors in other layouts are copied).  Rows of no sequence
+    get zeros and zero gradients.  Differentiable in q and k, once; for capture
+    into a HIP graph the same holds as for exact_attention_packed.
+    Returns (q_out, k_out)."""
+    return _rotate_function().apply(q, k, inv_freq, cu_seqlens, interleaved)
+
+
+def monarch_attn_paged_append(q, k, v, q_out, k_pages, v_pages, inv_freq, cu_seqlens, kv_lens, slots, interleaved: bool = False,
+                              stream=None):
+    """monarch_attn_rotate and monarch_attn_paged_write in one pass: rows of q
+    [total, Hq, d] turned by their positions into q_out, of k [total, Hkv, d]
+    turned into their slots (int64 [total], -1: nowhere) of k_pages
+    [pages, Hkv, page, d], of v as they are into v_pages.  cu_seqlens, kv_lens and
+    slots as monarch_attn_paged_plan makes them.  Returns (q_out, k_pages, v_pages)."""
+    sizes, strides = _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens)
+    B, total, Hq, Hkv, d, rot = sizes
+    if k is None:
+        raise TypeError("k must be a device tensor")
+    try:
+        ldv = _rows(v, q.dtype, q.device) if v.shape == k.shape else -1
+    except (AttributeError, ValueError):
+        ldv = -1
+    if ldv < 0:
+        _check_rows("v", v, q)
+        raise ValueError("v must match k in shape")
+    pages, _, page, _ = _check_cache(k_pages, v_pages, Hkv, d, q, "k")
+    if kv_lens is None:
+        raise TypeError("kv_lens must be a device tensor")
+    _check_each(q, ("q_out", q_out, q.shape, q.dtype), ("slots", slots, (total,), _torch().int64))
+    _call(LIB.monarch_attn_paged_append, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
+          v_pages.data_ptr(), inv_freq.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), *sizes, *strides, ldv,
+          pages, page, bool(interleaved), dtype_code(q.dtype), _stream(q, stream) or None)
+    return q_out, k_pages, v_pages
+
+
+def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=None, done_out=None, eos: int = -1, stream=None):
+    """A step of beam search: of every request's candidates (beam k, token t), of
+    value scores[k] + log_softmax(logits[k])[t], the M largest in order, equal ones
+    by the lowest (k, t).  logits [B, K, V] (rows may be strided; -infinity: not
+    allowed), scores float32 [B, K] (-infinity: a beam not in use); scores_out
+    float32, tokens and parents int32, [B, M] each.  A beam that is `done` (bool
+    [B, K]) offers `eos` at its own score and nothing else; done_out (bool [B, M]):
+    whether the beam was done or the token is eos.  K and M up to BEAM_MAX.
+    Returns (scores_out, tokens, parents), and done_out if it is given."""
+    rt = _torch()
+    try:
+        B, K, V = logits.shape
+        M = tokens.shape[1]
+        x, ld, z = logits.stride()
+        if K == 1:
+            ld = x if B > 1 else V
+        ok = logits.is_cuda and (z == 1 or V == 1) and (B == 1 or x == K * ld)
+        if B * K == 1:
+            ld = max(ld, V)
+    except (AttributeError, ValueError, IndexError):
+        ok = False
+    if not ok:
+        for name, t in (("logits", logits), ("tokens", tokens)):
+            if not isinstance(t, rt.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a device tensor")
+            if t.dim() != (3 if name == "logits" else 2):
+                raise ValueError(f"{name} must have {3 if name == 'logits' else 2} dimensions")
+        raise ValueError("logits must be a [B, K, V] tensor of rows in equal distances, each contiguous")
+    _check_each(logits, ("scores", scores, (B, K), rt.float32), ("scores_out", scores_out, (B, M), rt.float32),
+                ("tokens", tokens, (B, M), rt.int32), ("parents", parents, (B, M), rt.int32))
+    if done is not None:
+        _check_each(logits, ("done", done, (B, K), rt.bool))
+    if done_out is not None:
+        _check_each(logits, ("done_out", done_out, (B, M), rt.bool))
+    _call(LIB.monarch_attn_beam_select, logits, logits.data_ptr(), scores.data_ptr(), _address(done), scores_out.data_ptr(),
+          tokens.data_ptr(), parents.data_ptr(), _address(done_out), B, K, V, M, ld, eos, dtype_code(logits.dtype),
+          _stream(logits, stream) or None)
+    return (scores_out, tokens, parents) if done_out is None else (scores_out, tokens, parents, done_out)
+
+
+def monarch_attn_paged_reorder(k_pages, v_pages, block_table, parents, lens, move_table: bool = True, stream=None):
+    """The paged cache of K beams a request in the order of their parents, in place:
+    beam c of request b (sequence b K + c of block_table, int32 [B K, blocks]) goes on from beam
+    parents[b, c] (int32 [B, K]), with lens (int32 [B K], alike for the beams of a
+    request) tokens in the cache.  Table entries of full pages become the parent's
+    (unless move_table is false: the table is shared by the layers and moved once), the rows of
+    the page begun are copied into the beam's own.  Returns (k_pages, v_pages, block_table)."""
+    rt = _torch()
+    try:
+        B, K = parents.shape
+        rows, blocks = block_table.shape
+        _, heads, _, d = k_pages.shape
+        ok = parents.is_cuda
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok:
+        for name, t, dims in (("parents", parents, 2), ("block_table", block_table, 2), ("k_pages", k_pages, 4)):
+            if not isinstance(t, rt.Tensor) or not t.is_cuda:
+                raise TypeError(f"{name} must be a device tensor")
+            if t.dim() != dims:
+                raise ValueError(f"{name} must have {dims} dimensions")
+    pages, Hkv, page, d = _check_cache(k_pages, v_pages, None, d, k_pages, "itself")
+    int32 = rt.int32
+    _check_each(k_pages, ("parents", parents, (B, K), int32), ("block_table", block_table, (B * K, blocks), int32),
+                ("lens", lens, (B * K,), int32))
+    _call(LIB.monarch_attn_paged_reorder, k_pages, k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), parents.data_ptr(),
+          lens.data_ptr(), B, K, Hkv, d, pages, page, blocks, bool(move_table), dtype_code(k_pages.dtype),
+          _stream(k_pages, stream) or None)
+    return k_pages, v_pages, block_table
 
 
 def monarch_attn_check(N: int, d: int, m: int, b: int, T: int, dtype: int) -> int:
