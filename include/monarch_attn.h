@@ -648,7 +648,7 @@ int monarch_attn_paged_append(const void *q, const void *k, const void *v, void 
  * lowest k V + t first.  Values are formed in 64 bits from sums of fp32 exponentials.  Within a beam
  * the order is that of the logits, also where its score is too large for the sums to differ.
  * K and M up to MONARCH_ATTN_BEAM_MAX, M <= K V, V up to MONARCH_ATTN_BEAM_MAX_VOCAB.
- * Workspace: 8 M + 8 bytes for every 8192 tokens of a beam.
+ * Workspace: up to 8 M + 8 bytes for every 8192 tokens of a beam.
  */
 int monarch_attn_beam_select(const void *logits, const float *scores, const uint8_t *done, float *scores_out, int32_t *tokens,
                              int32_t *parents, uint8_t *done_out, int64_t B, int64_t K, int64_t V, int64_t M, int64_t ld, int32_t eos,

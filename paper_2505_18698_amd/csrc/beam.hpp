@@ -30,196 +30,373 @@ __device__ inline double unordered(uint64_t u) { return __longlong_as_double((in
 // A logit and its token in the order of the candidates of a beam; 0 is behind all of them.
 __device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t)ordered(x) << 32 | (0xffffffffu - token); }
 
-// Of the wave's values the largest one that at least m lanes reach (0 where fewer have one).
+// Of the wave's values one that at least m lanes reach, and no more than the m-th largest is above by
+// 2^-11 of itself (0 where fewer than m have one): its sign, exponent and 11 more bits, one after another.
 __device__ inline uint32_t reached_by(uint32_t x, int m)
 {
     uint32_t t = 0;
-#pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) {
         const uint32_t with = t | 1u << bit;
         if (__popcll(__ballot(x >= with)) >= m) t = with;
     }
     return t;
 }
 
-// One part of a row a workgroup, held in registers: its largest logit, its sum of exponentials and
-// its M best.  Of the lanes' best the M-th of a wave bounds the M-th of the part from below, and the
-// largest such bound of the four waves is reached by few elements: those go to a list, in any order,
-// and each finds its place by counting the larger ones.
+// How many of the first n entries of a list in LDS are larger than `mine`: eight at a time, so that their
+// reads wait for each other no more than once.  (Up to seven behind the n-th are read.)
+template <typename E> __device__ inline int larger_ones(const E *list, int n, const E &mine)
+{
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {
+        E x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = list[j + u];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += j + u < n && x[u] > mine;
+    }
+    return rank;
+}
+
+// The sum over a wave, the same in all lanes.
+template <typename F> __device__ inline float over_wave(float x, F &&f)
+{
+    for (int s = 1; s < 64; s <<= 1) x = f(x, __shfl_xor(x, s));
+    return x;
+}
+
+// A part of a row a workgroup, in chunks of 8192 tokens that are held in registers while the next one
+// arrives: its largest logit, its sum of exponentials and its M best, in order.
+//
+// What reaches a bound goes to a list, in any order, and each entry finds its place by counting the
+// larger ones.  The first chunk's bound: of the lanes' largest logits, the M-th of a wave, of the four
+// waves the largest.  Later on it is the M-th best so far (equal logits come too late), which few
+// exceed.  Where the list is too short all the same (thousands of equal logits, or ascending ones), a search
+// over keys finds a bound that few enough reach.
+//
+// What bounds it: 10 instructions a token, of which the exponential takes four issues, beside 2 bytes.
 template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSelect p)
 {
-    constexpr int VE = 16 / (int)sizeof(T), NV = 32 / VE, E = NV * VE;
-    // A wave's bound is reached by M lanes of it at most, with E elements each.
-    __shared__ uint64_t list[4 * kBeamMax * E];
-    __shared__ uint64_t bounds[4];
+    constexpr int E = 32, VE = 16 / (int)sizeof(T), NV = E / VE, kRoom = 1024;
+    __shared__ __attribute__((aligned(16))) uint64_t list[kRoom + 8], best[kBeamMax];
+    __shared__ uint32_t bounds[4];
     __shared__ float maxima[4], sums[4];
-    __shared__ int count;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int count, found[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % p.parts;
     const int64_t row = blockIdx.x / p.parts;
     if (p.done && p.done[row]) return;
     if (p.scores[row] == -INFINITY) return;
-    if (tid == 0) count = 0;
     const T *x0 = (const T *)p.logits + row * p.ld;
-    // vectors lie at whole 16 bytes, whatever the row does; element e of vector v is token v VE - shift + e
-    const int shift = (int)((uintptr_t)x0 % 16 / sizeof(T));
-    float x[E];
+    // A row starts anywhere in 16 bytes.  Its whole vectors, 16 bytes each, start at token `head`; the few
+    // tokens in front of them belong to the first chunk of the row, those behind to the last, one a thread.
+    const int head = min(p.V, (int)((16 - (uintptr_t)x0 % 16) % 16 / sizeof(T)));
+    const int vectors = (p.V - head) / VE, end = head + vectors * VE;
+    const int first = part * p.part_vectors, behind = min(vectors, first + p.part_vectors);
+    const int chunks = max(1, (behind - first + NV * 256 - 1) / (NV * 256));
+    u32x4 raw[NV];
+    int lone = -1;  // this thread's token in front of the vectors, or behind them
+    T lone_x;
+    auto fetch = [&](int chunk) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int64_t t0 = ((int64_t)(part * NV + i) * 256 + tid) * VE - shift;
-        T y[VE];
-        if (t0 >= 0 && t0 + VE <= p.V) {
-            __builtin_memcpy(y, __builtin_assume_aligned(x0 + t0, 16), 16);
-        } else {
+        for (int i = 0; i < NV; ++i) {
+            const int v = first + (chunk * NV + i) * 256 + tid;
+            T none[VE];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) y[e] = t0 + e >= 0 && t0 + e < p.V ? x0[t0 + e] : (T)-INFINITY;
+            for (int e = 0; e < VE; ++e) none[e] = (T)-INFINITY;
+            __builtin_memcpy(&raw[i], none, 16);
+            if (v < behind) raw[i] = *((const u32x4 *)(x0 + head) + v);
         }
+        lone = -1, lone_x = (T)-INFINITY;
+        if (part == 0 && chunk == 0 && tid < head) lone = tid;
+        if (part == p.parts - 1 && chunk == chunks - 1 && tid >= 64 && end + tid - 64 < p.V) lone = end + tid - 64;
+        if (lone >= 0) lone_x = x0[lone];
+    };
+    fetch(0);
+    if (tid == 0) count = 0;
+    // of this thread's elements: the largest in units of log 2 (NaN stays), and the sum relative to it
+    float most = -INFINITY, sum = 0.f;
+    int kept = 0;                       // entries of the list that are the best so far
+    float bound = -INFINITY;            // with kept = M: the logit of the last of them
+#pragma unroll 1
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        float x[E];
+        bool some[NV];  // of the wave's vectors
 #pragma unroll
-        for (int e = 0; e < VE; ++e) x[i * VE + e] = (float)y[e];
-    }
-    auto token = [&](int j) { return ((part * NV + j / VE) * 256 + tid) * VE - shift + j % VE; };
+        for (int i = 0; i < NV; ++i) {
+            T y[VE];
+            __builtin_memcpy(y, &raw[i], 16);
+            some[i] = first + (chunk * NV + i) * 256 + wave * 64 < behind;
+#pragma unroll
+            for (int e = 0; e < VE; ++e) x[i * VE + e] = (float)y[e];
+        }
+        const float y = (float)lone_x;
+        const int at_y = lone;
+        if (chunk + 1 < chunks) fetch(chunk + 1);
+        const int t0 = head + (first + chunk * NV * 256) * VE;       // the first token of the chunk's vectors
+        const int from = part == 0 && chunk == 0 ? 0 : t0;           // of the chunk
+        auto token = [&](int j) { return t0 + (j / VE * 256 + tid) * VE + j % VE; };
 
-    float most = -INFINITY;
+        float top = y, tops[NV];
 #pragma unroll
-    for (int j = 0; j < E; ++j) most = max_nan(most, x[j]);
-    const float base = fabsf(most) < INFINITY ? most : 0.f;
-    float sum = 0.f;
+        for (int i = 0; i < NV; ++i) {
+            tops[i] = x[i * VE];
 #pragma unroll
-    for (int j = 0; j < E; ++j) sum += __builtin_amdgcn_exp2f((x[j] - base) * kLog2e);
-    uint64_t best = 0;
+            for (int e = 1; e < VE; ++e) tops[i] = max_nan(tops[i], x[i * VE + e]);
+            top = max_nan(top, tops[i]);
+        }
+        const float now = max_nan(most, top * kLog2e), base = fabsf(now) < INFINITY ? now : 0.f;
+        float a = __builtin_amdgcn_exp2f(__builtin_fmaf(y, kLog2e, -base)), b = 0.f;
 #pragma unroll
-    for (int j = E - 1; j >= 0; --j)
-        if (x[j] == most && (uint32_t)token(j) < (uint32_t)p.V) best = key_of(x[j], (uint32_t)token(j));
+        for (int i = 0; i < NV; ++i)
+            if (some[i])
+#pragma unroll
+                for (int e = 0; e < VE; e += 2) {
+                    a += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i * VE + e], kLog2e, -base));
+                    b += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i * VE + e + 1], kLog2e, -base));
+                }
+        sum = sum * (most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most - base)) + (a + b);
+        most = now;
 
-    // (a row of which a logit is NaN or +infinity has no candidates: its keys are not read)
-    float wave_most = most;
-    for (int s = 1; s < 64; s <<= 1) wave_most = max_nan(wave_most, __shfl_xor(wave_most, s));
-    const float wave_base = fabsf(wave_most) < INFINITY ? wave_most : 0.f;
-    sum *= most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((base - wave_base) * kLog2e);
-    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-    uint64_t bound = (uint64_t)reached_by((uint32_t)(best >> 32), p.M) << 32;
-    if (bound && __popcll(__ballot(best >= bound)) > p.M) {  // several lanes with the last one's logit: the lowest tokens
-        const uint32_t hi = (uint32_t)(bound >> 32);
-        const int above = __popcll(__ballot((uint32_t)(best >> 32) > hi));
-        bound |= reached_by((uint32_t)(best >> 32) == hi ? (uint32_t)best : 0u, p.M - above);
+        float low = -INFINITY;  // bound of the first chunk's candidates
+        if (kept == 0) {
+            const uint32_t mine = reached_by(ordered(top), p.M);
+            if (lane == 0) bounds[wave] = mine;
+            __syncthreads();
+            low = unordered(max(max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3])), ordered(-INFINITY)));
+        }
+        uint32_t hits = 0;
+        bool lone_hits = false;
+        if (kept < p.M) {
+            lone_hits = at_y >= 0 && y >= low;
+            if (!(top < low))
+#pragma unroll
+                for (int j = 0; j < E; ++j) hits |= x[j] >= low ? 1u << j : 0u;
+        } else if (!(top <= bound)) {
+            lone_hits = y > bound;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (tops[i] > bound)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) hits |= x[i * VE + e] > bound ? 1u << (i * VE + e) : 0u;
+        }
+        while (hits || lone_hits) {  // few: their logits are read again, for registers cannot be picked by number
+            const int t = lone_hits ? at_y : token(__builtin_ctz(hits));
+            if (!lone_hits) hits &= hits - 1;
+            const bool mine = lone_hits || t < head + behind * VE;
+            lone_hits = false;
+            if (!mine) continue;
+            const float z = (float)x0[t];
+            // (-infinity: of the M first tokens of the chunk alone, which have enough where any is needed)
+            if (z == -INFINITY && t - from >= p.M) continue;
+            const int at = atomicAdd(&count, 1);
+            if (at < kRoom) list[at] = key_of(z, (uint32_t)t);
+        }
+        __syncthreads();
+        int n = count;
+        if (n > kRoom) {
+            // a key that at least M, and no more than the room, reach: bit by bit, from all threads' counts of
+            // the chunk, read again
+            auto reach = [&](int i, uint64_t with) {  // (the last one is the lone token)
+                int t = t0 + i * 256 + tid;
+                if (i == E || t >= head + behind * VE) t = i == E ? at_y : -1;
+                const float z = t >= 0 ? (float)x0[t] : NAN;
+                const uint64_t mine = z == z && (kept == 0 || z > bound) ? key_of(z, (uint32_t)t) : 0;
+                return mine >= with ? mine : 0;
+            };
+            uint64_t key = 0;
+#pragma unroll 1
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t with = key | 1ull << bit;
+                int c = 0;
+#pragma unroll 4
+                for (int i = 0; i <= E; ++i) c += reach(i, with) != 0;
+                for (int s = 1; s < 64; s <<= 1) c += __shfl_xor(c, s);
+                __syncthreads();
+                if (lane == 0) found[wave] = c;
+                __syncthreads();
+                c = found[0] + found[1] + found[2] + found[3];
+                if (c >= p.M) key = with;
+                if (c >= p.M && c <= kRoom - kBeamMax) break;
+            }
+            if (tid == 0) count = kept;
+            __syncthreads();
+#pragma unroll 1
+            for (int i = 0; i <= E; ++i)
+                if (const uint64_t mine = reach(i, key)) {
+                    const int at = atomicAdd(&count, 1);
+                    if (at < kRoom) list[at] = mine;
+                }
+            __syncthreads();
+            n = min(count, kRoom);
+        }
+        if (n > kept) {
+            for (int i = tid; i < n; i += 256) {
+                const uint64_t mine = list[i];
+                const int rank = larger_ones(list, n, mine);
+                if (rank < p.M) best[rank] = mine;
+            }
+            __syncthreads();
+            kept = min(n, p.M);
+            if (tid < kept) list[tid] = best[tid];
+            if (tid == 0) count = kept;
+            if (kept == p.M) bound = unordered((uint32_t)(best[p.M - 1] >> 32));
+            __syncthreads();
+        }
     }
-    if (lane == 0) bounds[wave] = bound, maxima[wave] = wave_most, sums[wave] = sum;
+
+    const float wave_most = over_wave(most, [](float a, float b) { return max_nan(a, b); });
+    const float base = fabsf(wave_most) < INFINITY ? wave_most : 0.f;
+    sum = over_wave(sum * (most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most - base)), [](float a, float b) { return a + b; });
+    if (lane == 0) maxima[wave] = wave_most, sums[wave] = sum;
     __syncthreads();
-    bound = max(max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3])), (uint64_t)1);
-    if (tid == 0) {
+    // (a row of which a logit is NaN or +infinity has no candidates: its keys are not read)
+    uint64_t *out = p.keys + (int64_t)blockIdx.x * p.M;
+    if (tid < p.M) out[tid] = tid < kept ? list[tid] : 0;
+    if (tid == 64) {
         float m = maxima[0], s = 0.f;
         for (int i = 1; i < 4; ++i) m = max_nan(m, maxima[i]);
-        for (int i = 0; i < 4; ++i) s += sums[i] * (maxima[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((maxima[i] - m) * kLog2e));
+        for (int i = 0; i < 4; ++i) s += sums[i] * (maxima[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(maxima[i] - m));
         p.part_max[blockIdx.x] = m, p.part_sum[blockIdx.x] = s;
     }
-    if (best >= bound) {
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const uint32_t t = (uint32_t)token(j);
-            if (t < (uint32_t)p.V && key_of(x[j], t) >= bound) list[atomicAdd(&count, 1)] = key_of(x[j], t);
-        }
-    }
-    __syncthreads();
-    uint64_t *out = p.keys + (int64_t)blockIdx.x * p.M;
-    const int n = count;
-    for (int i = tid; i < n; i += 256) {
-        const uint64_t mine = list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > mine;
-        if (rank < p.M) out[rank] = mine;
-    }
-    if (tid >= n && tid < p.M) out[tid] = 0;
 }
 
 // One request a workgroup: every beam's sum from its parts, in 64 bits, so that candidates of
-// different beams that are close to each other come out in order; then the M best of the parts' lists, all of which are
-// in order: only the lists of the M best first entries count, and of these the entries that reach
-// the last of them.
+// different beams that are close to each other come out in order; then the M best of the parts'
+// lists.  All of these are in order: of more than 1024 entries, only the M lists of the best first
+// ones count.  A bound as in beam_parts leaves few entries, each of which finds its place by
+// counting the larger ones.  What bounds it: the way to memory and back, once where the lists are short.
 struct BeamEntry {
-    uint64_t value, at;  // ordered(candidate); ~(beam V + token), so that both are "more is first"
-    __device__ inline bool operator>(const BeamEntry &o) const { return value > o.value || (value == o.value && at > o.at); }
+    double value;  // the candidate, or -infinity
+    uint32_t at;   // beam V + token; kNoEntry: none
+    __device__ inline bool operator>(const BeamEntry &o) const { return value > o.value || (value == o.value && at < o.at); }
 };
+constexpr uint32_t kNoEntry = 0xffffffffu;
+static_assert((uint64_t)kBeamMax * MONARCH_ATTN_BEAM_MAX_VOCAB < kNoEntry, "candidates have 32-bit numbers");
+struct BeamHead {
+    BeamEntry e;
+    int list;
+    __device__ inline bool operator>(const BeamHead &o) const { return e > o.e; }
+};
+// The upper half of ordered(value), by which entries are bounded; 0: none.
+__device__ inline uint32_t height(const BeamEntry &e) { return e.at == kNoEntry ? 0 : (uint32_t)(ordered(e.value) >> 32); }
+
+// A height that M of the workgroup's values at least reach, from the waves' own ones (1 where no wave has M).
+__device__ inline uint32_t bound_of(uint32_t x, int m, uint32_t *shared)
+{
+    const uint32_t mine = reached_by(x, m);
+    if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = mine;
+    __syncthreads();
+    return max(max(max(shared[0], shared[1]), max(shared[2], shared[3])), 1u);
+}
 
 static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
 {
+    constexpr int kAhead = 1024;  // keys that are on their way before the sums are known
+    constexpr int kEach = kAhead / 256;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    BeamEntry *heads = reinterpret_cast<BeamEntry *>(lds);  // of the lists; one behind them: the bound
-    __shared__ BeamEntry list[kBeamMax * kBeamMax];
-    __shared__ double lse[kBeamMax];
+    BeamHead *heads = reinterpret_cast<BeamHead *>(lds);  // of the lists, where there are many
+    __shared__ BeamEntry list[kAhead + 8];
+    __shared__ double lse[kBeamMax], score_of[kBeamMax];
     __shared__ int kind[kBeamMax];  // of a beam: 0 candidates by its logits, 1 done, 2 all of them -infinity
-    __shared__ int open[kBeamMax];  // lists that count
-    __shared__ int opened, count;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int open[kBeamMax];  // the lists that count
+    __shared__ uint32_t bounds[2][4];
+    __shared__ int count, tops;
+    static_assert(kBeamMax * kBeamMax <= kAhead, "entries of the lists that count");
+    const int tid = threadIdx.x;
     const int64_t row0 = (int64_t)blockIdx.x * p.K;
-    const int lists = p.K * p.parts;
-    if (tid == 0) opened = 0, count = 0;
-    for (int k = wave; k < p.K; k += 4) {
+    const int lists = p.K * p.parts, all = lists * p.M;
+    const uint64_t *keys = p.keys + row0 * p.parts * p.M;
+    const bool whole = all <= kAhead;  // else the lists' first entries come first
+    uint64_t key[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) key[j] = keys[whole ? min(tid + 256 * j, all - 1) : min(tid + 256 * j, lists - 1) * p.M];
+    if (tid == 0) count = 0, tops = 0;
+    const int width = p.K <= 4 ? 64 : p.K <= 8 ? 32 : p.K <= 16 ? 16 : 8;  // threads a beam
+    if (const int k = tid / width, i0 = tid % width; k < p.K) {
         const int64_t row = row0 + k;
-        const float score = p.scores[row];
+        const float *maxima = p.part_max + row * p.parts, *sums = p.part_sum + row * p.parts;
+        // (a beam that is done or not in use has written nothing there: what is read is not taken)
+        const float m0 = i0 < p.parts ? maxima[i0] : -INFINITY, s0 = i0 < p.parts ? sums[i0] : 0.f, score = p.scores[row];
         const bool dead = !(score > -INFINITY), ended = p.done && p.done[row];
-        float most = -INFINITY;
-        double sum = 0.0;
-        if (!dead && !ended) {
-            for (int i = lane; i < p.parts; i += 64) most = max_nan(most, p.part_max[row * p.parts + i]);
-            for (int s = 1; s < 64; s <<= 1) most = max_nan(most, __shfl_xor(most, s));
-            if (fabsf(most) < INFINITY)
-                for (int i = lane; i < p.parts; i += 64)
-                    sum += (double)p.part_sum[row * p.parts + i] * exp((double)p.part_max[row * p.parts + i] - (double)most);
-            for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-        }
-        if (lane == 0) {
-            kind[k] = dead ? 2 : ended ? 1 : fabsf(most) < INFINITY ? 0 : 2;
-            lse[k] = (double)most + log(sum);
+        float most = m0;
+        for (int i = i0 + width; i < p.parts; i += width) most = max_nan(most, maxima[i]);
+        for (int s = 1; s < width; s <<= 1) most = max_nan(most, __shfl_xor(most, s));
+        const bool fine = fabsf(most) < INFINITY;
+        double sum = s0 * exp2((double)m0 - (double)most);
+        for (int i = i0 + width; i < p.parts; i += width) sum += (double)sums[i] * exp2((double)maxima[i] - (double)most);
+        for (int s = 1; s < width; s <<= 1) sum += __shfl_xor(sum, s);
+        if (i0 == 0) {
+            kind[k] = dead ? 2 : ended ? 1 : fine ? 0 : 2;
+            // (in the unit that the exponentials had, kLog2e in 32 bits: off by 2e-8 of the row's entropy)
+            lse[k] = ((double)most + log2(sum)) / (double)kLog2e;
+            score_of[k] = score;
         }
     }
     __syncthreads();
-    // entry i of a list, or one behind all others
-    auto entry = [&](int l, int i) {
-        const int k = l / p.parts, part = l - k * p.parts;
-        const double score = p.scores[row0 + k];
-        BeamEntry e{0, 0};
+    // entry i of list l, of that key, or none
+    auto entry = [&](int l, int i, uint64_t key) {
+        const int k = l / p.parts;
+        BeamEntry e{-(double)INFINITY, kNoEntry};
         if (kind[k] == 0) {
-            const uint64_t key = p.keys[((row0 + k) * p.parts + part) * p.M + i];
             if (key == 0) return e;
-            const double x = score + ((double)unordered((uint32_t)(key >> 32)) - lse[k]);
-            e.value = ordered(x == x ? x : -INFINITY);
-            e.at = ~((uint64_t)k * p.V + (0xffffffffu - (uint32_t)key));
-        } else if (part == 0 && i < p.V) {
+            const double x = score_of[k] + ((double)unordered((uint32_t)(key >> 32)) - lse[k]);
+            if (x == x) e.value = x;
+            e.at = (uint32_t)(k * p.V) + (0xffffffffu - (uint32_t)key);
+        } else if (l == k * p.parts && i < p.V) {
             const bool first = kind[k] == 1 && i == 0;  // done: the end token, then the others, in front of it and behind it
             const int t = kind[k] == 2 ? i : first ? p.eos : i - 1 < p.eos ? i - 1 : i;
-            e.value = ordered(first ? score : -(double)INFINITY);
-            e.at = ~((uint64_t)k * p.V + t);
+            if (first) e.value = score_of[k];
+            e.at = (uint32_t)(k * p.V + t);
         }
         return e;
     };
-    for (int l = tid; l < lists; l += 256) heads[l] = entry(l, 0);
-    if (tid == 0) heads[lists] = BeamEntry{0, 0};
-    __syncthreads();
-    for (int l = tid; l < lists; l += 256) {
-        const BeamEntry mine = heads[l];
-        if (mine.value == 0) continue;
-        int rank = 0;
-        for (int j = 0; j < lists; ++j) rank += heads[j] > mine;
-        if (rank < p.M) open[atomicAdd(&opened, 1)] = l;
-        if (rank == p.M - 1) heads[lists] = mine;
+    BeamEntry mine[kEach];
+    uint32_t top = 0;
+    auto take = [&](int some, auto &&list_of, auto &&number_of) {  // the entries of this thread's keys
+        top = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int x = tid + 256 * j;
+            mine[j] = BeamEntry{-(double)INFINITY, kNoEntry};
+            if (256 * j < some && x < some) mine[j] = entry(list_of(x), number_of(x), key[j]);
+            top = max(top, height(mine[j]));
+        }
+    };
+    if (whole) {
+        take(all, [&](int x) { return x / p.M; }, [&](int x) { return x % p.M; });
+    } else {
+        take(lists, [](int x) { return x; }, [](int) { return 0; });
+        const uint32_t low = bound_of(top, p.M, bounds[0]);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (height(mine[j]) >= low) heads[atomicAdd(&tops, 1)] = BeamHead{mine[j], tid + 256 * j};
+        __syncthreads();
+        const int n = tops;
+        for (int i = tid; i < n; i += 256) {
+            const int rank = larger_ones(heads, n, heads[i]);
+            if (rank < p.M) open[rank] = heads[i].list;
+        }
+        __syncthreads();
+        const int some = min(n, p.M) * p.M;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (const int x = tid + 256 * j; x < some) key[j] = keys[open[x / p.M] * p.M + x % p.M];
+        take(some, [&](int x) { return open[x / p.M]; }, [&](int x) { return x % p.M; });
     }
-    __syncthreads();
-    const BeamEntry bound = heads[lists];
-    for (int i = tid; i < opened * p.M; i += 256) {
-        const BeamEntry e = entry(open[i / p.M], i % p.M);
-        if (e.value != 0 && !(bound > e)) list[atomicAdd(&count, 1)] = e;
-    }
+    const uint32_t low = bound_of(top, p.M, bounds[1]);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (height(mine[j]) >= low) list[atomicAdd(&count, 1)] = mine[j];
     __syncthreads();
     const int n = count;
     for (int i = tid; i < n; i += 256) {
-        const BeamEntry mine = list[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > mine;
+        const BeamEntry e = list[i];
+        const int rank = larger_ones(list, n, e);
         if (rank >= p.M) continue;
-        const uint64_t at = ~mine.at;
-        const int k = (int)(at / (uint32_t)p.V), t = (int)(at % (uint32_t)p.V);
+        const int k = (int)(e.at / (uint32_t)p.V), t = (int)(e.at % (uint32_t)p.V);
         const int64_t to = (int64_t)blockIdx.x * p.M + rank;
-        p.scores_out[to] = (float)unordered(mine.value);
+        p.scores_out[to] = (float)e.value;
         p.tokens[to] = t, p.parents[to] = k;
         if (p.done_out) p.done_out[to] = (p.done && p.done[row0 + k]) || t == p.eos;
     }

@@ -33,19 +33,19 @@ int run_rotate(Launcher &L, const ma::Rotate &p, int32_t dtype, bool append)
 
 int run_beam_select(Launcher &L, const ma::BeamSelect &p, int32_t dtype)
 {
-    const dim3 grid((unsigned)((int64_t)p.B * p.K * p.parts)), block(256);
+    const dim3 grid((unsigned)((int64_t)p.B * p.K * p.parts));
     const int rc = L.run(kBeamParts, [&] {
         return launched([&] {
             switch (dtype) {
-            case MA_F32: ma::beam_parts<float><<<grid, block, 0, L.stream>>>(p); break;
-            case MA_BF16: ma::beam_parts<__bf16><<<grid, block, 0, L.stream>>>(p); break;
-            default: ma::beam_parts<_Float16><<<grid, block, 0, L.stream>>>(p); break;
+            case MA_F32: ma::beam_parts<float><<<grid, dim3(256), 0, L.stream>>>(p); break;
+            case MA_BF16: ma::beam_parts<__bf16><<<grid, dim3(256), 0, L.stream>>>(p); break;
+            default: ma::beam_parts<_Float16><<<grid, dim3(256), 0, L.stream>>>(p); break;
             }
         });
     });
     if (rc != MA_OK) return rc;
-    const size_t lds = (size_t)(p.K * p.parts + 1) * sizeof(ma::BeamEntry);
-    return L.run(kBeamJoin, [&] { return launched([&] { ma::beam_join<<<dim3((unsigned)p.B), block, lds, L.stream>>>(p); }); });
+    const size_t lds = ((size_t)p.K * p.parts + 8) * sizeof(ma::BeamHead);
+    return L.run(kBeamJoin, [&] { return launched([&] { ma::beam_join<<<dim3((unsigned)p.B), dim3(256), lds, L.stream>>>(p); }); });
 }
 
 int run_paged_reorder(Launcher &L, const ma::PagedReorder &p)

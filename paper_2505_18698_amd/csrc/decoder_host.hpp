@@ -31,9 +31,9 @@ struct BeamSelect {
     uint8_t *done_out;      // [B, M] or null
     int64_t ld;
     int B, K, V, M, eos;
-    int parts;              // parts of a row
+    int parts, part_vectors;  // parts of a row, and 16-byte vectors a part
     uint64_t *keys;         // [B K, parts, M] the best of every part, as keys
-    float *part_max, *part_sum;  // [B K, parts] its largest logit and the sum of exp(logit - largest)
+    float *part_max, *part_sum;  // [B K, parts] its largest logit in units of log 2 and the sum of exp(logit - largest)
 };
 
 struct PagedReorder {
@@ -54,9 +54,6 @@ constexpr int kBeamMax = MONARCH_ATTN_BEAM_MAX;
 namespace ma_host {
 
 enum DecoderKind { kRotate = 17, kBeamParts = 18, kBeamJoin = 19, kReorder = 20 };
-
-// Elements of a row that a workgroup of the selection takes.
-constexpr int kBeamPart = 256 * 32;
 
 int run_rotate(Launcher &L, const ma::Rotate &p, int32_t dtype, bool append);
 int run_beam_select(Launcher &L, const ma::BeamSelect &p, int32_t dtype);

@@ -144,6 +144,28 @@ def test_concentrated(ma, M):
         assert torch.equal(at, want)
 
 
+@pytest.mark.parametrize("kind", ["random", "up", "down", "equal", "few allowed", "last only"])
+def test_many_rows(ma, kind):
+    """Rows of several chunks a workgroup: later chunks against the best so far."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    B, K, V, M = 64, 8, 39999, 32
+    step = torch.arange(float(V), device="cuda") / 4096
+    x = {"random": lambda: torch.randn(B, K, V, generator=gen, device="cuda"), "up": lambda: step.expand(B, K, V).contiguous(),
+         "down": lambda: -step.expand(B, K, V).contiguous(), "equal": lambda: torch.full((B, K, V), -2.5, device="cuda"),
+         "few allowed": lambda: torch.randn(B, K, V, generator=gen, device="cuda").masked_fill(
+             torch.rand(B, K, V, generator=gen, device="cuda") < 0.9998, -math.inf),
+         "last only": lambda: torch.full((B, K, V), -math.inf, device="cuda").index_fill(2, torch.tensor([V - 2], device="cuda"), 1.0)}[kind]()
+    scores = -torch.arange(float(K), device="cuda").expand(B, K).contiguous() / 3
+    out, tokens, parents, _ = got = _select(ma, x, scores, M)
+    _check(tuple(t if t is None else t[:3] for t in got), x[:3], scores[:3], M)
+    want = _candidates(x, scores, None, -1).flatten(1).sort(dim=1, descending=True, stable=True)
+    best = want.values[:, :M]
+    finite = torch.isfinite(best)
+    assert torch.equal(torch.isfinite(out), finite) and bool((torch.where(finite, out - best, 0.0).abs() <= 2 * CLOSE + 2.0 ** -24 * 40).all())
+    if kind != "random":
+        assert torch.equal(parents.long() * V + tokens.long(), want.indices[:, :M])
+
+
 def test_first_step_and_dead_beams(ma):
     """Only the first beam in use; none; beams without an allowed token, with NaN or with +infinity."""
     gen = torch.Generator(device="cuda").manual_seed(4)
