@@ -477,8 +477,8 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  *                keys (clamped to 0..their number), as in a padded batch.  The others are not read.
  * Every row sees all keys of its sequence; rows of a sequence without keys get a
  * zero output and lse -infinity.  The lengths of queries and keys are independent.
- * Workspace: as in monarch_attn_exact_paged_fwd, where the mean number of keys a sequence is more
- * than a quarter of the tokens given there.
+ * Workspace: as in monarch_attn_exact_paged_fwd, where the mean number of keys a sequence (of a padded
+ * batch half the width) is more than that given there.
  */
 int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
                                  const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total,
@@ -491,8 +491,8 @@ int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, vo
  * out, dout, dq : [total, Hq, d], contiguous; dk, dv: [total_k, Hkv, d], contiguous.
  * dk and dv are zero in the rows behind k_lens[i] of a sequence, and of sequences without
  * queries.  Rows of no sequence (by cu_q, by cu_k) are left, or with clear written as zero.
- * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a key row and key head), and up to three
- * fp32 copies of dk and dv.
+ * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a key row and key head), and where
+ * there are few walks for the device up to eight fp32 copies of dk and dv, or of dq.
  */
 int monarch_attn_exact_cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
                                  const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_q, const int32_t *cu_k,

@@ -152,7 +152,7 @@ int packed_bwd(const void *q, const void *k, const void *v, const void *out, con
     p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each);
     if (dtype == MA_F16) p.norm_g = (float *)(c.ws + 2 * each), p.norm_v = (float *)(c.ws + 3 * each);
     p.stat_blocks = (int)std::min<int64_t>(kStatBlocks, (total + 15) / 16 * Hq);
-    p.pieces = (int)pieces;
+    p.pieces = (int)pieces, p.pieces_q = 1;
     p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;
     return run_launches(stream, BwdLaunch::run, &x);
@@ -251,12 +251,21 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     return run_launches(stream, FwdLaunch::run, &x);
 }
 
-// The split of a cross call: that of a paged one, by the keys that its longest sequence may have. The
-// host knows how many there are in all: the longest one is taken for four times the mean one.
-PagedSplit cross_split(int64_t total, int64_t total_k, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t num_cus, int32_t dtype)
+// The split of a cross call: that of a paged one, by the mean number of keys, which is what the host
+// knows of them (of a padded batch half the width).  Many rows, whose steps take longer, are split from a quarter
+// of that on where there are few tiles of them for the device, or few for long walks.  (Whole and split, bf16. Four rows a sequence, 12 heads of 64: 32
+// sequences of 300 to 500 keys 12 and 19 us, of 100 to 1500 18 and 24. Many rows: 12 sequences of up to 400
+// rows over up to 1500 keys, 16 heads on 4 of 128: 40 and 47 us; 24 of up to 512 over up to 2048, 12 heads of
+// 64: 39 and 43; 64 of up to 512 over up to 1000, 16 heads: 115 and 138; 8 of up to 1024 over up to 8192, 16 heads on 4
+// of 128: 174 and 137; 512 over 8192: 130 and 55. fp32, 16 of up to 300 over up to 1000, 12 heads of 64: 83 and 67.)
+PagedSplit cross_split(int64_t total, int64_t total_k, bool padded, int64_t B, int64_t G, int64_t Hkv, int64_t d, int64_t num_cus, int32_t dtype)
 {
-    const int64_t longest = std::min(total_k, 4 * ((total_k + B - 1) / std::max<int64_t>(1, B)));
-    return paged_split(total, B, G, Hkv, d, longest, num_cus, dtype);
+    const int64_t mean = (total_k + std::max<int64_t>(1, B) - 1) / std::max<int64_t>(1, B) / (padded ? 2 : 1);
+    const bool few = paged_rows(total, B, G, dtype) == kSeqFewRows;
+    PagedSplit s = paged_split(total, B, G, Hkv, d, few ? mean : std::min(total_k, 4 * mean), num_cus, dtype);
+    const bool long_walks = mean > (dtype == MA_F32 ? 128 : 1024);
+    if (s.split && !few && 4 * s.tiles >= (long_walks ? 8 : 3) * s.units) s.split = false, s.units = s.tiles;
+    return s;
 }
 
 int check_cross(int64_t B, int64_t total, int64_t total_k, int64_t Hq, int64_t Hkv, int64_t d, int64_t ldq, int64_t ldk,
@@ -292,7 +301,7 @@ int cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
     MA_TRY(begin_call(c));
-    PagedSplit s = cross_split(total, total_k, B, G, Hkv, d, c.num_cus, dtype);
+    PagedSplit s = cross_split(total, total_k, k_lens != nullptr, B, G, Hkv, d, c.num_cus, dtype);
     if (s.split && B > 0) {
         MA_TRY(check_grid(s.units, Hkv));
         MA_TRY(call_workspace(stream, s.bytes_o + s.bytes_l + s.bytes_parts, c));
@@ -313,6 +322,22 @@ int cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse
     x.how = SeqPlan{ma::kCross, s.split, s.rows, s.units};
     x.dtype = dtype;
     return run_launches(stream, FwdLaunch::run, &x);
+}
+
+// Pieces of the walks of a cross call's gradient. A key tile walks the rows of its sequence, a row tile the
+// keys, in steps of 4 and 3 products: where the mean walk is longer than what a workgroup's share of all steps
+// is (two workgroups a compute unit), it is cut.  (bf16, the whole gradient: 512 rows of 16 heads on 4 of 128
+// over 8192 keys: 151 us, dQ in one piece 182, in 8 144; 2 sequences of 4096 rows over up to 512 keys: 150 us
+// with 8 pieces of dK and dV, 186 with 4, 520 with one; 8 of up to 1024 over up to 8192: 400 us in one piece each, 430 in two.)
+struct CrossPieces {
+    int64_t keys, rows;
+};
+CrossPieces cross_pieces(int64_t B, int64_t total, int64_t total_k, int64_t tiles_q, int64_t tiles_k, int64_t Hkv, int64_t G, int64_t num_cus)
+{
+    const double n = std::max<int64_t>(1, B), walk_k = 4.0 * (double)G * total / n / kSeqBwdKeys, walk_q = 3.0 * total_k / n / kSeqBwdKeys;
+    const double share = (walk_k * tiles_k + walk_q * tiles_q) * Hkv / (2.0 * num_cus);
+    auto cut = [&](double walk) { return (int64_t)std::max(1.0, std::min(8.0, std::ceil(walk / std::max(share, 16.0)))); };
+    return CrossPieces{cut(walk_k), cut(walk_q)};
 }
 
 int cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest, const void *dout,
@@ -342,12 +367,13 @@ int cross_bwd(const void *q, const void *k, const void *v, const void *out, cons
     MA_TRY(check_overlaps(outs, ins));
     CallScope c;
     MA_TRY(begin_call(c));
-    const int64_t pieces = bwd_pieces(total, tiles_k, Hkv, G, c.num_cus);
-    const size_t part = pieces > 1 ? (size_t)(pieces * total_k * Hkv) * tile_d(d) * 4 : 0;
+    const CrossPieces pieces = cross_pieces(B, total, total_k, tiles_q, tiles_k, Hkv, G, c.num_cus);
+    const size_t part = pieces.keys > 1 ? (size_t)(pieces.keys * total_k * Hkv) * tile_d(d) * 4 : 0;
+    const size_t part_q = pieces.rows > 1 ? (size_t)(pieces.rows * total * Hq) * tile_d(d) * 4 : 0;
     const size_t each = stat_bytes_of(total, Hq), norms = dtype == MA_F16 ? each + stat_bytes_of(total_k, Hkv) : 0;
     const size_t stat_bytes = 2 * each + norms;
-    MA_TRY(check_grid(tiles_k * pieces + tiles_q, Hkv));
-    MA_TRY(call_workspace(stream, stat_bytes + 2 * part, c));
+    MA_TRY(check_grid(tiles_k * pieces.keys + tiles_q * pieces.rows, Hkv));
+    MA_TRY(call_workspace(stream, stat_bytes + 2 * part + part_q, c));
     BwdLaunch x{};
     ma::SeqBwd &p = x.p;
     p.q = q, p.k = k, p.v = v, p.out = out, p.dout = dout, p.lse = lse, p.rest = rest;
@@ -361,7 +387,8 @@ int cross_bwd(const void *q, const void *k, const void *v, const void *out, cons
     p.lse2 = (float *)c.ws, p.delta = (float *)(c.ws + each);
     if (dtype == MA_F16) p.norm_g = (float *)(c.ws + 2 * each), p.norm_v = (float *)(c.ws + 3 * each);
     p.stat_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(kStatBlocks, (std::max(total * G, total_k) + 15) / 16 * Hkv));
-    p.pieces = (int)pieces;
+    p.pieces = (int)pieces.keys, p.pieces_q = (int)pieces.rows;
+    p.part_q = (float *)(c.ws + stat_bytes + 2 * part);
     p.part_k = (float *)(c.ws + stat_bytes), p.part_v = (float *)(c.ws + stat_bytes + part);
     x.dtype = dtype;
     return run_launches(stream, BwdLaunch::run, &x);

@@ -144,8 +144,9 @@ template <typename T, int D, int WR, Keys KEYS, bool SPLIT> struct SeqAttn {
     static_assert(WR * KW <= W, "rows and keys over the waves");
     static constexpr int TILE = BN * S::ROW;
     // Tiles that are there or on their way.  Short contexts of few rows are bound
-    // by the latency of one tile after another: up to four, as the room allows.
-    static constexpr int STAGES = WR != 1 || S::kF32 ? 2 : SPLIT ? (D <= 64 ? 4 : 2) : D <= 64 ? 3 : 2;
+    // by the latency of one tile after another: up to four, as the room allows.  (Cross attention: two, and two
+    // workgroups a compute unit; 64 sequences of 4 rows over up to 100 keys, 12 heads of 64: 10 us, 15 with three.)
+    static constexpr int STAGES = WR != 1 || S::kF32 || (KEYS == kCross && !SPLIT) ? 2 : SPLIT ? (D <= 64 ? 4 : 2) : D <= 64 ? 3 : 2;
     static constexpr int LDS_BYTES = 2 * STAGES * TILE + 16;  // K and V
     using Copy = TileCopy<T, D, BN, W>;
     // A row's weights are taken relative to a reference that follows its running maximum only when

@@ -212,7 +212,8 @@ template <typename T, int D, Keys KEYS> struct SeqBwdQ {
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
         const int kvh = uniform(block % p.Hkv);
-        const int64_t t = p.tiles_q - 1 - block / p.Hkv;  // later rows see more keys: they start first
+        const int pieces = KEYS == kCross ? p.pieces_q : 1, piece = uniform(block / p.Hkv % pieces);
+        const int64_t t = p.tiles_q - 1 - block / p.Hkv / pieces;  // later rows see more keys: they start first
         const int seq = uniform(seq_of_tile(p.seqs, t, p.G, R, lane));
         if (seq < 0) return;
         const int tile = uniform((int)(t - tile0(p.seqs, seq, p.G, R)));
@@ -220,7 +221,11 @@ template <typename T, int D, Keys KEYS> struct SeqBwdQ {
         const int key_row0 = KEYS == kCross ? uniform(p.keys.start(seq)) : row0, keys = KEYS == kCross ? uniform(p.keys.count(seq)) : n;
         const int rows = n * p.G, r0 = tile * R, tok0 = r0 / p.G;
         auto visible = [&](int r) { return p.causal ? min(r, rows - 1) / p.G + 1 : keys; };
-        const int see_all = uniform(visible(r0)), last = uniform(visible(r0 + R - 1));
+        // the keys of this piece, whole tiles of them but for the last one's
+        const int steps = (uniform(visible(r0 + R - 1)) + BN - 1) / BN;
+        const int begin = KEYS == kCross ? uniform((int)((int64_t)steps * piece / pieces)) * BN : 0;
+        const int see_all = uniform(visible(r0));
+        const int last = KEYS == kCross ? min(see_all, uniform((int)((int64_t)steps * (piece + 1) / pieces)) * BN) : uniform(visible(r0 + R - 1));
         const int wr0 = r0 + wave % WR * 32, part = wave / WR * 32 * KT;
         const int see_most = uniform(visible(wr0 + 31));
 
@@ -240,7 +245,7 @@ template <typename T, int D, Keys KEYS> struct SeqBwdQ {
         const float lse2 = p.lse2[at], delta = p.delta[at];
         float scale = 1.f;  // of this row's dS
         if constexpr (BwdScale<T>::kScaled) {
-            float most = BwdScale<T>::template own_largest<NTH>(p.norm_v + (int64_t)kvh * (KEYS == kCross ? p.keys : p.seqs).total + key_row0, last, 1, 0), none = 0.f;
+            float most = BwdScale<T>::template own_largest<NTH>(p.norm_v + (int64_t)kvh * (KEYS == kCross ? p.keys : p.seqs).total + key_row0, KEYS == kCross ? keys : last, 1, 0), none = 0.f;
             BwdScale<T>::template all_largest<NTH>(most, none, lds);
             scale = BwdScale<T>::of(p.norm_g[at], most);
         }
@@ -259,8 +264,8 @@ template <typename T, int D, Keys KEYS> struct SeqBwdQ {
         f32x16 dq[S::ND];
 #pragma unroll
         for (int dt = 0; dt < S::ND; ++dt) dq[dt] = f32x16{};
-        bring(0, 0);
-        int key0 = 0, buf = 0;
+        bring(begin, 0);
+        int key0 = begin, buf = 0;
         // (a copy of the step for each buffer: its LDS addresses are constants)
         const int whole = min(see_all, last) - BN;
         auto unmasked = [&](int b) {
@@ -296,8 +301,15 @@ template <typename T, int D, Keys KEYS> struct SeqBwdQ {
 #pragma unroll
                 for (int i = 0; i < S::ND * 16; ++i) dq[i / 16][i % 16] += sh[(((w - 1) * WR + wave) * S::ND * 16 + i) * 64];
         }
+        const float by = vis == 1 ? 0.f : p.c * kLn2 / scale;
+        if constexpr (KEYS == kCross)
+            if (pieces > 1) {
+                const Span ps(p.part_q + ((int64_t)piece * p.seqs.total + row0 + tok0) * Hq * D);
+                store_row<float, S::ND>(ps, dq, by, (tok * Hq + head) * D, D, wr0 + (lane & 31) < rows, lane);
+                return;
+            }
         const Span os((T *)p.dq + (int64_t)(row0 + tok0) * Hq * p.d);
-        store_row<T, S::ND>(os, dq, vis == 1 ? 0.f : p.c * kLn2 / scale, (tok * Hq + head) * p.d, p.d, wr0 + (lane & 31) < rows, lane);
+        store_row<T, S::ND>(os, dq, by, (tok * Hq + head) * p.d, p.d, wr0 + (lane & 31) < rows, lane);
     }
 };
 
@@ -558,10 +570,25 @@ template <typename T, int D, Keys KEYS> __global__ __launch_bounds__(256, sizeof
         K::run(p, lds, block - blocks_q);
 }
 
-// The pieces' sums of dK and dV added up, four columns a thread.
+// The pieces' sums added up, four columns a thread: dK and dV, and of cross attention dQ.
 template <typename T, int D, Keys KEYS> __global__ __launch_bounds__(256) void seq_bwd_join(SeqBwd p)
 {
     constexpr int C = D / 4;
+    if constexpr (KEYS == kCross) {
+        const int Hq = p.Hkv * p.G;
+        const int64_t first = (int64_t)p.seqs.start(0) * Hq, rows = p.pieces_q == 1 ? 0 : (int64_t)p.seqs.start(p.seqs.B) * Hq - first;
+        const int64_t each = (int64_t)p.seqs.total * Hq * D;
+        for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * C; i += (int64_t)gridDim.x * 256) {
+            const int64_t row = first + i / C;
+            const int col = (int)(i % C) * 4;
+            if (col >= p.d) continue;
+            const float *q = p.part_q + row * D + col;
+            f32x4 a = *(const f32x4 *)q;
+            for (int x = 1; x < p.pieces_q; ++x) a += *(const f32x4 *)(q + x * each);
+            store4<T>((T *)p.dq + row * p.d + col, a);
+        }
+        if (p.pieces == 1) return;
+    }
     const Seqs &keys = KEYS == kCross ? p.keys : p.seqs;
     const int64_t first = (int64_t)keys.start(0) * p.Hkv, rows = (int64_t)keys.start(keys.B) * p.Hkv - first;
     const int64_t each = (int64_t)keys.total * p.Hkv * D;

@@ -15,13 +15,14 @@ template <typename T, int D, ma::Keys KEYS> int run_seq_bwd_d(Launcher &L, const
         return launched([&] { ma::seq_stats<T, KEYS><<<dim3((unsigned)p.stat_blocks), block, 0, L.stream>>>(p); });
     });
     if (rc != MA_OK) return rc;
-    const int blocks_q = (int)((int64_t)p.tiles_q * p.Hkv), blocks_k = (int)((int64_t)p.tiles_k * p.pieces * p.Hkv);
+    const int blocks_q = (int)((int64_t)p.tiles_q * p.pieces_q * p.Hkv), blocks_k = (int)((int64_t)p.tiles_k * p.pieces * p.Hkv);
     rc = L.run(kSeqBwd, [&] {
         return launched([&] { ma::seq_bwd<T, D, KEYS><<<dim3((unsigned)blocks_q + (unsigned)blocks_k), block, 0, L.stream>>>(p, blocks_q); });
     });
-    if (rc != MA_OK || p.pieces == 1) return rc;
+    if (rc != MA_OK || (p.pieces == 1 && p.pieces_q == 1)) return rc;
     // at most 8 workgroups a compute unit
-    const int64_t blocks = std::min<int64_t>(2048, ((int64_t)(KEYS == ma::kCross ? p.keys : p.seqs).total * p.Hkv * (D / 4) + 255) / 256);
+    const int64_t rows = std::max((int64_t)(KEYS == ma::kCross ? p.keys : p.seqs).total * p.Hkv, p.pieces_q == 1 ? 0 : (int64_t)p.seqs.total * p.Hkv * p.G);
+    const int64_t blocks = std::min<int64_t>(2048, (rows * (D / 4) + 255) / 256);
     return L.run(kSeqBwdJoin, [&] { return launched([&] { ma::seq_bwd_join<T, D, KEYS><<<dim3((unsigned)blocks), block, 0, L.stream>>>(p); }); });
 }
 

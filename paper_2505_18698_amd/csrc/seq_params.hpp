@@ -81,6 +81,10 @@ struct SeqBwd {
     // dK and dV of every piece, row and key head, in rows of the tile width
     int pieces;
     float *part_k, *part_v;
+    // cross: pieces that the keys of a row tile are cut into; with more than one, dQ of every piece, row
+    // and head, in rows of the tile width
+    int pieces_q;
+    float *part_q;
 };
 
 struct PagedPlan {
