@@ -239,8 +239,12 @@ def _stream(q, stream):
 
 def _call(fn, q, *args):
     """fn(*args) with q's device current; raises on a failure status."""
-    rt = _torch()
-    index = q.device.index
+    _call_on(q.device.index, fn, *args)
+
+
+def _call_on(index, fn, *args):
+    """fn(*args) with that device current; raises on a failure status."""
+    rt = _TORCH or _torch()
     if rt.current_device() == index:
         rc = fn(*args)
     else:
@@ -451,6 +455,23 @@ def _is(t, shape, dtype, device):
     return t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous()
 
 
+def _are(index, *tensors):
+    """Whether each (tensor, shape, dtype) is a contiguous tensor of that kind on the device of that index."""
+    for t, shape, dtype in tensors:
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+            return False
+    return True
+
+
+def _fit(t, rows, heads, d, dtype, index):
+    """The row stride of t, if it is [rows, heads, d] of that kind with the heads of a row adjacent, else -1."""
+    if t.dtype is dtype and t.shape == (rows, heads, d) and t.get_device() == index:
+        x, y, z = t.stride()
+        if (z == 1 or d == 1) and (y == d or heads == 1):
+            return x if rows > 1 else heads * d
+    return -1
+
+
 def _check_rows(name, t, like, like_name="q"):
     """Raise unless t is [rows, heads, d] on the device and of the dtype of `like`, the heads of a row adjacent."""
     if not isinstance(t, _torch().Tensor) or not t.is_cuda:
@@ -558,7 +579,8 @@ def _packed_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_seqlens, causal, rest, c
 
 def _whole(t):
     """t, contiguous and 16-byte aligned."""
-    t = t.contiguous()
+    if not t.is_contiguous():
+        t = t.contiguous()
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
@@ -624,14 +646,11 @@ def _check_cross(q, k, v, cu_q, cu_k, k_lens):
     """Sizes (B, total, total_k, Hq, Hkv, d) and row strides of q [total, Hq, d], k and v [total_k, Hkv, d]."""
     rt = _torch()
     try:
-        total, Hq, d = q.shape
-        total_k, Hkv, _ = k.shape
-        (B,) = cu_q.shape
-        dtype, device, int32 = q.dtype, q.device, rt.int32
-        ldq, ldk, ldv = _rows(q, dtype, device), _rows(k, dtype, device), _rows(v, dtype, device)
-        if q.is_cuda and ldq >= 0 and ldk >= 0 and ldv >= 0 and k.shape == v.shape and k.shape[2] == d and B > 0 \
-                and _is(cu_q, (B,), int32, device) and _is(cu_k, (B,), int32, device) \
-                and (k_lens is None or _is(k_lens, (B - 1,), int32, device)):
+        (total, Hq, d), (total_k, Hkv, _), (B,) = q.shape, k.shape, cu_q.shape
+        dtype, index, int32 = q.dtype, q.get_device(), rt.int32
+        ldq, ldk, ldv = _fit(q, total, Hq, d, dtype, index), _fit(k, total_k, Hkv, d, dtype, index), _fit(v, total_k, Hkv, d, dtype, index)
+        if index >= 0 and ldq >= 0 and ldk >= 0 and ldv >= 0 and B > 0 and _are(index, (cu_q, (B,), int32), (cu_k, (B,), int32)) \
+                and (k_lens is None or _are(index, (k_lens, (B - 1,), int32))):
             return (B - 1, total, total_k, Hq, Hkv, d), (ldq, ldk, ldv)
     except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
         pass
@@ -674,8 +693,10 @@ def _address(t):
 
 
 def _cross_fwd(q, k, v, out, cu_q, cu_k, k_lens, lse, rest, clear, stream, dims):
-    _call(LIB.monarch_attn_exact_cross_fwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _address(lse), _address(rest),
-          cu_q.data_ptr(), cu_k.data_ptr(), _address(k_lens), *dims, bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
+    index = q.get_device()
+    _call_on(index, LIB.monarch_attn_exact_cross_fwd, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _address(lse),
+             _address(rest), cu_q.data_ptr(), cu_k.data_ptr(), _address(k_lens), *dims, bool(clear), dtype_code(q.dtype),
+             (_TORCH.current_stream(index) if stream is None else _stream(q, stream)) or None)
 
 
 def monarch_attn_exact_cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, k_lens=None, rest=None, clear: bool = False,
@@ -695,9 +716,11 @@ def monarch_attn_exact_cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k
 
 
 def _cross_bwd(q, k, v, out, lse, dout, dq, dk, dv, cu_q, cu_k, k_lens, rest, clear, stream, dims):
-    _call(LIB.monarch_attn_exact_cross_bwd, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), _address(rest),
-          dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), _address(k_lens), *dims,
-          bool(clear), dtype_code(q.dtype), _stream(q, stream) or None)
+    index = q.get_device()
+    _call_on(index, LIB.monarch_attn_exact_cross_bwd, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+             None if rest is None else rest.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), cu_q.data_ptr(),
+             cu_k.data_ptr(), None if k_lens is None else k_lens.data_ptr(), *dims, bool(clear), _TORCH.codes[q.dtype],
+             (_TORCH.current_stream(index) if stream is None else _stream(q, stream)) or None)
 
 
 _CROSS_FN = None
@@ -708,6 +731,15 @@ def _cross_function():
     global _CROSS_FN
     if _CROSS_FN is None:
         import torch
+
+        def grads(ctx, dout):
+            q, k, v, out, lse, cu_q, cu_k, k_lens, rest = ctx.saved_tensors
+            dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(k.shape)
+            _cross_bwd(q, k, v, out, lse, _whole(dout), dq, dk, dv, cu_q, cu_k, k_lens, rest, True, None, ctx.dims)
+            return dq, dk, dv, None, None, None
+
+        # (a graph of the gradient, which is refused when it is used, takes 10 us more)
+        once = torch.autograd.function.once_differentiable(grads)
 
         class ExactCrossAttentionFn(torch.autograd.Function):
             @staticmethod
@@ -723,12 +755,8 @@ def _cross_function():
                 return out
 
             @staticmethod
-            @torch.autograd.function.once_differentiable
             def backward(ctx, dout):
-                q, k, v, out, lse, cu_q, cu_k, k_lens, rest = ctx.saved_tensors
-                dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
-                _cross_bwd(q, k, v, out, lse, _whole(dout), dq, dk, dv, cu_q, cu_k, k_lens, rest, True, None, ctx.dims)
-                return dq, dk, dv, None, None, None
+                return once(ctx, dout) if torch.is_grad_enabled() else grads(ctx, dout)
 
         _CROSS_FN = ExactCrossAttentionFn
     return _CROSS_FN
@@ -861,14 +889,13 @@ def _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens):
     """Sizes (B, total, Hq, Hk, d, rot) and row strides of q [total, Hq, d] and k [total, Hk, d] or None."""
     rt = _torch()
     try:
-        total, Hq, d = q.shape
-        Hk = 0 if k is None else k.shape[1]
+        (total, Hq, d), Hk = q.shape, 0 if k is None else k.shape[1]
         (B,), (pairs,) = cu_seqlens.shape, inv_freq.shape
-        dtype, device, int32 = q.dtype, q.device, rt.int32
-        ldq, ldk = _rows(q, dtype, device), 0 if k is None else _rows(k, dtype, device)
-        if q.is_cuda and ldq >= 0 and ldk >= 0 and (k is None or k.shape == (total, Hk, d)) and B > 0 \
-                and _is(cu_seqlens, (B,), int32, device) and _is(inv_freq, (pairs,), rt.float32, device) \
-                and (kv_lens is None or _is(kv_lens, (B - 1,), int32, device)):
+        dtype, index = q.dtype, q.get_device()
+        ldq, ldk = _fit(q, total, Hq, d, dtype, index), 0 if k is None else _fit(k, total, Hk, d, dtype, index)
+        if index >= 0 and ldq >= 0 and ldk >= 0 and B > 0 \
+                and _are(index, (cu_seqlens, (B,), rt.int32), (inv_freq, (pairs,), rt.float32)) \
+                and (kv_lens is None or _are(index, (kv_lens, (B - 1,), rt.int32))):
             return (B - 1, total, Hq, Hk, d, 2 * pairs), (ldq, ldk)
     except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
         pass
@@ -906,9 +933,10 @@ def monarch_attn_rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, kv_lens=None, 
 
 
 def _rotate(q, k, q_out, k_out, inv_freq, cu_seqlens, kv_lens, interleaved, inverse, clear, stream, dims):
-    _call(LIB.monarch_attn_rotate, q, q.data_ptr(), _address(k), q_out.data_ptr(), None if k is None else k_out.data_ptr(),
-          inv_freq.data_ptr(), cu_seqlens.data_ptr(), _address(kv_lens), *dims, bool(interleaved), bool(inverse), bool(clear),
-          dtype_code(q.dtype), _stream(q, stream) or None)
+    index = q.get_device()
+    _call_on(index, LIB.monarch_attn_rotate, q.data_ptr(), None if k is None else k.data_ptr(), q_out.data_ptr(),
+             None if k is None else k_out.data_ptr(), inv_freq.data_ptr(), cu_seqlens.data_ptr(), _address(kv_lens), *dims, bool(interleaved),
+             bool(inverse), bool(clear), dtype_code(q.dtype), (_TORCH.current_stream(index) if stream is None else _stream(q, stream)) or None)
 
 
 _ROTATE_FN = None
@@ -919,6 +947,15 @@ def _rotate_function():
     global _ROTATE_FN
     if _ROTATE_FN is None:
         import torch
+
+        def grads(ctx, g, h):
+            (inv_freq, cu_seqlens), (interleaved, sizes) = ctx.saved_tensors, ctx.call
+            g, h = _whole(g), _whole(h)
+            dq, dk = g.new_empty(g.shape), h.new_empty(h.shape)
+            _rotate(g, h, dq, dk, inv_freq, cu_seqlens, None, interleaved, True, True, None, sizes + (sizes[2] * sizes[4], sizes[3] * sizes[4]))
+            return dq, dk, None, None, None
+
+        once = torch.autograd.function.once_differentiable(grads)
 
         class RotatePackedFn(torch.autograd.Function):
             @staticmethod
@@ -932,14 +969,8 @@ def _rotate_function():
                 return q_out, k_out
 
             @staticmethod
-            @torch.autograd.function.once_differentiable
             def backward(ctx, dq_out, dk_out):
-                (inv_freq, cu_seqlens), (interleaved, sizes) = ctx.saved_tensors, ctx.call
-                g, h = _in_rows(dq_out), _in_rows(dk_out)
-                dq, dk = g.new_empty(g.shape), h.new_empty(h.shape)
-                strides = _rows(g, g.dtype, g.device), _rows(h, g.dtype, g.device)
-                _rotate(g, h, dq, dk, inv_freq, cu_seqlens, None, interleaved, True, True, None, sizes + strides)
-                return dq, dk, None, None, None
+                return once(ctx, dq_out, dk_out) if torch.is_grad_enabled() else grads(ctx, dq_out, dk_out)
 
         _ROTATE_FN = RotatePackedFn
     return _ROTATE_FN
@@ -961,8 +992,24 @@ def monarch_attn_paged_append(q, k, v, q_out, k_pages, v_pages, inv_freq, cu_seq
     turned into their slots (int64 [total], -1: nowhere) of k_pages
     [pages, Hkv, page, d], of v as they are into v_pages.  cu_seqlens, kv_lens and
     slots as monarch_attn_paged_plan makes them.  Returns (q_out, k_pages, v_pages)."""
-    sizes, strides = _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens)
-    B, total, Hq, Hkv, d, rot = sizes
+    rt = _TORCH or _torch()
+    try:  # (a short call is bound by these checks: one pass, without names)
+        (total, Hq, d), index, dtype = q.shape, q.get_device(), q.dtype
+        pages, Hkv, page, _ = cache = k_pages.shape
+        (B,), (pairs,) = kv_lens.shape, inv_freq.shape
+        ldq, ldk, ldv = _fit(q, total, Hq, d, dtype, index), _fit(k, total, Hkv, d, dtype, index), _fit(v, total, Hkv, d, dtype, index)
+        if index >= 0 and ldq >= 0 and ldk >= 0 and ldv >= 0 and cache[3] == d and _are(
+                index, (q_out, (total, Hq, d), dtype), (k_pages, cache, dtype), (v_pages, cache, dtype), (inv_freq, (pairs,), rt.float32),
+                (cu_seqlens, (B + 1,), rt.int32), (kv_lens, (B,), rt.int32), (slots, (total,), rt.int64)):
+            _call_on(index, LIB.monarch_attn_paged_append, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
+                     v_pages.data_ptr(), inv_freq.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), B, total, Hq, Hkv,
+                     d, 2 * pairs, ldq, ldk, ldv, pages, page, bool(interleaved), dtype_code(dtype),
+                     (rt.current_stream(index) if stream is None else _stream(q, stream)) or None)
+            return q_out, k_pages, v_pages
+    except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
+        pass
+    sizes, _ = _check_rotation(q, k, inv_freq, cu_seqlens, kv_lens)
+    _, total, Hq, Hkv, d, _ = sizes
     if k is None:
         raise TypeError("k must be a device tensor")
     try:
@@ -972,14 +1019,11 @@ def monarch_attn_paged_append(q, k, v, q_out, k_pages, v_pages, inv_freq, cu_seq
     if ldv < 0:
         _check_rows("v", v, q)
         raise ValueError("v must match k in shape")
-    pages, _, page, _ = _check_cache(k_pages, v_pages, Hkv, d, q, "k")
+    _check_cache(k_pages, v_pages, Hkv, d, q, "k")
     if kv_lens is None:
         raise TypeError("kv_lens must be a device tensor")
     _check_each(q, ("q_out", q_out, q.shape, q.dtype), ("slots", slots, (total,), _torch().int64))
-    _call(LIB.monarch_attn_paged_append, q, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
-          v_pages.data_ptr(), inv_freq.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), *sizes, *strides, ldv,
-          pages, page, bool(interleaved), dtype_code(q.dtype), _stream(q, stream) or None)
-    return q_out, k_pages, v_pages
+    raise ValueError("all tensors must be device tensors")
 
 
 def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=None, done_out=None, eos: int = -1, stream=None):
@@ -991,24 +1035,30 @@ def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=N
     [B, K]) offers `eos` at its own score and nothing else; done_out (bool [B, M]):
     whether the beam was done or the token is eos.  K and M up to BEAM_MAX.
     Returns (scores_out, tokens, parents), and done_out if it is given."""
-    rt = _torch()
-    try:
-        B, K, V = logits.shape
+    rt = _TORCH or _torch()
+    try:  # (one pass without names, as above)
+        (B, K, V), index = logits.shape, logits.get_device()
         M = tokens.shape[1]
         x, ld, z = logits.stride()
         if K == 1:
             ld = x if B > 1 else V
-        ok = logits.is_cuda and (z == 1 or V == 1) and (B == 1 or x == K * ld)
-        if B * K == 1:
-            ld = max(ld, V)
+        rows = (z == 1 or V == 1) and (B == 1 or x == K * ld)
+        out = (B, M)
+        if rows and index >= 0 and _are(index, (scores, (B, K), rt.float32), (scores_out, out, rt.float32), (tokens, out, rt.int32),
+                                        (parents, out, rt.int32)) \
+                and (done is None or _are(index, (done, (B, K), rt.bool))) and (done_out is None or _are(index, (done_out, out, rt.bool))):
+            _call_on(index, LIB.monarch_attn_beam_select, logits.data_ptr(), scores.data_ptr(), None if done is None else done.data_ptr(),
+                     scores_out.data_ptr(), tokens.data_ptr(), parents.data_ptr(), None if done_out is None else done_out.data_ptr(), B, K, V,
+                     M, ld, eos, dtype_code(logits.dtype), (rt.current_stream(index) if stream is None else _stream(logits, stream)) or None)
+            return (scores_out, tokens, parents) if done_out is None else (scores_out, tokens, parents, done_out)
     except (AttributeError, ValueError, IndexError):
-        ok = False
-    if not ok:
-        for name, t in (("logits", logits), ("tokens", tokens)):
-            if not isinstance(t, rt.Tensor) or not t.is_cuda:
-                raise TypeError(f"{name} must be a device tensor")
-            if t.dim() != (3 if name == "logits" else 2):
-                raise ValueError(f"{name} must have {3 if name == 'logits' else 2} dimensions")
+        rows = False
+    for name, t, dims in (("logits", logits, 3), ("tokens", tokens, 2)):
+        if not isinstance(t, rt.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        if t.dim() != dims:
+            raise ValueError(f"{name} must have {dims} dimensions")
+    if not rows:
         raise ValueError("logits must be a [B, K, V] tensor of rows in equal distances, each contiguous")
     _check_each(logits, ("scores", scores, (B, K), rt.float32), ("scores_out", scores_out, (B, M), rt.float32),
                 ("tokens", tokens, (B, M), rt.int32), ("parents", parents, (B, M), rt.int32))
@@ -1016,10 +1066,7 @@ def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=N
         _check_each(logits, ("done", done, (B, K), rt.bool))
     if done_out is not None:
         _check_each(logits, ("done_out", done_out, (B, M), rt.bool))
-    _call(LIB.monarch_attn_beam_select, logits, logits.data_ptr(), scores.data_ptr(), _address(done), scores_out.data_ptr(),
-          tokens.data_ptr(), parents.data_ptr(), _address(done_out), B, K, V, M, ld, eos, dtype_code(logits.dtype),
-          _stream(logits, stream) or None)
-    return (scores_out, tokens, parents) if done_out is None else (scores_out, tokens, parents, done_out)
+    raise ValueError("all tensors must be device tensors")
 
 
 def monarch_attn_paged_reorder(k_pages, v_pages, block_table, parents, lens, move_table: bool = True, stream=None):
@@ -1029,28 +1076,28 @@ def monarch_attn_paged_reorder(k_pages, v_pages, block_table, parents, lens, mov
     request) tokens in the cache.  Table entries of full pages become the parent's
     (unless move_table is false: the table is shared by the layers and moved once), the rows of
     the page begun are copied into the beam's own.  Returns (k_pages, v_pages, block_table)."""
-    rt = _torch()
-    try:
-        B, K = parents.shape
-        rows, blocks = block_table.shape
-        _, heads, _, d = k_pages.shape
-        ok = parents.is_cuda
-    except (AttributeError, ValueError):
-        ok = False
-    if not ok:
-        for name, t, dims in (("parents", parents, 2), ("block_table", block_table, 2), ("k_pages", k_pages, 4)):
-            if not isinstance(t, rt.Tensor) or not t.is_cuda:
-                raise TypeError(f"{name} must be a device tensor")
-            if t.dim() != dims:
-                raise ValueError(f"{name} must have {dims} dimensions")
-    pages, Hkv, page, d = _check_cache(k_pages, v_pages, None, d, k_pages, "itself")
-    int32 = rt.int32
-    _check_each(k_pages, ("parents", parents, (B, K), int32), ("block_table", block_table, (B * K, blocks), int32),
-                ("lens", lens, (B * K,), int32))
-    _call(LIB.monarch_attn_paged_reorder, k_pages, k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), parents.data_ptr(),
-          lens.data_ptr(), B, K, Hkv, d, pages, page, blocks, bool(move_table), dtype_code(k_pages.dtype),
-          _stream(k_pages, stream) or None)
-    return k_pages, v_pages, block_table
+    rt = _TORCH or _torch()
+    try:  # (one pass without names, as above)
+        (B, K), index, dtype = parents.shape, k_pages.get_device(), k_pages.dtype
+        blocks = block_table.shape[1]
+        pages, Hkv, page, d = cache = k_pages.shape
+        if index >= 0 and _are(index, (k_pages, cache, dtype), (v_pages, cache, dtype), (parents, (B, K), rt.int32),
+                               (block_table, (B * K, blocks), rt.int32), (lens, (B * K,), rt.int32)):
+            _call_on(index, LIB.monarch_attn_paged_reorder, k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), parents.data_ptr(),
+                     lens.data_ptr(), B, K, Hkv, d, pages, page, blocks, bool(move_table), dtype_code(dtype),
+                     (rt.current_stream(index) if stream is None else _stream(k_pages, stream)) or None)
+            return k_pages, v_pages, block_table
+    except (AttributeError, ValueError, IndexError):
+        pass
+    for name, t, dims in (("parents", parents, 2), ("block_table", block_table, 2), ("k_pages", k_pages, 4)):
+        if not isinstance(t, rt.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        if t.dim() != dims:
+            raise ValueError(f"{name} must have {dims} dimensions")
+    _check_cache(k_pages, v_pages, None, k_pages.shape[3], k_pages, "itself")
+    _check_each(k_pages, ("parents", parents, tuple(parents.shape), rt.int32),
+                ("block_table", block_table, (parents.numel(), block_table.shape[1]), rt.int32), ("lens", lens, (parents.numel(),), rt.int32))
+    raise ValueError("all tensors must be device tensors")
 
 
 def monarch_attn_check(N: int, d: int, m: int, b: int, T: int, dtype: int) -> int:
