@@ -30,13 +30,13 @@ __device__ inline double unordered(uint64_t u) { return __longlong_as_double((in
 // A logit and its token in the order of the candidates of a beam; 0 is behind all of them.
 __device__ inline uint64_t key_of(float x, uint32_t token) { return (uint64_t)ordered(x) << 32 | (0xffffffffu - token); }
 
-// Of the wave's values one that at least m lanes reach, and no more than the m-th largest is above by
-// 2^-11 of itself (0 where fewer than m have one): its sign, exponent and 11 more bits, one after another.
-__device__ inline uint32_t reached_by(uint32_t x, int m)
+// Of the wave's values the m-th largest, but for its lower `LOW` bits (0 where fewer than m have one): at
+// least m lanes reach it.
+template <int LOW> __device__ inline uint32_t reached_by(uint32_t x, int m)
 {
     uint32_t t = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 12; --bit) {
+    for (int bit = 31; bit >= LOW; --bit) {
         const uint32_t with = t | 1u << bit;
         if (__popcll(__ballot(x >= with)) >= m) t = with;
     }
@@ -81,7 +81,9 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
     __shared__ __attribute__((aligned(16))) uint64_t list[kRoom + 8], best[kBeamMax];
     __shared__ uint32_t bounds[4];
     __shared__ float maxima[4], sums[4];
-    __shared__ int count, found[4];
+    // entries of the list, of this chunk and of the next one: a wave may be there before the others have
+    // read how many this one has
+    __shared__ int counts[2], found[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % p.parts;
     const int64_t row = blockIdx.x / p.parts;
@@ -113,13 +115,14 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
         if (lone >= 0) lone_x = x0[lone];
     };
     fetch(0);
-    if (tid == 0) count = 0;
+    if (tid == 0) counts[0] = counts[1] = 0;
     // of this thread's elements: the largest in units of log 2 (NaN stays), and the sum relative to it
     float most = -INFINITY, sum = 0.f;
     int kept = 0;                       // entries of the list that are the best so far
     float bound = -INFINITY;            // with kept = M: the logit of the last of them
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk) {
+        int &count = counts[chunk & 1];
         float x[E];
         bool some[NV];  // of the wave's vectors
 #pragma unroll
@@ -160,7 +163,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
 
         float low = -INFINITY;  // bound of the first chunk's candidates
         if (kept == 0) {
-            const uint32_t mine = reached_by(ordered(top), p.M);
+            const uint32_t mine = reached_by<12>(ordered(top), p.M);  // (11 bits behind the exponent are enough)
             if (lane == 0) bounds[wave] = mine;
             __syncthreads();
             low = unordered(max(max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3])), ordered(-INFINITY)));
@@ -239,7 +242,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
             __syncthreads();
             kept = min(n, p.M);
             if (tid < kept) list[tid] = best[tid];
-            if (tid == 0) count = kept;
+            if (tid == 0) counts[0] = counts[1] = kept;
             if (kept == p.M) bound = unordered((uint32_t)(best[p.M - 1] >> 32));
             __syncthreads();
         }
@@ -284,7 +287,7 @@ __device__ inline uint32_t height(const BeamEntry &e) { return e.at == kNoEntry 
 // A height that M of the workgroup's values at least reach, from the waves' own ones (1 where no wave has M).
 __device__ inline uint32_t bound_of(uint32_t x, int m, uint32_t *shared)
 {
-    const uint32_t mine = reached_by(x, m);
+    const uint32_t mine = reached_by<0>(x, m);
     if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = mine;
     __syncthreads();
     return max(max(max(shared[0], shared[1]), max(shared[2], shared[3])), 1u);
