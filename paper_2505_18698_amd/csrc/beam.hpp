@@ -77,13 +77,11 @@ template <typename F> __device__ inline float over_wave(float x, F &&f)
 // What bounds it: 10 instructions a token, of which the exponential takes four issues, beside 2 bytes.
 template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSelect p)
 {
-    constexpr int E = 32, VE = 16 / (int)sizeof(T), NV = E / VE, kRoom = 1024;
+    constexpr int E = 32, VE = 16 / (int)sizeof(T), NV = E / VE, kRoom = 1024, kMany = 256;
     __shared__ __attribute__((aligned(16))) uint64_t list[kRoom + 8], best[kBeamMax];
     __shared__ uint32_t bounds[4];
     __shared__ float maxima[4], sums[4];
-    // entries of the list, of this chunk and of the next one: a wave may be there before the others have
-    // read how many this one has
-    __shared__ int counts[2], found[4];
+    __shared__ int count, found[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = blockIdx.x % p.parts;
     const int64_t row = blockIdx.x / p.parts;
@@ -115,14 +113,13 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
         if (lone >= 0) lone_x = x0[lone];
     };
     fetch(0);
-    if (tid == 0) counts[0] = counts[1] = 0;
+    if (tid == 0) count = 0;
     // of this thread's elements: the largest in units of log 2 (NaN stays), and the sum relative to it
     float most = -INFINITY, sum = 0.f;
-    int kept = 0;                       // entries of the list that are the best so far
+    int kept = 0, listed = 0;           // entries of the list that are the best so far, in order, and all
     float bound = -INFINITY;            // with kept = M: the logit of the last of them
 #pragma unroll 1
     for (int chunk = 0; chunk < chunks; ++chunk) {
-        int &count = counts[chunk & 1];
         float x[E];
         bool some[NV];  // of the wave's vectors
 #pragma unroll
@@ -197,6 +194,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
         }
         __syncthreads();
         int n = count;
+        __syncthreads();  // (all have read it before the next chunk adds to it)
         if (n > kRoom) {
             // a key that at least M, and no more than the room, reach: bit by bit, from all threads' counts of
             // the chunk, read again
@@ -220,9 +218,9 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
                 __syncthreads();
                 c = found[0] + found[1] + found[2] + found[3];
                 if (c >= p.M) key = with;
-                if (c >= p.M && c <= kRoom - kBeamMax) break;
+                if (c >= p.M && c <= kRoom - kMany) break;
             }
-            if (tid == 0) count = kept;
+            if (tid == 0) count = listed;
             __syncthreads();
 #pragma unroll 1
             for (int i = 0; i <= E; ++i)
@@ -233,7 +231,8 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
             __syncthreads();
             n = min(count, kRoom);
         }
-        if (n > kept) {
+        // (a few chunks' entries are put in order together: 2 us a chunk less)
+        if (n > kept && (kept < p.M || n > kMany || chunk == chunks - 1)) {
             for (int i = tid; i < n; i += 256) {
                 const uint64_t mine = list[i];
                 const int rank = larger_ones(list, n, mine);
@@ -242,10 +241,12 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
             __syncthreads();
             kept = min(n, p.M);
             if (tid < kept) list[tid] = best[tid];
-            if (tid == 0) counts[0] = counts[1] = kept;
+            n = kept;
+            if (tid == 0) count = kept;
             if (kept == p.M) bound = unordered((uint32_t)(best[p.M - 1] >> 32));
             __syncthreads();
         }
+        listed = n;
     }
 
     const float wave_most = over_wave(most, [](float a, float b) { return max_nan(a, b); });
