@@ -608,6 +608,7 @@ int monarch_attn_paged_write(const void *k, const void *v, void *k_pages, void *
  * kv_lens     : NULL: a row's position is its number in its sequence.  Else [B] device int32: the
  *               rows of sequence i are the last of its kv_lens[i] tokens, as in
  *               monarch_attn_exact_paged_fwd (a position before the first token is negative).
+ * total times Hq, or Hk, is below 2^31, else MA_EUNSUPPORTED.  No workspace.
  */
 int monarch_attn_rotate(const void *q, const void *k, void *q_out, void *k_out, const float *inv_freq, const int32_t *cu_seqlens,
                         const int32_t *kv_lens, int64_t B, int64_t total, int64_t Hq, int64_t Hk, int64_t d, int64_t rot,
@@ -617,7 +618,8 @@ int monarch_attn_rotate(const void *q, const void *k, void *q_out, void *k_out, 
  * monarch_attn_paged_append -- monarch_attn_rotate and monarch_attn_paged_write in one
  * pass: the rows of q turned into q_out, those of k turned into their slots of k_pages, those of v
  * into v_pages.  cu_seqlens and kv_lens (not NULL) as monarch_attn_paged_plan makes them.
- * Rows of no sequence are not written anywhere, rows without a slot not into pages.
+ * Rows of no sequence are not written anywhere, rows without a slot not into pages.  Slots must
+ * differ from each other, as there.  No workspace.
  */
 int monarch_attn_paged_append(const void *q, const void *k, const void *v, void *q_out, void *k_pages, void *v_pages,
                               const float *inv_freq, const int32_t *cu_seqlens, const int32_t *kv_lens, const int64_t *slots,
@@ -635,7 +637,7 @@ int monarch_attn_paged_append(const void *q, const void *k, const void *v, void 
  *
  * logits    : [B, K, V], rows ld elements apart (any ld >= V; aligned to their element only).
  *             -infinity: a token that is not allowed.
- * scores    : [B, K] device floats, the beams' sums so far; -infinity: a beam that is not in
+ * scores    : [B, K] device floats, the beams' sums so far, finite, or -infinity: a beam that is not in
  *             use (as all but the first are at the start).
  * done      : NULL, or [B, K] bytes: a beam that has ended offers the token eos, at its own
  *             score, and nothing else.
@@ -668,7 +670,7 @@ int monarch_attn_beam_select(const void *logits, const float *scores, const uint
  *              ones, as monarch_attn_paged_plan gives them.
  * One call a layer, of which only one moves the table that the layers share.  A
  * page keeps being that of the sequence for which the plan took it: give the pages of a request back when all of
- * its beams have ended.
+ * its beams have ended.  B up to 65535.  No workspace.
  */
 int monarch_attn_paged_reorder(void *k_pages, void *v_pages, int32_t *block_table, const int32_t *parents, const int32_t *lens,
                                int64_t B, int64_t K, int64_t Hkv, int64_t d, int64_t pages, int64_t page, int64_t blocks,
