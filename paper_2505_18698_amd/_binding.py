@@ -993,6 +993,8 @@ def monarch_attn_paged_append(q, k, v, q_out, k_pages, v_pages, inv_freq, cu_seq
     [pages, Hkv, page, d], of v as they are into v_pages.  cu_seqlens, kv_lens and
     slots as monarch_attn_paged_plan makes them.  Returns (q_out, k_pages, v_pages)."""
     rt = _TORCH or _torch()
+    if stream is not None:
+        stream = _stream(q, stream)
     try:  # (a short call is bound by these checks: one pass, without names)
         (total, Hq, d), index, dtype = q.shape, q.get_device(), q.dtype
         pages, Hkv, page, _ = cache = k_pages.shape
@@ -1004,7 +1006,7 @@ def monarch_attn_paged_append(q, k, v, q_out, k_pages, v_pages, inv_freq, cu_seq
             _call_on(index, LIB.monarch_attn_paged_append, q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_pages.data_ptr(),
                      v_pages.data_ptr(), inv_freq.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), slots.data_ptr(), B, total, Hq, Hkv,
                      d, 2 * pairs, ldq, ldk, ldv, pages, page, bool(interleaved), dtype_code(dtype),
-                     (rt.current_stream(index) if stream is None else _stream(q, stream)) or None)
+                     (rt.current_stream(index) if stream is None else stream) or None)
             return q_out, k_pages, v_pages
     except (AttributeError, ValueError, IndexError):  # no tensor, or not of these dimensions
         pass
@@ -1036,6 +1038,8 @@ def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=N
     whether the beam was done or the token is eos.  K and M up to BEAM_MAX.
     Returns (scores_out, tokens, parents), and done_out if it is given."""
     rt = _TORCH or _torch()
+    if stream is not None:
+        stream = _stream(logits, stream)
     try:  # (one pass without names, as above)
         (B, K, V), index = logits.shape, logits.get_device()
         M = tokens.shape[1]
@@ -1049,7 +1053,7 @@ def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=N
                 and (done is None or _are(index, (done, (B, K), rt.bool))) and (done_out is None or _are(index, (done_out, out, rt.bool))):
             _call_on(index, LIB.monarch_attn_beam_select, logits.data_ptr(), scores.data_ptr(), None if done is None else done.data_ptr(),
                      scores_out.data_ptr(), tokens.data_ptr(), parents.data_ptr(), None if done_out is None else done_out.data_ptr(), B, K, V,
-                     M, ld, eos, dtype_code(logits.dtype), (rt.current_stream(index) if stream is None else _stream(logits, stream)) or None)
+                     M, ld, eos, dtype_code(logits.dtype), (rt.current_stream(index) if stream is None else stream) or None)
             return (scores_out, tokens, parents) if done_out is None else (scores_out, tokens, parents, done_out)
     except (AttributeError, ValueError, IndexError):
         rows = False
@@ -1077,6 +1081,8 @@ def monarch_attn_paged_reorder(k_pages, v_pages, block_table, parents, lens, mov
     (unless move_table is false: the table is shared by the layers and moved once), the rows of
     the page begun are copied into the beam's own.  Returns (k_pages, v_pages, block_table)."""
     rt = _TORCH or _torch()
+    if stream is not None:
+        stream = _stream(k_pages, stream)
     try:  # (one pass without names, as above)
         (B, K), index, dtype = parents.shape, k_pages.get_device(), k_pages.dtype
         blocks = block_table.shape[1]
@@ -1085,7 +1091,7 @@ def monarch_attn_paged_reorder(k_pages, v_pages, block_table, parents, lens, mov
                                (block_table, (B * K, blocks), rt.int32), (lens, (B * K,), rt.int32)):
             _call_on(index, LIB.monarch_attn_paged_reorder, k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), parents.data_ptr(),
                      lens.data_ptr(), B, K, Hkv, d, pages, page, blocks, bool(move_table), dtype_code(dtype),
-                     (rt.current_stream(index) if stream is None else _stream(k_pages, stream)) or None)
+                     (rt.current_stream(index) if stream is None else stream) or None)
             return k_pages, v_pages, block_table
     except (AttributeError, ValueError, IndexError):
         pass

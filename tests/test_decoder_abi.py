@@ -174,3 +174,17 @@ def test_binding_of_the_reordering(change, message):
              parents=torch.zeros(2, 3, dtype=torch.int32), lens=torch.zeros(6, dtype=torch.int32)) | change
     with pytest.raises(ValueError, match=message):
         ma.monarch_attn_paged_reorder(**{n: _on_device(t)[0] for n, t in x.items()})
+
+
+@pytest.mark.parametrize("call", ["append", "selection", "reordering"])
+def test_what_is_no_stream(call):
+    """What is wrong with the stream is not said of the tensors."""
+    with pytest.raises(AttributeError, match="cuda_stream"):
+        if call == "append":
+            ma.monarch_attn_paged_append(**{n: t for n, t in _tensors().items() if n != "k_out"}, stream="s")
+        elif call == "selection":
+            ma.monarch_attn_beam_select(**_selection(), eos=1, stream="s")
+        else:
+            x = dict(k_pages=torch.zeros(3, 2, 8, 64), v_pages=torch.zeros(3, 2, 8, 64), block_table=torch.zeros(6, 4, dtype=torch.int32),
+                     parents=torch.zeros(2, 3, dtype=torch.int32), lens=torch.zeros(6, dtype=torch.int32))
+            ma.monarch_attn_paged_reorder(**{n: _on_device(t)[0] for n, t in x.items()}, stream="s")
