@@ -79,7 +79,7 @@ int append(const void *q, const void *k, const void *v, void *q_out, void *k_pag
     const int rows = rotate_rows(total, Hq + 2 * Hkv, d, dtype);
     MA_TRY(check_grid((total + rows - 1) / rows, 1));
     if (total == 0 || B == 0) return MA_OK;
-    const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
+    const size_t cache = cache_bytes(pages, Hkv, page, d, dtype);
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
                          {"k", k, span_bytes(total, ldk, Hkv * d, dtype)},
                          {"v", v, span_bytes(total, ldv, Hkv * d, dtype)},
@@ -181,7 +181,7 @@ int reorder(void *k_pages, void *v_pages, int32_t *table, const int32_t *parents
     MA_TRY(check_pages(pages, page));
     if (blocks < 0 || blocks > 0x7fffffff) return fail(MA_EINVAL, "blocks must be in 0..2^31 - 1");
     if (B == 0 || K == 1 || blocks == 0) return MA_OK;  // (a beam alone is its own parent)
-    const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
+    const size_t cache = cache_bytes(pages, Hkv, page, d, dtype);
     const Range ins[] = {{"parents", parents, (size_t)(B * K) * 4}, {"lens", lens, (size_t)(B * K) * 4}};
     const Range outs[] = {{"k_pages", k_pages, cache}, {"v_pages", v_pages, cache}, {"block_table", table, (size_t)(B * K * blocks) * 4}};
     MA_TRY(check_ranges(ins, {4, 4}));

@@ -211,7 +211,7 @@ int paged_fwd(const void *q, const void *k_pages, const void *v_pages, void *out
     const int64_t G = Hq / Hkv;
     MA_TRY(check_grid(tiles_of(total, G, B, paged_rows(total, B, G, dtype)), Hkv));
     if (B == 0 || total == 0) return MA_OK;
-    const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
+    const size_t cache = cache_bytes(pages, Hkv, page, d, dtype);
     const Range ins[] = {{"q", q, span_bytes(total, ldq, Hq * d, dtype)},
                          {"k_pages", k_pages, cache},
                          {"v_pages", v_pages, cache},
@@ -429,7 +429,7 @@ int paged_write(const void *k, const void *v, void *k_pages, void *v_pages, cons
     const int64_t per = paged_write_rows(Hkv * d * (int64_t)elem_bytes(dtype) / 16);
     MA_TRY(check_grid((rows + per - 1) / per, 1));
     if (rows == 0 || pages == 0) return MA_OK;
-    const size_t cache = (size_t)pages * Hkv * page * d * elem_bytes(dtype);
+    const size_t cache = cache_bytes(pages, Hkv, page, d, dtype);
     const Range ins[] = {{"k", k, span_bytes(rows, ldk, Hkv * d, dtype)}, {"v", v, span_bytes(rows, ldv, Hkv * d, dtype)},
                          {"slots", slots, (size_t)rows * 8}};
     const Range outs[] = {{"k_pages", k_pages, cache}, {"v_pages", v_pages, cache}};

@@ -107,6 +107,13 @@ inline int check_pages(int64_t pages, int64_t page)
     return MA_OK;
 }
 
+// Bytes of the pages of K or of V, as far as any memory goes.
+inline size_t cache_bytes(int64_t pages, int64_t Hkv, int64_t page, int64_t d, int32_t dtype)
+{
+    const unsigned __int128 n = (unsigned __int128)pages * Hkv * page * d * elem_bytes(dtype);
+    return n >> 62 ? size_t(1) << 62 : (size_t)n;
+}
+
 inline int log2_of(int64_t page)
 {
     int x = 0;
