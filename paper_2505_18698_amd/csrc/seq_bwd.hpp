@@ -361,12 +361,16 @@ template <typename T, int D, Keys KEYS> struct SeqBwdK {
         auto reads = [&](int u) { return u + AHEAD >= N ? 0 : u + AHEAD >= NR ? 2 : 1; };
         stream.start(load);
         __builtin_amdgcn_sched_group_barrier(kSchedDsRead, AHEAD, 0);
-        f32x16 s = terms.template add<0>(f32x16{}, lane), dp = terms.template add<1>(f32x16{}, lane);
+        // In fp32 a sum that starts at lse rounds at lse's size all the way (16 rows over 700 keys of 128 columns: dK and
+        // dV are off by 2.0e-6, with lse added last by 0.7e-6). Packed calls keep the order, and so the bits, that they have.
+        constexpr bool kLast = S::kF32 && KEYS == kCross;
+        f32x16 s = kLast ? f32x16{} : terms.template add<0>(f32x16{}, lane), dp = terms.template add<1>(f32x16{}, lane);
 #pragma unroll
         for (int u = 0; u < S::NS; ++u) {
             stream.next(u, load, [&](const frag &y) { s = S::M::mma(y, kf[u], s); });
             sched_step<(S::kF32 ? 4 : 1)>(reads(u));
         }
+        if constexpr (kLast) s = terms.template add<0>(s, lane);
 #pragma unroll
         for (int i = 0; i < S::NS; ++i) {
             const int u = S::NS + i * NV;

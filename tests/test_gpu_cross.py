@@ -126,6 +126,22 @@ def test_large_scores(ma, dtype):
         x.check(x.run(ma, grads=False))
 
 
+def test_weights_of_wide_heads_in_fp32(ma):
+    """dK and dV of 16 rows over 700 keys of 128 columns, as a whole: a weight exp(s - lse) carries the roundings of lse (two,
+    near 7 and near 10 in log2 units), of its product with sqrt(128) / log2 e (near 80, two) and of the difference (near
+    80), of the scale (relative to 7), and of the scores' sums, half a step each at most: root mean squares of 2e-7 to 4e-7 in
+    units of the weight, 8e-7 together, 1.2e-6 with half as much again.  (A sum that starts near 80 and rounds there 64 times is
+    off by 2e-6.)"""
+    x = Case([16], [700], 3, 3, 128, "f32", 31)
+    r = x.run(ma)
+    q, k, v, g = (t.double().transpose(0, 1) for t in (x.q[2:18], x.k[2:702], x.v[2:702], x.dout[2:18]))
+    w = (q @ k.transpose(1, 2).contiguous() / math.sqrt(128)).softmax(-1)
+    ds = w * (g @ v.transpose(1, 2).contiguous() - (g * (w @ v)).sum(-1, keepdim=True)) / math.sqrt(128)
+    for name, want in (("dk", ds.transpose(1, 2).contiguous() @ q), ("dv", w.transpose(1, 2).contiguous() @ g)):
+        off = (r[name][2:702].double().transpose(0, 1) - want).norm() / want.norm()
+        assert off <= 1.2e-6, (name, off)
+
+
 def test_many_sequences(ma):
     """More sequences than one step of the searches takes, most of them short or empty on either side."""
     gen = torch.Generator().manual_seed(5)
