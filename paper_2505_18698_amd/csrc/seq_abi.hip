@@ -336,8 +336,9 @@ CrossPieces cross_pieces(int64_t B, int64_t total, int64_t total_k, int64_t tile
 {
     const double n = std::max<int64_t>(1, B), walk_k = 4.0 * (double)G * total / n / kSeqBwdKeys, walk_q = 3.0 * total_k / n / kSeqBwdKeys;
     const double share = (walk_k * tiles_k + walk_q * tiles_q) * Hkv / (2.0 * num_cus);
-    auto cut = [&](double walk) { return (int64_t)std::max(1.0, std::min(8.0, std::ceil(walk / std::max(share, 16.0)))); };
-    return CrossPieces{cut(walk_k), cut(walk_q)};
+    // (no sums to cut where a walk's own side has no rows: their join would be a launch of no workgroup)
+    auto cut = [&](double walk, int64_t rows) { return rows == 0 ? 1 : (int64_t)std::max(1.0, std::min(8.0, std::ceil(walk / std::max(share, 16.0)))); };
+    return CrossPieces{cut(walk_k, total_k), cut(walk_q, total)};
 }
 
 int cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest, const void *dout,

@@ -226,6 +226,32 @@ def test_one_side_empty(ma):
     assert x.k.shape[0] == 0 and bool((r["out"] == 0).all()) and bool((r["dq"] == 0).all()) and bool((r["lse"] == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_long_walks_of_an_empty_side(ma, dtype):
+    """Many rows over no keys at all, no rows at all over many keys: the walks are long, but there is nothing to cut."""
+    for lens, Hq, Hkv in (([300], 2, 2), ([512], 4, 1), ([600, 0, 2000], 4, 2), ([5000], 1, 1)):
+        print(lens, Hq, Hkv, dtype, flush=True)
+        x = Case(lens, [0] * len(lens), Hq, Hkv, 64, dtype, 26, first=0, spare=0)
+        r = x.run(ma)
+        assert x.k.shape[0] == 0 and bool((r["out"] == 0).all()) and bool((r["dq"] == 0).all()) and bool((r["lse"] == -math.inf).all())
+        q, k, v = (t.detach().clone().requires_grad_() for t in (x.q, x.k, x.v))
+        ma.exact_cross_attention(q, k, v, x.cu, x.cu_k).backward(x.dout)
+        torch.cuda.synchronize()
+        assert bool((q.grad == 0).all()) and k.grad.shape == x.k.shape and v.grad.shape == x.v.shape
+    for keys in ([5000], [20000, 0, 900]):
+        print(keys, dtype, flush=True)
+        x = Case([0] * len(keys), keys, 2, 1, 64, dtype, 27, first=0, spare=0)
+        r = x.run(ma)
+        assert x.q.shape[0] == 0 and bool((r["dk"] == 0).all()) and bool((r["dv"] == 0).all())
+    for rows, keys in ((3000, 0), (0, 3000)):  # no sequence: all rows cleared
+        q, k = (torch.ones(n, 4, 64, device="cuda", dtype=DTYPES[dtype]) for n in (rows, keys))
+        lse, cu = torch.zeros(4, rows, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        dq, dk, dv = q.clone(), k.clone(), k.clone()
+        ma.monarch_attn_exact_cross_bwd(q, k, k, q, lse, q, dq, dk, dv, cu, cu, clear=True)
+        torch.cuda.synchronize()
+        assert bool((dq == 0).all()) and bool((dk == 0).all()) and bool((dv == 0).all())
+
+
 def test_row_starts_out_of_range(ma):
     """Starts beyond the tensors are clamped: the sequences that are whole are right.  Starts that decrease, which the
     interface excludes, lead to no access out of range, and leave the forward pass of the others right."""
