@@ -275,19 +275,29 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
 // counting the larger ones.  What bounds it: the way to memory and back, once where the lists are short
 // (5.2 us for one request of 4 beams, 6.8 for 64 of 8; one of 16 beams over 25 parts, 32 taken, 23 by events).
 struct BeamEntry {
-    double value;  // the candidate, or -infinity
-    uint32_t at;   // beam V + token; kNoEntry: none
-    __device__ inline bool operator>(const BeamEntry &o) const { return value > o.value || (value == o.value && at < o.at); }
+    double value;    // the candidate, or -infinity
+    uint64_t place;  // beam, logit and token (place_of); of equal values the largest comes first; 0: none
+    __device__ inline bool operator>(const BeamEntry &o) const { return value > o.value || (value == o.value && place > o.place); }
 };
-constexpr uint32_t kNoEntry = 0xffffffffu;
-static_assert((uint64_t)kBeamMax * MONARCH_ATTN_BEAM_MAX_VOCAB < kNoEntry, "candidates have 32-bit numbers");
+// The lowest beam first, of a beam the largest logit (as in a key), of equal logits the lowest token.  Different
+// logits of a beam can be the same value in 64 bits, beside a large score or where they are small beside the log of
+// their sum.  The parts' lists are in the order of the logits, and so are the entries; which of a row's parts
+// an entry came from makes no difference then.
+constexpr int kTokenBits = 19;
+static_assert(MONARCH_ATTN_BEAM_MAX_VOCAB <= 1 << kTokenBits && kBeamMax < 1 << (64 - 32 - kTokenBits), "all three in 64 bits");
+__device__ inline uint64_t place_of(int beam, uint32_t logit, int token)
+{
+    return (uint64_t)(kBeamMax - beam) << (32 + kTokenBits) | (uint64_t)logit << kTokenBits | ((1u << kTokenBits) - 1 - (uint32_t)token);
+}
+__device__ inline int beam_of(uint64_t place) { return kBeamMax - (int)(place >> (32 + kTokenBits)); }
+__device__ inline int token_of(uint64_t place) { return (1 << kTokenBits) - 1 - (int)(place & ((1u << kTokenBits) - 1)); }
 struct BeamHead {
     BeamEntry e;
     int list;
     __device__ inline bool operator>(const BeamHead &o) const { return e > o.e; }
 };
 // The upper half of ordered(value), by which entries are bounded; 0: none.
-__device__ inline uint32_t height(const BeamEntry &e) { return e.at == kNoEntry ? 0 : (uint32_t)(ordered(e.value) >> 32); }
+__device__ inline uint32_t height(const BeamEntry &e) { return e.place == 0 ? 0 : (uint32_t)(ordered(e.value) >> 32); }
 
 // A height that M of the workgroup's values at least reach, from the waves' own ones (1 where no wave has M).
 __device__ inline uint32_t bound_of(uint32_t x, int m, uint32_t *shared)
@@ -345,17 +355,17 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
     // entry i of list l, of that key, or none
     auto entry = [&](int l, int i, uint64_t key) {
         const int k = l / p.parts;
-        BeamEntry e{-(double)INFINITY, kNoEntry};
+        BeamEntry e{-(double)INFINITY, 0};
         if (kind[k] == 0) {
             if (key == 0) return e;
             const double x = score_of[k] + ((double)unordered((uint32_t)(key >> 32)) - lse[k]);
             if (x == x) e.value = x;
-            e.at = (uint32_t)(k * p.V) + (0xffffffffu - (uint32_t)key);
+            e.place = place_of(k, (uint32_t)(key >> 32), (int)(0xffffffffu - (uint32_t)key));
         } else if (l == k * p.parts && i < p.V) {
             const bool first = kind[k] == 1 && i == 0;  // done: the end token, then the others, in front of it and behind it
             const int t = kind[k] == 2 ? i : first ? p.eos : i - 1 < p.eos ? i - 1 : i;
             if (first) e.value = score_of[k];
-            e.at = (uint32_t)(k * p.V + t);
+            e.place = place_of(k, 0, t);
         }
         return e;
     };
@@ -366,7 +376,7 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const int x = tid + 256 * j;
-            mine[j] = BeamEntry{-(double)INFINITY, kNoEntry};
+            mine[j] = BeamEntry{-(double)INFINITY, 0};
             if (256 * j < some && x < some) mine[j] = entry(list_of(x), number_of(x), key[j]);
             top = max(top, height(mine[j]));
         }
@@ -402,7 +412,7 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
         const BeamEntry e = list[i];
         const int rank = larger_ones(list, n, e);
         if (rank >= p.M) continue;
-        const int k = (int)(e.at / (uint32_t)p.V), t = (int)(e.at % (uint32_t)p.V);
+        const int k = beam_of(e.place), t = token_of(e.place);
         const int64_t to = (int64_t)blockIdx.x * p.M + rank;
         p.scores_out[to] = (float)e.value;
         p.tokens[to] = t, p.parents[to] = k;

@@ -213,6 +213,32 @@ def test_scores_of_any_size(ma):
         assert int(parents) == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [40, 20000, 200003])
+def test_order_within_a_beam(ma, V, dtype):
+    """The larger logit comes first, then the lower token, also where the values of different logits are the same in 64 bits:
+    under large scores, and of logits that are small beside the log of their sum.  Between beams the lower one."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    x = torch.randn(1, 3, V, generator=gen, device="cuda")
+    tiny = 2.0 ** -24 if dtype == "f16" else 1e-20  # (fp16 has no smaller ones: a few different values)
+    for scale, sizes in ((1.0, (-1e9, 1e6, -1e30, 1e30, 3e38, -3e38)), (tiny, (0.0, -1e30))):
+        y = (x * scale).to(DTYPES[dtype])
+        order = y[0].double().sort(dim=1, descending=True, stable=True).indices
+        for size in sizes:
+            for M in (1, 5, 32):
+                for used in ([2], [0], [1, 2]):
+                    if len(used) > 1 and scale == 1.0 and abs(size) < 1e29:
+                        continue  # (values of two beams that differ)
+                    s = torch.full((1, 3), -math.inf, device="cuda")
+                    s[0, used] = size
+                    out, tokens, parents, _ = _select(ma, y, s, M)
+                    if scale == 1.0 or len(used) == 1 or dtype != "f16":  # (fp16: sums of two beams that may differ)
+                        assert bool((parents == used[0]).all()), (size, M, used)
+                        assert tokens[0].tolist() == order[used[0], :M].tolist(), (size, M, used)
+                    want = _candidates(y, s, None, -1)[0, parents[0].long(), tokens[0].long()]
+                    assert bool(((out[0] - want).abs() <= CLOSE + want.abs() * 2.0 ** -24).all()), (size, M, used)
+
+
 def test_same_bits_again_and_on_two_streams(ma):
     gen = torch.Generator(device="cuda").manual_seed(6)
     x = [(torch.randn(4, 4, 50001, generator=gen, device="cuda") * 3).bfloat16() for _ in range(2)]
