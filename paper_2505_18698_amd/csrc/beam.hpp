@@ -65,6 +65,9 @@ template <typename F> __device__ inline float over_wave(float x, F &&f)
     return x;
 }
 
+// exp(x - base) of logits, base no less than x; 0 of -infinity, whatever base is.
+__device__ inline float exp_behind(float x, float base) { return x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x - base) * kLog2e); }
+
 // A part of a row a workgroup, in chunks of 8192 tokens that are held in registers while the next one
 // arrives: its largest logit, its sum of exponentials and its M best, in order.
 //
@@ -81,6 +84,7 @@ template <typename F> __device__ inline float over_wave(float x, F &&f)
 template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSelect p)
 {
     constexpr int E = 32, VE = 16 / (int)sizeof(T), NV = E / VE, kRoom = 1024, kMany = 256;
+    constexpr float kNear = 0x1p20f;  // of a reference below it the rounding is a sixteenth at most
     __shared__ __attribute__((aligned(16))) uint64_t list[kRoom + 8], best[kBeamMax];
     __shared__ uint32_t bounds[4];
     __shared__ float maxima[4], sums[4];
@@ -117,7 +121,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
     };
     fetch(0);
     if (tid == 0) count = 0;
-    // of this thread's elements: the largest in units of log 2 (NaN stays), and the sum relative to it
+    // of this thread's elements: the largest (NaN stays), and the sum of exponentials relative to it
     float most = -INFINITY, sum = 0.f;
     int kept = 0, listed = 0;           // entries of the list that are the best so far, in order, and all
     float bound = -INFINITY;            // with kept = M: the logit of the last of them
@@ -148,17 +152,28 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
             for (int e = 1; e < VE; ++e) tops[i] = max_nan(tops[i], x[i * VE + e]);
             top = max_nan(top, tops[i]);
         }
-        const float now = max_nan(most, top * kLog2e), base = fabsf(now) < INFINITY ? now : 0.f;
-        float a = __builtin_amdgcn_exp2f(__builtin_fmaf(y, kLog2e, -base)), b = 0.f;
+        const float now = max_nan(most, top), base = fabsf(now) < INFINITY ? now : 0.f;
+        float a = 0.f, b = 0.f;
+        auto add_up = [&](auto &&exp_of) {
+            a = exp_of(y);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (some[i])
+            for (int i = 0; i < NV; ++i)
+                if (some[i])
 #pragma unroll
-                for (int e = 0; e < VE; e += 2) {
-                    a += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i * VE + e], kLog2e, -base));
-                    b += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i * VE + e + 1], kLog2e, -base));
-                }
-        sum = sum * (most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most - base)) + (a + b);
+                    for (int e = 0; e < VE; e += 2) a += exp_of(x[i * VE + e]), b += exp_of(x[i * VE + e + 1]);
+        };
+        // exp(x - base): one instruction in front of the exponential, from the reference in units of log 2, which is
+        // rounded; what that took is put right behind the sum.  Of large ones it would be too much for an exponential
+        // (all of a thread's tokens masked with -1e10: 2^440), and the largest have no such reference.
+        if (__all(fabsf(base) < kNear)) {
+            const float scaled = base * kLog2e;
+            add_up([&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, kLog2e, -scaled)); });
+            const float by = __builtin_amdgcn_exp2f(-__builtin_fmaf(base, kLog2e, -scaled));
+            a *= by, b *= by;
+        } else {
+            add_up([&](float z) { return exp_behind(z, base); });
+        }
+        sum = sum * exp_behind(most, base) + (a + b);
         most = now;
 
         float low = -INFINITY;  // bound of the first chunk's candidates
@@ -254,7 +269,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
 
     const float wave_most = over_wave(most, [](float a, float b) { return max_nan(a, b); });
     const float base = fabsf(wave_most) < INFINITY ? wave_most : 0.f;
-    sum = over_wave(sum * (most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most - base)), [](float a, float b) { return a + b; });
+    sum = over_wave(sum * exp_behind(most, base), [](float a, float b) { return a + b; });
     if (lane == 0) maxima[wave] = wave_most, sums[wave] = sum;
     __syncthreads();
     // (a row of which a logit is NaN or +infinity has no candidates: its keys are not read)
@@ -263,7 +278,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
     if (tid == 64) {
         float m = maxima[0], s = 0.f;
         for (int i = 1; i < 4; ++i) m = max_nan(m, maxima[i]);
-        for (int i = 0; i < 4; ++i) s += sums[i] * (maxima[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(maxima[i] - m));
+        for (int i = 0; i < 4; ++i) s += sums[i] * exp_behind(maxima[i], m);
         p.part_max[blockIdx.x] = m, p.part_sum[blockIdx.x] = s;
     }
 }
@@ -315,7 +330,8 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
     extern __shared__ __attribute__((aligned(16))) char lds[];
     BeamHead *heads = reinterpret_cast<BeamHead *>(lds);  // of the lists, where there are many
     __shared__ BeamEntry list[kAhead + 8];
-    __shared__ double lse[kBeamMax], score_of[kBeamMax];
+    // the log of a beam's sum relative to its largest logit (beside which, of 1e20, 64 bits would not hold it), that logit, its score
+    __shared__ double lse[kBeamMax], largest[kBeamMax], score_of[kBeamMax];
     __shared__ int kind[kBeamMax];  // of a beam: 0 candidates by its logits, 1 done, 2 all of them -infinity
     __shared__ int open[kBeamMax];  // the lists that count
     __shared__ uint32_t bounds[2][4];
@@ -341,14 +357,15 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
         for (int i = i0 + width; i < p.parts; i += width) most = max_nan(most, maxima[i]);
         for (int s = 1; s < width; s <<= 1) most = max_nan(most, __shfl_xor(most, s));
         const bool fine = fabsf(most) < INFINITY;
-        double sum = s0 * exp2((double)m0 - (double)most);
-        for (int i = i0 + width; i < p.parts; i += width) sum += (double)sums[i] * exp2((double)maxima[i] - (double)most);
+        auto weight = [&](float m) { return exp2(((double)m - (double)most) * (double)kLog2e); };
+        double sum = s0 * weight(m0);
+        for (int i = i0 + width; i < p.parts; i += width) sum += (double)sums[i] * weight(maxima[i]);
         for (int s = 1; s < width; s <<= 1) sum += __shfl_xor(sum, s);
         if (i0 == 0) {
             kind[k] = dead ? 2 : ended ? 1 : fine ? 0 : 2;
             // (in the unit that the exponentials had, kLog2e in 32 bits: off by 2e-8 of the row's entropy)
-            lse[k] = ((double)most + log2(sum)) / (double)kLog2e;
-            score_of[k] = score;
+            lse[k] = log2(sum) / (double)kLog2e;
+            largest[k] = most, score_of[k] = score;
         }
     }
     __syncthreads();
@@ -358,7 +375,7 @@ static __global__ __launch_bounds__(256) void beam_join(BeamSelect p)
         BeamEntry e{-(double)INFINITY, 0};
         if (kind[k] == 0) {
             if (key == 0) return e;
-            const double x = score_of[k] + ((double)unordered((uint32_t)(key >> 32)) - lse[k]);
+            const double x = score_of[k] + (((double)unordered((uint32_t)(key >> 32)) - largest[k]) - lse[k]);
             if (x == x) e.value = x;
             e.place = place_of(k, (uint32_t)(key >> 32), (int)(0xffffffffu - (uint32_t)key));
         } else if (l == k * p.parts && i < p.V) {

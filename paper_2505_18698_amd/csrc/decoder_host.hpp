@@ -33,7 +33,7 @@ struct BeamSelect {
     int B, K, V, M, eos;
     int parts, part_vectors;  // parts of a row, and 16-byte vectors a part
     uint64_t *keys;         // [B K, parts, M] the best of every part, as keys
-    float *part_max, *part_sum;  // [B K, parts] its largest logit in units of log 2 and the sum of exp(logit - largest)
+    float *part_max, *part_sum;  // [B K, parts] its largest logit and the sum of exp(logit - largest)
 };
 
 struct PagedReorder {

@@ -239,6 +239,65 @@ def test_order_within_a_beam(ma, V, dtype):
                     assert bool(((out[0] - want).abs() <= CLOSE + want.abs() * 2.0 ** -24).all()), (size, M, used)
 
 
+def _check_far(got, logits, scores, M):
+    """As _check, for finite logits of any size: they count relative to the largest of their row, from which 64 bits
+    may round them alike; then within a beam the logits decide."""
+    out, tokens, parents, _ = got
+    B, K, V = logits.shape
+    x = logits.double() - logits.double().amax(-1, keepdim=True)
+    cand = scores.double()[..., None] + (x - x.exp().sum(-1, keepdim=True).log())
+    at = parents.long() * V + tokens.long()
+    assert bool(((parents >= 0) & (parents < K) & (tokens >= 0) & (tokens < V)).all())
+    mine, best = cand.flatten(1).gather(1, at), cand.flatten(1).sort(dim=1, descending=True).values[:, :M]
+    assert bool(((mine - best).abs() <= 2 * CLOSE + best.abs() * 2.0 ** -51).all())
+    assert bool(((out.double() - mine).abs() <= CLOSE + mine.abs() * 2.0 ** -24).all())
+    for b in range(B):
+        assert len(set(at[b].tolist())) == M
+        for k in range(K):
+            mine_k = tokens[b][parents[b] == k].tolist()
+            assert mine_k == logits[b, k].double().sort(descending=True, stable=True).indices[: len(mine_k)].tolist()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("V", [7, 9001, 100003])
+def test_logits_of_any_size(ma, V, dtype):
+    """Rows all of whose logits are the same finite value, the lowest and the largest of the type among them; and masks of
+    such values beside ordinary logits, few or nearly all of them."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    dt = DTYPES[dtype]
+    most = torch.finfo(dt).max
+    scores = torch.tensor([[-0.5, -0.25, -1.0]], device="cuda")
+    M = min(8, V)
+    for size in (1e3, 3e4, 1e6, 1e9, 3e9, 1e10, 7e10, 1e20, 1e30, 3e37, 1e38, 2.3e38, 2.4e38, most):
+        if size > most:
+            continue
+        for value in (-size, size):
+            print(V, dtype, value, flush=True)
+            x = torch.full((1, 3, V), value, device="cuda", dtype=dt)
+            _check_far(_select(ma, x, scores, M), x, scores, M)  # all of one size
+            y = torch.randn(1, 3, V, generator=gen, device="cuda").to(dt)
+            for share in (0.001, 0.5, 0.999):
+                some = torch.rand(1, 3, V, generator=gen, device="cuda") < share
+                some[:, :, V // 2] = False
+                z = y.masked_fill(some, value)
+                _check_far(_select(ma, z, scores, M), z, scores, M)
+                z[0, 1] = value
+                _check_far(_select(ma, z, scores, M), z, scores, M)
+            if V > 8192:  # the large ones in an early or a late chunk only
+                for part in (slice(0, 8000), slice(V - 500, V)):
+                    z = y.clone()
+                    z[:, :, part] = value
+                    _check_far(_select(ma, z, scores, M), z, scores, M)
+    wide = torch.cat([torch.full((1, 3, V), f * most, device="cuda", dtype=dt) for f in (-1.0, 1.0)], 2)  # both ends of the range
+    _check_far(_select(ma, wide, scores, M), wide, scores, M)
+    many = (torch.randn(128, 4, V, generator=gen, device="cuda") * 3).to(dt).masked_fill(torch.rand(128, 4, V, generator=gen, device="cuda") < 0.98, -1e4)
+    if dtype != "f16":
+        many = many.masked_fill(many == many.min(), -7e10)
+    s = torch.zeros(128, 4, device="cuda")
+    got = _select(ma, many, s, M)
+    _check_far(tuple(t if t is None else t[:2] for t in got), many[:2], s[:2], M)
+
+
 def test_same_bits_again_and_on_two_streams(ma):
     gen = torch.Generator(device="cuda").manual_seed(6)
     x = [(torch.randn(4, 4, 50001, generator=gen, device="cuda") * 3).bfloat16() for _ in range(2)]
