@@ -377,7 +377,11 @@ int monarch_attn_set_path(int32_t path);
  * 3 last L half-step with the Monarch product and the store of O,
  * 4 the one-workgroup-per-head kernel, 5 the sum of the objective shares,
  * 6 exact attention, 7 an L half-step of the gradient, 8 an R half-step of
- * the gradient, 9 the one-workgroup-per-group-of-classes kernel); it returns
+ * the gradient, 9 the one-workgroup-per-group-of-classes kernel, 10 attention
+ * over sequences, packed, paged or cross, 11 the join of its splits, 12 the row
+ * statistics of its gradient, 13 the gradient, 14 the join of its pieces, 15 the
+ * paged plan, 16 the paged write, 17 rotation and append, 18 the parts of a beam
+ * selection, 19 their join, 20 the paged reorder); it returns
  * the number of launches of that call, or -1 on error.
  */
 int monarch_attn_timing_enable(int32_t flag);
@@ -454,8 +458,8 @@ int monarch_attn_exact_packed_fwd(const void *q, const void *k, const void *v, v
  * sequence's gradient depends on the values of another.  Values of a sequence
  * that are not finite can reach all gradients of that sequence.
  * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a row and key head); and where there are few key tiles
- * for the device (fewer than about 2000 over all key heads) up to three fp32 copies of dk and dv,
- * which a further launch adds up.
+ * for the device (fewer than about 2000 over all key heads) up to three fp32 copies of dk and of dv, in heads of d
+ * rounded up to 64, 96 or 128 columns, which a further launch adds up.
  */
 int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse,
                                   const void *rest, const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_seqlens,
@@ -477,8 +481,11 @@ int monarch_attn_exact_packed_bwd(const void *q, const void *k, const void *v, c
  *                keys (clamped to 0..their number), as in a padded batch.  The others are not read.
  * Every row sees all keys of its sequence; rows of a sequence without keys get a
  * zero output and lse -infinity.  The lengths of queries and keys are independent.
- * Workspace: as in monarch_attn_exact_paged_fwd, where the mean number of keys a sequence (of a padded
- * batch half the width) is more than that given there.
+ * Workspace: as in monarch_attn_exact_paged_fwd, with the mean number of keys, total_k / B (of a padded batch half
+ * of it), in place of the table's tokens.  Calls of more than 32 packed rows a sequence on average are split from
+ * a quarter of that on, where they have few row tiles for the device.  The host does not know the lengths: few rows over
+ * one long context among many short ones run whole, as the mean says (4 rows over 20000 keys beside 31 requests of 4
+ * over 64, 12 heads of 64 in bf16: 115 us; in a call of its own the long one takes 22).
  */
 int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, void *out, float *lse, void *rest,
                                  const int32_t *cu_q, const int32_t *cu_k, const int32_t *k_lens, int64_t B, int64_t total,
@@ -492,7 +499,8 @@ int monarch_attn_exact_cross_fwd(const void *q, const void *k, const void *v, vo
  * dk and dv are zero in the rows behind k_lens[i] of a sequence, and of sequences without
  * queries.  Rows of no sequence (by cu_q, by cu_k) are left, or with clear written as zero.
  * Workspace: 8 bytes a row and query head (fp16: 12, and 4 a key row and key head), and where
- * there are few walks for the device up to eight fp32 copies of dk and dv, or of dq.
+ * there are few walks for the device up to eight fp32 copies of dk and of dv, and up to eight of dq, in
+ * heads of d rounded up to 64, 96 or 128 columns.
  */
 int monarch_attn_exact_cross_bwd(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *rest,
                                  const void *dout, void *dq, void *dk, void *dv, const int32_t *cu_q, const int32_t *cu_k,

@@ -78,9 +78,9 @@ __device__ inline float exp_behind(float x, float base) { return x == -INFINITY 
 // over keys finds a bound that few enough reach.
 //
 // What bounds it: about 12 vector instructions a token, of which the exponential takes four issues, beside 2
-// bytes. 64 requests of 8 beams over 50001 tokens in bf16 (51 MB, 16 taken): 19.4 us, vector instructions
-// issue in 44 % of the time; by events, 14 of 21 us are the pass over the logits, 3 the first chunk's
-// candidates, 4 the later ones'. 128000 tokens: 34 us by events. 4 beams over 32000 in fp32: 6.4 us, latency.
+// bytes. 64 requests of 8 beams over 50001 tokens in bf16 (51 MB, 16 taken): 19.6 us, vector instructions
+// issue in 45 % of the time (28.4 us for 26.7 of the whole call where tokens masked with -1e9 or less fill threads); by events, 14 of 21 us are the pass over the logits, 3 the first chunk's
+// candidates, 4 the later ones'. 128000 tokens: 34 us by events. 4 beams over 32000 in fp32: 6.6 us, latency.
 template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSelect p)
 {
     constexpr int E = 32, VE = 16 / (int)sizeof(T), NV = E / VE, kRoom = 1024, kMany = 256;
@@ -288,7 +288,7 @@ template <typename T> __global__ __launch_bounds__(256) void beam_parts(BeamSele
 // lists.  All of these are in order: of more than 1024 entries, only the M lists of the best first
 // ones count.  A bound as in beam_parts leaves few entries, each of which finds its place by
 // counting the larger ones.  What bounds it: the way to memory and back, once where the lists are short
-// (5.2 us for one request of 4 beams, 6.8 for 64 of 8; one of 16 beams over 25 parts, 32 taken, 23 by events).
+// (5.1 us for one request of 4 beams, 6.7 for 64 of 8; one of 16 beams over 25 parts, 32 taken, 23 by events).
 struct BeamEntry {
     double value;    // the candidate, or -infinity
     uint64_t place;  // beam, logit and token (place_of); of equal values the largest comes first; 0: none
