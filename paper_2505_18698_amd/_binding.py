@@ -1040,6 +1040,8 @@ def monarch_attn_beam_select(logits, scores, scores_out, tokens, parents, done=N
     rt = _TORCH or _torch()
     if stream is not None:
         stream = _stream(logits, stream)
+    if not -0x80000000 <= eos <= 0x7fffffff:  # (ctypes would take its lower 32 bits)
+        raise ValueError(f"eos must be a token (got {eos})")
     try:  # (one pass without names, as above)
         (B, K, V), index = logits.shape, logits.get_device()
         M = tokens.shape[1]

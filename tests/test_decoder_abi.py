@@ -165,6 +165,13 @@ def test_binding_of_the_selection(change, message):
         ma.monarch_attn_beam_select(**_selection(**change), eos=1)
 
 
+@pytest.mark.parametrize("eos", [1 << 32, (1 << 32) + 1, -(1 << 32) + 1, 1 << 31, 1 << 64])
+def test_eos_beyond_32_bits(eos):
+    """No token, also where its lower bits are one."""
+    with pytest.raises(ValueError, match="eos must be a token"):
+        ma.monarch_attn_beam_select(**_selection(), eos=eos)
+
+
 @pytest.mark.parametrize("change,message", [
     (dict(parents=torch.zeros(6, dtype=torch.int32)), "parents must have 2"), (dict(parents=torch.zeros(2, 3)), "parents must be"),
     (dict(block_table=torch.zeros(5, 4, dtype=torch.int32)), "block_table must be"), (dict(lens=torch.zeros(2, dtype=torch.int32)), "lens must be"),
