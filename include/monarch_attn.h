@@ -644,7 +644,7 @@ int monarch_attn_paged_append(const void *q, const void *k, const void *v, void 
  * the M largest in descending order; equal ones by the lowest k V + t.
  *
  * logits    : [B, K, V], rows ld elements apart (any ld >= V; aligned to their element only).
- *             -infinity: a token that is not allowed.
+ *             -infinity: a token that is not allowed.  Finite logits may have any size (masks of -1e30 among them).
  * scores    : [B, K] device floats, the beams' sums so far, finite, or -infinity: a beam that is not in
  *             use (as all but the first are at the start).
  * done      : NULL, or [B, K] bytes: a beam that has ended offers the token eos, at its own
